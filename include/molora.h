@@ -58,6 +58,9 @@ typedef enum { MOLORA_F32 = 0, MOLORA_BF16 = 1 } molora_dtype_t;
 #define MOLORA_DEV_ID_OUT_OF_RANGE 0x1u /* some token id lies in no vocabulary range: routed to -1          */
 #define MOLORA_DEV_BAD_ROUTE 0x2u       /* some routing value lies outside [-1, C): treated as unrouted       */
 #define MOLORA_DEV_TIMEOUT 0x4u         /* a bounded device-side wait gave up (results of that call invalid)   */
+#define MOLORA_DEV_BAD_SEQUENCE 0x8u    /* a sequence's page lies outside the pool or its table, or its lengths contradict each other: those tokens
+                                           are left out (not written, not attended to)                             */
+#define MOLORA_DEV_BAD_DRAFT 0x10u      /* a drafted token lies outside the vocabulary (refused), or a distribution has no mass (token -1) */
 
 #define MOLORA_MAX_ADAPTERS 256
 #define MOLORA_MAX_PROJECTIONS 8
@@ -358,6 +361,97 @@ molora_status_t molora_hotset_commit(molora_hotset_t *h, int32_t slot, void *mai
 molora_status_t molora_route_hotset(const int32_t *ids, const int32_t *adapter_id, int64_t N, const int32_t *breaks,
                                     int32_t M, const int32_t *slot_table_dev, int32_t n_catalog, int32_t S,
                                     int32_t *r_out, uint32_t *dev_status, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * The paged 8-bit key / value cache of the layers whose projections this library adapts: what stands between the
+ * adapted q / k / v projections of a step and its adapted output projection.  (The paper serves through an engine that
+ * has these; it defines none of them.)
+ *   codes   k, v: device e4m3 [n_pages][kv_heads][page][dim], dense, 16-byte aligned
+ *   scales  k_scale, v_scale: device fp32 [n_pages][kv_heads], one for each BLOCK of `page` tokens of one head:
+ *           value = code * scale.  molora_kv_append writes powers of two; molora_kv_attend takes any positive finite scale
+ *           (those of v are read as if clamped to [2^-100, 2^100]).
+ * page is 16, 32, 64 or 128 tokens, dim 64 or 128, kv_heads >= 1.
+ * The sequences of a step:
+ *   page_table  device int32 [B][max_pages], row pitch ld_table: token p of sequence b is row p % page of page
+ *               page_table[b][p / page]; entries behind a sequence's last token are not read
+ *   cu_tokens   device int32 [B + 1], non-decreasing from 0: sequence b's NEW tokens are rows cu_tokens[b] .. cu_tokens[b+1] - 1
+ *               of q, k, v; rows from cu_tokens[B] on belong to no sequence and are left as they are
+ *   kv_lens     device int32 [B]: tokens of sequence b INCLUDING the new ones, so that its j-th of n new tokens stands at
+ *               position kv_lens[b] - n + j
+ * Pages outside [0, n_pages), lengths beyond max_pages * page and positions below 0 never fault: those tokens are left out
+ * and MOLORA_DEV_BAD_SEQUENCE is OR-ed into dev_status. */
+typedef struct {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int32_t n_pages, kv_heads, page, dim;
+} molora_kv_cache_t;
+typedef struct {
+    const int32_t *page_table;
+    int64_t ld_table;
+    const int32_t *cu_tokens;
+    const int32_t *kv_lens;
+    int32_t B, max_pages;
+} molora_sequences_t;
+
+/* Position rotation of q and k, and k and v into the cache, in one launch.  With p the position of a token and
+ * w_i = p * inv_freq[i] (product and reduction in 64 bits), i < rotary / 2, the pair (a, b) of a head's elements
+ * (i, i + rotary / 2) -- or (2i, 2i + 1) if interleaved -- becomes
+ *     (a cos w_i - b sin w_i, b cos w_i + a sin w_i);
+ * elements from `rotary` on, and all of v, stay.  A block's scale becomes the smallest power of two s with
+ * amax <= 448 s over its NEW values (the finite ones; at least 2^-64, at most 2^64), but never less than what a block that
+ * older tokens stand in has already; where it grows, their codes are divided by the growth (exact but for values that become subnormal).
+ * New codes are rounded to nearest even; infinities saturate, NaN stays NaN.
+ * k, v    device [N][kv_heads * dim] of type dt, pitches ldk, ldv (multiples of 8 elements), 16-byte aligned
+ * q       device [N][heads * dim], pitch ldq, or NULL (heads then 0); q_out the same with pitch ldqo, may be q itself but may
+ *         not overlap it otherwise
+ * inv_freq  device fp32 [rotary / 2], or NULL if rotary is 0; rotary a multiple of 16, at most dim
+ * The pages that a call writes belong to one sequence each (shared ones are copied by the caller first); tokens of a
+ * block behind a sequence's new length (drafts that were refused) are overwritten by the next append and count for nothing
+ * else than the scale, which never shrinks while the block is in use. */
+molora_status_t molora_kv_append(const molora_kv_cache_t *cache, const molora_sequences_t *seqs, molora_dtype_t dt, int64_t N,
+                                 const void *k, int64_t ldk, const void *v, int64_t ldv, const void *q, int64_t ldq,
+                                 void *q_out, int64_t ldqo, int32_t heads, const float *inv_freq, int32_t rotary,
+                                 int32_t interleaved, uint32_t *dev_status, void *stream);
+
+/* Attention of the step's queries over the cache (after molora_kv_append).  For every new token at position p and every
+ * query head h, reading key / value head h / (heads / kv_heads):
+ *     out = sum_j softmax_j(scale * q . K_j) V_j   over j < kv_lens, j <= p if causal, j > p - window if window > 0
+ * Rows that see no token get out = 0 and lse = -infinity.
+ * q       device [N][heads * dim] of type dt, pitch ldq; out the same, pitch ldo; heads a multiple of kv_heads
+ * lse     device fp32 [N][heads] or NULL: natural logarithm of the softmax's sum
+ * window  0, or (causal only) the number of newest tokens that a row sees, itself included
+ * max_tokens  the most new tokens that a sequence of this call has, as far as the caller knows (N if it does not); the
+ *         choice of kernel goes by it, results do not depend on it
+ * ws, ws_bytes  device scratch of at least molora_kv_attend_workspace_bytes(...) bytes, 256-byte aligned, need not be cleared;
+ *         calls that share it must not overlap on the GPU
+ * Scores and sums are fp32, q and the codes enter the tensor cores exactly (fp16 with the rows of q scaled by powers of
+ * two; fp32 q as two terms, 22 bits), weights rounded to fp16 (two terms for fp32), one rounding to dt at the end.
+ * Tokens that a row does not see leave no trace in it, whatever their codes; a NaN among the codes of a token makes the rows NaN that do
+ * see it. */
+size_t molora_kv_attend_workspace_bytes(molora_dtype_t dt, int32_t heads, int32_t kv_heads, int32_t dim, int64_t max_tokens);
+molora_status_t molora_kv_attend(const molora_kv_cache_t *cache, const molora_sequences_t *seqs, molora_dtype_t dt, int64_t N,
+                                 const void *q, int64_t ldq, void *out, int64_t ldo, float *lse, int32_t heads, float scale,
+                                 int32_t causal, int32_t window, int64_t max_tokens, void *ws, size_t ws_bytes,
+                                 uint32_t *dev_status, void *stream);
+
+/* Verification of drafted tokens: how many of the n drafted tokens x_0 .. x_{n-1} of a sequence stand, and the token after
+ * them, from the target's distributions p_0 .. p_n, the drafter's q_0 .. q_{n-1} and given random numbers u in [0, 1):
+ *     token i is accepted while  u_i q_i(x_i) < p_i(x_i);
+ *     at the first refusal, at i, one token is drawn from max(p_i - q_i, 0), after n accepted ones from p_n (also where
+ *     max(p - q, 0) has no mass): the lowest t with sum_{s <= t} > u_S * total.
+ * Distributions need not be normalised.  Comparisons, differences and sums are in 64 bits.
+ * target  device [B][S + 1][V] of type dt, pitches target_ld_seq, target_ld (elements) of a sequence and of a row
+ * draft   device [B][S][V] likewise, or NULL: the drafted tokens are certain (q_i(x_i) = 1, 0 elsewhere)
+ * drafted device int32 [B][S];  n_drafted  device int32 [B], each in [0, S] (clamped), or NULL: S for all
+ * uniform device fp32 [B][S + 1]: u_0 .. u_{S-1} for the drafts, u_S for the drawn token
+ * tokens  device int32 [B][S + 1]: the accepted tokens, the drawn one, then -1;  accepted  device int32 [B]
+ * 0 <= S <= MOLORA_MAX_DRAFTS, 1 <= V < 2^30.  A drafted token outside [0, V) is refused, a distribution without mass gives
+ * token -1; both set MOLORA_DEV_BAD_DRAFT. */
+#define MOLORA_MAX_DRAFTS 31
+molora_status_t molora_verify_drafts(const void *target, int64_t target_ld_seq, int64_t target_ld, const void *draft,
+                                     int64_t draft_ld_seq, int64_t draft_ld, molora_dtype_t dt, const int32_t *drafted,
+                                     const int32_t *n_drafted, const float *uniform, int32_t B, int32_t S, int32_t V,
+                                     int32_t *tokens, int32_t *accepted, uint32_t *dev_status, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Failure-detection self-test.  Every device-side wait of the tensor-core apply kernel (on an mbarrier that a

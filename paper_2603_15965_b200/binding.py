@@ -51,6 +51,16 @@ EVENT_DONE_FN = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_
 EVENT_DESTROY_FN = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_void_p)
 
 
+class _KvCacheC(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("page", ctypes.c_int32), ("dim", ctypes.c_int32)]
+
+
+class _SequencesC(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("ld_table", ctypes.c_int64), ("cu_tokens", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p),
+                ("B", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
 class _HotsetBackendC(ctypes.Structure):
     _fields_ = [("copy_h2d", COPY_FN), ("event_record", EVENT_RECORD_FN), ("event_done", EVENT_DONE_FN),
                 ("event_destroy", EVENT_DESTROY_FN), ("user", ctypes.c_void_p)]
@@ -129,6 +139,14 @@ def load_library():
                                                     i32]
     lib.molora_forward_host.argtypes = [ctypes.c_int, vp, vp, i32, vp, vp, i32, ctypes.POINTER(_HostProjC), i32,
                                         ctypes.c_int, i64, i32, vp, sz, vp, vp]
+    cache, seqs = ctypes.POINTER(_KvCacheC), ctypes.POINTER(_SequencesC)
+    lib.molora_kv_append.argtypes = [cache, seqs, ctypes.c_int, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i32, i32, vp, vp]
+    lib.molora_kv_attend_workspace_bytes.restype = sz
+    lib.molora_kv_attend_workspace_bytes.argtypes = [ctypes.c_int, i32, i32, i32, i64]
+    lib.molora_kv_attend.argtypes = [cache, seqs, ctypes.c_int, i64, vp, i64, vp, i64, vp, i32, f32, i32, i32, i64, vp, sz, vp, vp]
+    lib.molora_verify_drafts.argtypes = [vp, i64, i64, vp, i64, i64, ctypes.c_int, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]
+    for name in ("molora_kv_append", "molora_kv_attend", "molora_verify_drafts"):
+        getattr(lib, name).restype = ctypes.c_int
     lib.molora_hotset_create.argtypes = [i32, i32, i32, vp, ctypes.POINTER(_HotsetBackendC), ctypes.POINTER(vp)]
     lib.molora_hotset_destroy.argtypes = [vp]
     lib.molora_hotset_destroy.restype = None
@@ -492,6 +510,52 @@ def molora_forward_host(router: int, projs, arena: torch.Tensor, route_src: Opti
     _check("molora_forward_host", lib.molora_forward_host(
         router, _ptr(route_src), _ptr(breaks), M, _ptr(G), _ptr(bias), gate_proj, arr, len(arr), dt, N, C,
         _ptr(arena), arena.numel() * arena.element_size(), _ptr(dev_status), _stream(stream)))
+
+
+# ----------------------------------------------------------------------------- paged 8-bit cache, draft verification
+@dataclass
+class KVCache:
+    """The paged cache of one layer: e4m3 codes (torch.float8_e4m3fn, or uint8) [pages, kv_heads, page, dim] and fp32 scales
+    [pages, kv_heads], one for each page of each head; value = code * scale.  page 16, 32, 64 or 128; dim 64 or 128."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def molora_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, page_table: torch.Tensor, cu_tokens: torch.Tensor,
+                     kv_lens: torch.Tensor, q: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None,
+                     interleaved: bool = False, q_out: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                     stream=None) -> Optional[torch.Tensor]:
+    """Rotate q and k by their positions (``inv_freq`` fp32 [rotary / 2]; None: no rotation) and write k and v into the cache.
+    k, v [tokens, kv_heads, dim], q [tokens, heads, dim], tokens of any pitch; kv_lens [B] counts the new tokens,
+    which are the rows cu_tokens[b] .. cu_tokens[b + 1].  Returns the rotated q (``q_out``, which may be q), None without q."""
+    return (_marshal or _load_marshal()).kv_append(k, v, cache, page_table, cu_tokens, kv_lens, q, inv_freq, interleaved, q_out, dev_status, stream)
+
+
+def molora_kv_attend_workspace_bytes(dt: int, heads: int, kv_heads: int, dim: int, max_tokens: int) -> int:
+    return int(load_library().molora_kv_attend_workspace_bytes(dt, heads, kv_heads, dim, max_tokens))
+
+
+def molora_kv_attend(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, cu_tokens: torch.Tensor, kv_lens: torch.Tensor,
+                     scale: Optional[float] = None, causal: bool = True, window: int = 0, max_tokens: Optional[int] = None,
+                     out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                     dev_status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of the new tokens' queries [tokens, heads, dim] over the cache; ``scale`` None: dim ** -0.5; ``window``: newest tokens
+    that a row sees (0: all); ``max_tokens``: the most new tokens of a sequence, where known (the kernel is chosen by it).
+    Rows that see nothing are 0, their ``lse`` (fp32 [tokens, heads], natural logarithm) -inf.  ``out`` must not overlap q."""
+    return (_marshal or _load_marshal()).kv_attend(q, cache, page_table, cu_tokens, kv_lens, scale, causal, window, max_tokens, out, lse, ws, dev_status,
+                                                   stream)
+
+
+def molora_verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], drafted: torch.Tensor, uniform: torch.Tensor,
+                         n_drafted: Optional[torch.Tensor] = None, tokens: Optional[torch.Tensor] = None,
+                         accepted: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                         stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Accept drafted tokens [B, S] against the target's probabilities [B, S + 1, V] and the drafter's [B, S, V] (None: the drafts are
+    certain) with uniform random numbers fp32 [B, S + 1], and draw the token after them.  Returns (tokens int32 [B, S + 1]: the
+    accepted ones, the drawn one, then -1; accepted int32 [B])."""
+    return (_marshal or _load_marshal()).verify_drafts(target, draft, drafted, uniform, n_drafted, tokens, accepted, dev_status, stream)
 
 
 # ----------------------------------------------------------------------------- hot-set slot table (Definition 5.1)

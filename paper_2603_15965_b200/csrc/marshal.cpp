@@ -16,6 +16,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <cmath>
 #include <string>
 #include <vector>
 
@@ -24,7 +25,7 @@
 namespace {
 
 PyObject* g_raise_status = nullptr;      // binding._check(function name, status)
-PyObject *s_x, *s_y, *s_A, *s_B, *s_scale, *s_row_scale, *s_cuda_stream, *s_data_ptr;
+PyObject *s_x, *s_y, *s_A, *s_B, *s_scale, *s_row_scale, *s_cuda_stream, *s_data_ptr, *s_k, *s_v, *s_k_scale, *s_v_scale;
 
 struct PyRaised {};                      // a Python exception is set
 [[noreturn]] void raise(PyObject* type, const std::string& text)
@@ -489,6 +490,235 @@ PyObject* apply_topk(PyObject* const* a)
     Py_RETURN_NONE;
 }
 
+// ---- the paged cache and draft verification: every tensor of a call on the current device
+void on_current_device(const at::Tensor& t, const char* name)
+{
+    if (!t.is_cuda() || t.device().index() != c10::cuda::current_device())
+        raise(PyExc_ValueError, std::string(name) + ": expected a tensor on the current CUDA device");
+}
+// [N, heads, dim] with dense heads; the pitch of a token
+struct Heads {
+    int64_t N, heads, dim, pitch;
+};
+Heads heads_of(const at::Tensor& t, const char* name)
+{
+    if (!t.is_cuda() || t.dim() != 3 || (t.numel() > 0 && ((t.size(2) > 1 && t.stride(2) != 1) || (t.size(1) > 1 && t.stride(1) != t.size(2)))))
+        raise(PyExc_ValueError, std::string(name) + ": expected a CUDA tensor [tokens, heads, dim] with dense heads");
+    on_current_device(t, name);
+    const int64_t width = t.size(1) * t.size(2);
+    return {t.size(0), t.size(1), t.size(2), t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(t.stride(0), width)};
+}
+// (a single row's stride is whatever its maker left there: only a multiple of 8 is of use to the library)
+int64_t pitch_of(const Heads& h) { return h.N > 1 ? h.pitch : (h.heads * h.dim + 7) / 8 * 8; }
+
+struct Cache {
+    molora_kv_cache_t c{};
+    explicit Cache(PyObject* o)
+    {
+        Ref ok(PyObject_GetAttr(o, s_k)), ov(PyObject_GetAttr(o, s_v)), oks(PyObject_GetAttr(o, s_k_scale)), ovs(PyObject_GetAttr(o, s_v_scale));
+        const at::Tensor &k = codes(ok.p, "cache.k"), &v = codes(ov.p, "cache.v"), &ks = scales(oks.p, "cache.k_scale", k), &vs = scales(ovs.p, "cache.v_scale", k);
+        if (v.sizes() != k.sizes()) raise(PyExc_ValueError, "cache.k and cache.v must have one shape");
+        c.k = k.data_ptr(), c.v = v.data_ptr();
+        c.k_scale = static_cast<float*>(ks.data_ptr()), c.v_scale = static_cast<float*>(vs.data_ptr());
+        for (int i = 0; i < 4; ++i)
+            if (k.size(i) > INT32_MAX) raise(PyExc_ValueError, "cache: a dimension is too large");
+        c.n_pages = (int32_t)k.size(0), c.kv_heads = (int32_t)k.size(1), c.page = (int32_t)k.size(2), c.dim = (int32_t)k.size(3);
+    }
+
+private:
+    static const at::Tensor& codes(PyObject* o, const char* name)
+    {
+        const at::Tensor& t = tensor(o, name);
+        if (!t.is_cuda() || t.dim() != 4 || !t.is_contiguous() || (t.scalar_type() != at::kByte && t.scalar_type() != at::kFloat8_e4m3fn))
+            raise(PyExc_ValueError, std::string(name) + ": expected a dense e4m3 (or uint8) CUDA tensor [pages, heads, page, dim]");
+        on_current_device(t, name);
+        return t;
+    }
+    static const at::Tensor& scales(PyObject* o, const char* name, const at::Tensor& k)
+    {
+        const at::Tensor& t = tensor(o, name);
+        if (!t.is_cuda() || t.scalar_type() != at::kFloat || t.dim() != 2 || !t.is_contiguous() || t.size(0) != k.size(0) || t.size(1) != k.size(1))
+            raise(PyExc_ValueError, std::string(name) + ": expected a dense fp32 CUDA tensor [pages, heads]");
+        on_current_device(t, name);
+        return t;
+    }
+};
+struct Sequences {
+    molora_sequences_t s{};
+    Sequences(PyObject* table, PyObject* cu, PyObject* lens)
+    {
+        const at::Tensor &t = tensor(table, "page_table"), &c = i32_dev(cu, "cu_tokens"), &l = i32_dev(lens, "kv_lens");
+        if (!t.is_cuda() || t.scalar_type() != at::kInt || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1))
+            raise(PyExc_ValueError, "page_table: expected a row-major int32 CUDA tensor [sequences, pages]");
+        on_current_device(t, "page_table");
+        on_current_device(c, "cu_tokens");
+        on_current_device(l, "kv_lens");
+        if (c.dim() != 1 || l.dim() != 1 || c.numel() != l.numel() + 1 || t.size(0) != l.numel() || l.numel() > INT32_MAX || t.size(1) > INT32_MAX)
+            raise(PyExc_ValueError, "page_table [B, pages], cu_tokens [B + 1] and kv_lens [B] must agree in B");
+        s.page_table = i32(t), s.ld_table = t.size(0) > 1 ? t.stride(0) : t.size(1);
+        s.cu_tokens = i32(c), s.kv_lens = i32(l);
+        s.B = (int32_t)l.numel(), s.max_pages = (int32_t)t.size(1);
+    }
+};
+
+// ---- (k, v, cache, page_table, cu_tokens, kv_lens, q, inv_freq, interleaved, q_out, dev_status, stream)
+PyObject* kv_append(PyObject* const* a)
+{
+    const at::Tensor &k = tensor(a[0], "k"), &v = tensor(a[1], "v");
+    const Heads hk = heads_of(k, "k"), hv = heads_of(v, "v");
+    const Cache cache(a[2]);
+    const Sequences seqs(a[3], a[4], a[5]);
+    const molora_dtype_t dt = dtype_code(k);
+    if (v.scalar_type() != k.scalar_type() || hv.N != hk.N || hk.heads != cache.c.kv_heads || hv.heads != cache.c.kv_heads || hk.dim != cache.c.dim ||
+        hv.dim != cache.c.dim)
+        raise(PyExc_ValueError, "k and v [tokens, kv_heads, dim] must match each other and the cache");
+    Heads hq{hk.N, 0, hk.dim, 0};
+    const bool with_q = a[6] != Py_None;
+    at::Tensor q, q_out;
+    if (with_q) {
+        q = tensor(a[6], "q");
+        hq = heads_of(q, "q");
+        if (q.scalar_type() != k.scalar_type() || hq.N != hk.N || hq.dim != hk.dim || hq.heads > INT32_MAX)
+            raise(PyExc_ValueError, "q [tokens, heads, dim] must match k");
+    }
+    int64_t ldqo = 0;
+    if (a[9] != Py_None) {
+        if (!with_q) raise(PyExc_ValueError, "q_out without q");
+        q_out = tensor(a[9], "q_out");
+        const Heads ho = heads_of(q_out, "q_out");
+        if (q_out.scalar_type() != q.scalar_type() || ho.N != hq.N || ho.heads != hq.heads || ho.dim != hq.dim) raise(PyExc_ValueError, "q_out must have the shape and type of q");
+        ldqo = pitch_of(ho);
+    }
+    const float* freq = nullptr;
+    int64_t rotary = 0;
+    if (a[7] != Py_None) {
+        const at::Tensor& f = tensor(a[7], "inv_freq");
+        if (!f.is_cuda() || f.scalar_type() != at::kFloat || f.dim() != 1 || !f.is_contiguous() || f.numel() > INT32_MAX / 2)
+            raise(PyExc_ValueError, "inv_freq: expected a dense fp32 CUDA tensor [rotary / 2]");
+        on_current_device(f, "inv_freq");
+        freq = static_cast<const float*>(f.data_ptr());
+        rotary = 2 * f.numel();
+    }
+    const int interleaved = PyObject_IsTrue(a[8]);
+    if (interleaved < 0) throw PyRaised{};
+    uint32_t* status = status_word(a[10]);
+    const Stream stream(a[11]);
+    call("molora_kv_append", [&] {
+        if (with_q && !q_out.defined()) {
+            q_out = allocate(stream, [&] { return at::empty({hq.N, hq.heads, hq.dim}, q.options()); });
+            ldqo = hq.heads * hq.dim;
+        }
+        return molora_kv_append(&cache.c, &seqs.s, dt, hk.N, k.data_ptr(), pitch_of(hk), v.data_ptr(), pitch_of(hv), with_q ? q.data_ptr() : nullptr,
+                                pitch_of(hq), with_q ? q_out.data_ptr() : nullptr, ldqo, (int32_t)hq.heads, freq, (int32_t)rotary, interleaved, status,
+                                stream.p);
+    });
+    if (!with_q) Py_RETURN_NONE;
+    return wrap(q_out);
+}
+
+// ---- (q, cache, page_table, cu_tokens, kv_lens, scale, causal, window, max_tokens, out, lse, ws, dev_status, stream)
+PyObject* kv_attend(PyObject* const* a)
+{
+    const at::Tensor& q = tensor(a[0], "q");
+    const Heads hq = heads_of(q, "q");
+    const Cache cache(a[1]);
+    const Sequences seqs(a[2], a[3], a[4]);
+    const molora_dtype_t dt = dtype_code(q);
+    if (hq.dim != cache.c.dim || hq.heads > INT32_MAX) raise(PyExc_ValueError, "q [tokens, heads, dim] must match the cache");
+    double scale = 1.0 / std::sqrt((double)hq.dim);
+    if (a[5] != Py_None) {
+        scale = PyFloat_AsDouble(a[5]);
+        if (scale == -1.0 && PyErr_Occurred()) throw PyRaised{};
+    }
+    const int causal = PyObject_IsTrue(a[6]);
+    if (causal < 0) throw PyRaised{};
+    const int64_t window = integer(a[7]), most = a[8] == Py_None ? 0 : integer(a[8]);
+    if (window > INT32_MAX || window < INT32_MIN) raise(PyExc_ValueError, "window does not fit 32 bits");
+    at::Tensor out;
+    int64_t ldo = hq.heads * hq.dim;
+    if (a[9] != Py_None) {
+        out = tensor(a[9], "out");
+        const Heads ho = heads_of(out, "out");
+        if (out.scalar_type() != q.scalar_type() || ho.N != hq.N || ho.heads != hq.heads || ho.dim != hq.dim) raise(PyExc_ValueError, "out must have the shape and type of q");
+        ldo = pitch_of(ho);
+    }
+    float* lse = nullptr;
+    if (a[10] != Py_None) {
+        const at::Tensor& t = tensor(a[10], "lse");
+        if (!t.is_cuda() || t.scalar_type() != at::kFloat || t.dim() != 2 || !t.is_contiguous() || t.size(0) != hq.N || t.size(1) != hq.heads)
+            raise(PyExc_ValueError, "lse: expected a dense fp32 CUDA tensor [tokens, heads]");
+        on_current_device(t, "lse");
+        lse = static_cast<float*>(t.data_ptr());
+    }
+    Workspace ws(a[11], a[11] == Py_None ? molora_kv_attend_workspace_bytes(dt, (int32_t)hq.heads, cache.c.kv_heads, cache.c.dim, most > 0 ? most : hq.N) : 0);
+    if (ws.t.defined()) on_current_device(ws.t, "ws");
+    uint32_t* status = status_word(a[12]);
+    const Stream stream(a[13]);
+    call("molora_kv_attend", [&] {
+        if (!out.defined()) out = allocate(stream, [&] { return at::empty({hq.N, hq.heads, hq.dim}, q.options()); });
+        ws.make(q.device(), false, stream);
+        return molora_kv_attend(&cache.c, &seqs.s, dt, hq.N, q.data_ptr(), pitch_of(hq), out.data_ptr(), ldo, lse, (int32_t)hq.heads, (float)scale, causal,
+                                (int32_t)window, most, ws.p, ws.n, status, stream.p);
+    });
+    return wrap(out);
+}
+
+// ---- (target, draft, drafted, uniform, n_drafted, tokens, accepted, dev_status, stream)
+PyObject* verify_drafts(PyObject* const* a)
+{
+    const at::Tensor &target = tensor(a[0], "target"), &drafted = i32_dev(a[2], "drafted"), &uniform = tensor(a[3], "uniform");
+    auto rows = [](const at::Tensor& t, const char* name) {
+        if (!t.is_cuda() || t.dim() != 3 || (t.size(2) > 1 && t.stride(2) != 1)) raise(PyExc_ValueError, std::string(name) + ": expected a CUDA tensor [sequences, rows, vocabulary] with dense rows");
+        on_current_device(t, name);
+    };
+    rows(target, "target");
+    const int64_t B = target.size(0), S = target.size(1) - 1, V = target.size(2);
+    const molora_dtype_t dt = dtype_code(target);
+    if (S < 0 || B > INT32_MAX || V > INT32_MAX || S > INT32_MAX) raise(PyExc_ValueError, "target: expected [sequences, drafts + 1, vocabulary]");
+    on_current_device(drafted, "drafted");
+    if (drafted.dim() != 2 || drafted.size(0) != B || drafted.size(1) != S) raise(PyExc_ValueError, "drafted: expected [sequences, drafts]");
+    if (!uniform.is_cuda() || uniform.scalar_type() != at::kFloat || uniform.dim() != 2 || !uniform.is_contiguous() || uniform.size(0) != B || uniform.size(1) != S + 1)
+        raise(PyExc_ValueError, "uniform: expected a dense fp32 CUDA tensor [sequences, drafts + 1]");
+    on_current_device(uniform, "uniform");
+    const void* draft = nullptr;
+    int64_t dls = 0, dl = 0;
+    if (a[1] != Py_None) {
+        const at::Tensor& d = tensor(a[1], "draft");
+        rows(d, "draft");
+        if (d.scalar_type() != target.scalar_type() || d.size(0) != B || d.size(1) != S || d.size(2) != V)
+            raise(PyExc_ValueError, "draft: expected [sequences, drafts, vocabulary] of the target's type");
+        if (S > 0) draft = d.data_ptr();
+        dls = B > 1 ? d.stride(0) : S * V, dl = S > 1 ? d.stride(1) : V;
+    }
+    const int32_t* n = nullptr;
+    if (a[4] != Py_None) {
+        const at::Tensor& t = i32_dev(a[4], "n_drafted");
+        on_current_device(t, "n_drafted");
+        if (t.numel() != B) raise(PyExc_ValueError, "n_drafted: expected one number per sequence");
+        n = i32(t);
+    }
+    auto given = [&](PyObject* o, const char* name, int64_t count) {
+        if (o == Py_None) return;
+        const at::Tensor& t = i32_dev(o, name);
+        on_current_device(t, name);
+        if (t.numel() != count) raise(PyExc_ValueError, std::string(name) + ": wrong number of elements");
+    };
+    given(a[5], "tokens", B * (S + 1));
+    given(a[6], "accepted", B);
+    Out accepted(a[6], "accepted", B, target.device());
+    at::Tensor tokens;
+    if (a[5] != Py_None) tokens = tensor(a[5], "tokens");
+    uint32_t* status = status_word(a[7]);
+    const Stream stream(a[8]);
+    call("molora_verify_drafts", [&] {
+        int32_t* acc = accepted.get(stream);
+        if (!tokens.defined()) tokens = allocate(stream, [&] { return at::empty({B, S + 1}, drafted.options()); });
+        return molora_verify_drafts(target.data_ptr(), B > 1 ? target.stride(0) : (S + 1) * V, S > 0 ? target.stride(1) : V, draft, dls, dl, dt, i32(drafted), n,
+                                    static_cast<const float*>(uniform.data_ptr()), (int32_t)B, (int32_t)S, (int32_t)V, i32(tokens), acc, status, stream.p);
+    });
+    return tuple_of({tokens, accepted.t});
+}
+
 // ---- (raise_status)
 PyObject* bind(PyObject* const* a)
 {
@@ -518,6 +748,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n)
 #define ENTRY(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<name, n>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(route_vocab, 5), ENTRY(route_composite, 7), ENTRY(route_gate, 9), ENTRY(route_mlp, 11), ENTRY(group, 8),
                          ENTRY(apply_batched, 7), ENTRY(group_apply_batched, 10), ENTRY(topk_softmax, 3), ENTRY(apply_topk, 7), ENTRY(bind, 1),
+                         ENTRY(kv_append, 12), ENTRY(kv_attend, 14), ENTRY(verify_drafts, 9),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -533,5 +764,9 @@ PyMODINIT_FUNC PyInit__marshal()
     s_row_scale = PyUnicode_InternFromString("row_scale");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
+    s_k = PyUnicode_InternFromString("k");
+    s_v = PyUnicode_InternFromString("v");
+    s_k_scale = PyUnicode_InternFromString("k_scale");
+    s_v_scale = PyUnicode_InternFromString("v_scale");
     return PyModule_Create(&module);
 }
