@@ -73,9 +73,8 @@ molora_status_t molora_kv_append(const molora_kv_cache_t* cache, const molora_se
 
 size_t molora_kv_attend_workspace_bytes(molora_dtype_t dt, int32_t heads, int32_t kv_heads, int32_t dim, int64_t max_tokens)
 {
-    (void)dt, (void)max_tokens;
-    if ((dim != 64 && dim != 128) || kv_heads < 1 || heads < 1 || heads % kv_heads != 0) return 0;
-    return attend_rows_workspace_bytes(dim);
+    if ((dim != 64 && dim != 128) || kv_heads < 1 || heads < 1 || heads % kv_heads != 0 || max_tokens < 1 || (dt != MOLORA_F32 && dt != MOLORA_BF16)) return 0;
+    return attend_rows_workspace_bytes(dt, dim, max_tokens * (heads / kv_heads));
 }
 
 molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_sequences_t* seqs, molora_dtype_t dt, int64_t N, const void* q,
@@ -98,7 +97,7 @@ molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_se
     a.heads = heads, a.causal = causal != 0, a.window = window;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.dev_status = dev_status;
-    return launch_attend_rows(a, dt, ws, static_cast<cudaStream_t>(stream));
+    return launch_attend_rows(a, dt, max_tokens * (heads / cache->kv_heads), ws, static_cast<cudaStream_t>(stream));
 }
 
 molora_status_t molora_verify_drafts(const void* target, int64_t target_ld_seq, int64_t target_ld, const void* draft, int64_t draft_ld_seq,

@@ -1,48 +1,74 @@
-// Attention over the paged 8-bit cache for tiles of 16 query rows (molora_kv_attend): single tokens, drafted tokens, fp32.
+// Attention over the paged 8-bit cache for tiles of 8 to 32 query rows (molora_kv_attend): single tokens, drafted tokens, fp32.
 //
-// A row of a sequence is (new token, query head of the group that shares a key / value head); 16 consecutive rows, one
-// key / value head and the keys that they see are a UNIT.  The units' keys, cut into steps of 16, form one long list; every warp
-// of the grid takes an equal, contiguous share of it, whatever the lengths of the sequences.  A unit that lies inside one
-// share is written at once; one that is cut leaves its pieces (sum, maximum, weighted values, all fp32) in the
-// workspace, and a second kernel joins them in the order of the keys: results do not depend on timing.
+// A row of a sequence is (new token, query head of the group that shares a key / value head); 8 NT consecutive rows, one
+// key / value head and the keys that they see are a UNIT.  The units' keys, cut into steps of 32, form one long list; every CTA
+// of the grid takes an equal, contiguous share of it, whatever the lengths of the sequences, and its four warps a
+// quarter each of what the share has of a unit.  A unit that lies inside one share is written at once; one that is cut leaves its
+// pieces (sum, maximum, weighted values, all fp32) in the workspace, and a second kernel joins them in the order of the
+// keys: results do not depend on timing.  There are twice as many shares as resident CTAs, since SMs do not get equal shares of the
+// memory's bandwidth.
 //
-// Inside a warp nothing is shared and nothing synchronised: a lane asks for exactly the 16-byte vectors of codes that its
-// fragments need and waits for its own copies only (cp.async ring, kStages steps deep).
-//   S = Q K^T   mma m16n8k16: lane (g, t) holds of key g the elements 16 t .. 16 t + 15 of each 64; the order of the elements in the
-//               sum is free, so a 4-byte word of codes is one B fragment and Q's fragments follow the same order
-//   O = P V     lane (g, t) holds of the keys 2t, 2t+1, 2t+8, 2t+9 the D / 8 elements from g D / 8 on; byte permutes pair
-//               two keys of one element, and the accumulator's columns 2t, 2t+1 are then D / 4 neighbouring elements of the result
+// On its keys a warp shares nothing and synchronises with nobody: a lane asks for exactly the 16-byte vectors of codes that its
+// fragments need and waits for its own copies only (cp.async ring).  Keys and elements of the values are the 16 rows of the
+// tensor instruction (mma m16n8k16), query rows its 8 columns, so that a single token's few heads waste little:
+//   S^T = K Q^T   lane (g, t) holds of the keys g and g + 8 the elements 16 t .. 16 t + 15 of each 64; the order of the elements
+//                 in the sum is free, so a 4-byte word of codes is half an A fragment and Q's fragments follow the same order
+//   O^T = V^T P^T lane (g, t) holds of the keys 2t, 2t+1, 2t+8, 2t+9 the D / 8 elements from g D / 8 on; byte permutes pair
+//                 two keys of one element; the weights come into place by movmatrix, and a lane ends with D / 8 neighbouring
+//                 elements of two rows
 // Every e4m3 value is an fp16 value (one cvt for two); q is brought into fp16 by a power of two per row, exactly for bf16, in two
 // terms of 11 bits for fp32.  The scale of a block of K multiplies its scores; that of V is added, as a logarithm, to the exponent, so
 // that the weights handed to the tensor cores have the size of what they contribute, and the sum takes it off again.
 // Weights are at most 2^15 (fp16 normal down to 2^-29 of a row's largest): the reference of a row moves only when a score is
 // 2^8 over the weight it gave its largest, and then everything is rescaled.
 // What bounds it: the codes, 2 D bytes per (key, key / value head), from HBM.
+#include <type_traits>
+
 #include "kv_cache.cuh"
 
 namespace molora {
 namespace {
 
 constexpr int kWarpsPerCta = 4, kThreads = kWarpsPerCta * 32;
-constexpr int kCtasPerSm = 3;
-constexpr int kStages = 4;
-constexpr int kRows = 16, kStepKeys = 16;
-constexpr int kMinShare = 4;                 // steps: shorter shares cost more in joining than they save
+constexpr int kHalfKeys = 16, kStepKeys = 32;  // keys of a tensor instruction, and of a step: two of them, in one page or in two of 16
+constexpr int kMinShare = 4;                 // steps of a CTA: shorter shares cost more in joining than they save
+constexpr int kWaves = 2;                    // shares per resident CTA
+constexpr int kMaxTiles = 4;                 // 8-row tiles of a unit
 constexpr float kNone = -1e30f;              // reference of a row that has seen nothing
 constexpr float kTop = 7.f;                  // weight of a row's largest score when the reference is set: 2^7
+
+// CTAs per SM by what a thread holds (accumulators D / 4 NT, fragments of q D / 8 NT per term), and copies in flight per warp
+template <typename T, int D, int NT>
+struct Shape {
+    static constexpr int kTerms = sizeof(T) == 4 ? 2 : 1;
+    static constexpr int kWork = (D / 4 + D / 8 * kTerms) * NT;          // registers
+    static constexpr int kCtas = kWork <= 48 ? 3 : 2;
+    static constexpr bool kPairs = kWork <= 96;                           // two steps at a time
+    static constexpr int kStages = 2;                                     // steps in the ring of a warp
+    static constexpr int kHalfBytes = kHalfKeys * 2 * D;
+    static constexpr size_t kSmem = (size_t)kWarpsPerCta * kStages * 2 * kHalfBytes;      // (and 8 NT rows of fp32 values per warp fit it)
+    static_assert(kStages * 2 * kHalfBytes >= 8 * NT * D * 4, "a warp's share of the ring holds its rows");
+};
 
 // What a cut unit leaves behind.
 struct CutUnit {
     int32_t b, row_tile, head, pieces;       // pieces 0: no unit begins in this share and goes on in the next
 };
-__host__ __device__ constexpr int slot_floats(int dim) { return 2 * kRows + kRows * dim; }
+__host__ __device__ constexpr int slot_floats(int rows, int dim) { return 2 * rows + rows * dim; }
 __host__ __device__ inline size_t cut_bytes(int64_t workers) { return (size_t)((workers * (int64_t)sizeof(CutUnit) + 255) / 256 * 256); }
 
-__device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1)
+__device__ __forceinline__ void mma_f16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 8 x 8 matrix of 16-bit elements, transposed across the warp
+__device__ __forceinline__ uint32_t transposed(uint32_t v)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 {
@@ -55,24 +81,27 @@ __device__ __forceinline__ uint32_t pack_f16_rest(float lo, float hi, uint32_t t
     const float2 t = f16x2_to_f32x2(top);
     return pack_f16(lo - t.x, hi - t.y);
 }
-__device__ __forceinline__ void cp_async_8(uint32_t dst, const void* src)
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src)
 {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+    if constexpr (BYTES == 16) ptx::cp_async_16(dst, src);
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 
 // steps of every unit of a sequence, and where its keys begin
 struct Span {
-    int32_t lo;        // first key, a multiple of 16
-    int32_t steps;     // of 16 keys, per unit
+    int32_t lo;        // first key, a multiple of 32
+    int32_t steps;     // of 32 keys, per unit
     int32_t tiles;     // row tiles
 };
+template <int ROWS>
 __device__ __forceinline__ Span span_of(const Sequence& s, int group, int window)
 {
     Span r{0, 0, 0};
     if (s.n == 0) return r;
     r.lo = window > 0 ? max(0, s.first_pos() - window + 1) & ~(kStepKeys - 1) : 0;
     r.steps = max(1, (s.len - r.lo + kStepKeys - 1) / kStepKeys);
-    r.tiles = (int32_t)(((int64_t)s.n * group + kRows - 1) / kRows);
+    r.tiles = (int32_t)(((int64_t)s.n * group + ROWS - 1) / ROWS);
     return r;
 }
 
@@ -84,52 +113,69 @@ __device__ __forceinline__ void load16(const T* p, float* x)
     for (int i = 0; i < 16 / E; ++i) unpack<T>(ld128_rw_stream(p + i * E), x + i * E);
 }
 
-template <typename T, int D>
-__device__ __forceinline__ void store_run(T* p, const float* x)          // D / 4 neighbouring elements
+template <typename T, int N>
+__device__ __forceinline__ void store_run(T* p, const float* x)          // N neighbouring elements
 {
     constexpr int E = VecTraits<T>::kElems;
 #pragma unroll
-    for (int i = 0; i < D / 4 / E; ++i) stg128(p + i * E, pack<T>(x + i * E));
+    for (int i = 0; i < N / E; ++i) stg128(p + i * E, pack<T>(x + i * E));
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? kCtasPerSm : 2)
+__device__ __forceinline__ void store4(float* p, float4 v, float f) { *reinterpret_cast<float4*>(p) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f); }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v, float f)
+{
+    *reinterpret_cast<uint2*>(p) = make_uint2(f32x2_to_bf16x2(v.x * f, v.y * f), f32x2_to_bf16x2(v.z * f, v.w * f));
+}
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
     attend_rows_kernel(const __grid_constant__ AttendArgs a, CutUnit* __restrict__ cuts, float* __restrict__ slots)
 {
-    constexpr bool kTwo = sizeof(T) == 4;               // q and the weights in two fp16 terms
-    constexpr int kTerms = kTwo ? 2 : 1;
+    using Sh = Shape<T, D, NT>;
+    constexpr int kTerms = Sh::kTerms;                  // fp16 terms of q and of the weights
+    constexpr int kStages = Sh::kStages;
+    constexpr int kRows = 8 * NT;
     constexpr int HF = D / 64;                          // 64-element parts of a key
     constexpr int kVBytes = D / 8;                      // of a value, per lane
-    constexpr int kStageBytes = 32 * (2 * HF * 16 + 4 * kVBytes);
+    constexpr int kMT = D / 16;                         // 16-element tiles of the values
+    constexpr bool kPairs = Sh::kPairs;
     __shared__ int64_t s_upto[kThreads];                // steps of the sequences up to the end of thread i's part
-    __shared__ float2 s_scales[kWarpsPerCta][kStages];
+    __shared__ float4 s_scales[kWarpsPerCta][kStages][2];  // of a half: scale of K, logarithm and reciprocal of V's, whether its page can be used
+    __shared__ float s_m[kWarpsPerCta][kRows], s_l[kWarpsPerCta][kRows];
     extern __shared__ __align__(16) uint8_t ring_all[];
     ptx::grid_dependency_sync();
 
     const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int group = a.heads / a.c.kv_heads;
     const int plog = a.c.page_log2;
-    const uint32_t ring = ptx::smem_u32(ring_all) + (uint32_t)(warp * kStages * kStageBytes);
+    uint8_t* const ring = ring_all + warp * kStages * 2 * Sh::kHalfBytes;
+    const uint32_t ring_at = ptx::smem_u32(ring);
 
     // ---- the shares
     const int part = (a.c.B + kThreads - 1) / kThreads;
     int64_t mine = 0;
     for (int b = tid * part; b < min(a.c.B, (tid + 1) * part); ++b) {
         const Sequence sq = sequence_of(a.c, b, a.N);
-        const Span sp = span_of(sq, group, a.window);
+        const Span sp = span_of<kRows>(sq, group, a.window);
         mine += (int64_t)sp.steps * sp.tiles * a.c.kv_heads;
         if (sq.bad && blockIdx.x == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
     }
-    s_upto[tid] = mine;
-    __syncthreads();
-    for (int o = 1; o < kThreads; o <<= 1) {
-        const int64_t add = tid >= o ? s_upto[tid - o] : 0;
+    {
+        int64_t incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (lane == 31) s_upto[tid] = incl;
         __syncthreads();
-        s_upto[tid] += add;
+        for (int w = 0; w < warp; ++w) incl += s_upto[32 * w + 31];
+        __syncthreads();
+        s_upto[tid] = incl;
         __syncthreads();
     }
     const int64_t total = s_upto[kThreads - 1];
-    const int64_t workers = (int64_t)gridDim.x * kWarpsPerCta, w = (int64_t)blockIdx.x * kWarpsPerCta + warp;
+    const int64_t workers = gridDim.x, w = blockIdx.x;
     const int64_t share = max((total + workers - 1) / workers, (int64_t)kMinShare);
     int64_t at = w * share;
     const int64_t stop = min(total, at + share);
@@ -145,12 +191,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? kCtasPerSm : 2)
         int b = lo * part;
         int64_t base = lo > 0 ? s_upto[lo - 1] : 0;      // first step of sequence b
         Sequence sq = sequence_of(a.c, b, a.N);
-        Span sp = span_of(sq, group, a.window);
+        Span sp = span_of<kRows>(sq, group, a.window);
         while (at < stop) {
             while (base + (int64_t)sp.steps * sp.tiles * a.c.kv_heads <= at) {
                 base += (int64_t)sp.steps * sp.tiles * a.c.kv_heads;
                 sq = sequence_of(a.c, ++b, a.N);
-                sp = span_of(sq, group, a.window);
+                sp = span_of<kRows>(sq, group, a.window);
             }
             const int64_t unit = (at - base) / sp.steps;
             const int64_t unit_at = base + unit * sp.steps;                 // its first step
@@ -160,26 +206,82 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? kCtasPerSm : 2)
 
             // ---- the rows of the unit
             const int n_rows = (int)min((int64_t)kRows, (int64_t)sq.n * group - (int64_t)tile * kRows);
-            const int64_t tile_row = (int64_t)tile * kRows;
-            auto token_of = [&](int r) { return (int)((tile_row + r) / group); };
+            const int tile_row = tile * kRows;
+            auto token_of = [&](int r) { return (tile_row + min(r, n_rows - 1)) / group; };
             auto upper = [&](int token) { return a.causal ? max(0, min(sq.first_pos() + token + 1, sq.len)) : sq.len; };
             auto lower = [&](int token) { return a.window > 0 ? max(0, sq.first_pos() + token - a.window + 1) : 0; };
             const int tok_lo = token_of(0), tok_hi = token_of(n_rows - 1);
             const int hi_min = upper(tok_lo), hi_max = upper(tok_hi), lo_min = lower(tok_lo), lo_max = lower(tok_hi);
-            int hi_row[2], lo_row[2];
-            float rowf[2], m[2] = {kNone, kNone}, l[2] = {0.f, 0.f};
-            uint32_t qa[kTerms][4 * HF][4];
-            int64_t out_row[2];
-            int out_head[2];
+
+            // ---- its steps that some row sees, a contiguous part of them for each warp; the first come in while q does
+            const int u0 = max(first, (lo_min - sp.lo) / kStepKeys);
+            const int u1 = min(last, hi_max > sp.lo ? (hi_max - sp.lo + kStepKeys - 1) / kStepKeys : 0);
+            const int per_warp = (max(u1 - u0, 0) + kWarpsPerCta - 1) / kWarpsPerCta;
+            const int s0 = u0 + warp * per_warp, s1 = min(u1, s0 + per_warp);
+            const int32_t* table = a.c.table + (int64_t)b * a.c.ld_table;
+            int group0 = -1;                              // first of the 32 pages whose ids and scales the lanes hold
+            int32_t page_id = -1;
+            float page_ks = 0.f, page_lvs = 0.f, page_inv = 0.f;
+            auto load_pages = [&](int page) {
+                group0 = page;
+                page_id = -1;
+                if (((int64_t)(page + lane) << plog) < hi_max) {
+                    page_id = ptx::ld_dependent(table + page + lane);
+                    if (page_id < 0 || page_id >= a.c.n_pages) {
+                        page_id = -1;
+                        if (a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
+                    } else {
+                        const int64_t block = (int64_t)page_id * a.c.kv_heads + head;
+                        page_ks = ptx::ld_dependent(a.c.k_scale + block);
+                        const float vs = fminf(fmaxf(ptx::ld_dependent(a.c.v_scale + block), 7.8886090522e-31f), 1.2676506002e30f);      // 2^-100, 2^100
+                        page_lvs = log2f(vs), page_inv = 1.f / vs;
+                    }
+                }
+            };
+            // 16 keys from `row` (of all tokens of the pool) on
+            auto copy_half = [&](int64_t row, uint32_t dst) {
+                const uint8_t* k = a.c.k + row * D + (g * D + t * 16);
+                const uint32_t kdst = dst + (uint32_t)(lane * 16);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = min(g + 8 * i, n_rows - 1);
-                const int token = token_of(r);
-                const int qh = head * group + (int)((tile_row + r) - (int64_t)token * group);
-                hi_row[i] = upper(token), lo_row[i] = lower(token);
-                out_row[i] = (int64_t)sq.row0 + token, out_head[i] = qh;
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int f = 0; f < HF; ++f) copy_async<16>(kdst + (uint32_t)((j * HF + f) * 512), k + j * 8 * D + f * 64);
+                const uint8_t* v = a.c.v + row * D + (2 * t * D + g * kVBytes);
+                const uint32_t vdst = dst + 2 * HF * 512 + (uint32_t)(lane * kVBytes);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) copy_async<kVBytes>(vdst + (uint32_t)(j * 32 * kVBytes), v + ((j & 1) + 8 * (j >> 1)) * D);
+            };
+            auto issue = [&](int s) {
+                if (s < s1) {
+                    const int key = sp.lo + s * kStepKeys, page = key >> plog, put = (s - s0) & (kStages - 1);
+                    if (group0 < 0 || page >= group0 + 32 || (plog == 4 && page + 1 >= group0 + 32)) load_pages(page);
+                    const uint32_t dst = ring_at + (uint32_t)(put * 2 * Sh::kHalfBytes);
+                    const int32_t id = __shfl_sync(0xFFFFFFFFu, page_id, page - group0);
+                    const float4 sc = make_float4(page_ks, page_lvs, page_inv, page_id >= 0 ? 1.f : 0.f);
+                    const int64_t row = (((int64_t)id * a.c.kv_heads + head) << plog) + (key & ((1 << plog) - 1));
+                    if (lane == page - group0) s_scales[warp][put][0] = sc;
+                    if (id >= 0) copy_half(row, dst);
+                    if (plog > 4) {
+                        if (lane == page - group0) s_scales[warp][put][1] = sc;
+                        if (id >= 0) copy_half(row + kHalfKeys, dst + Sh::kHalfBytes);
+                    } else {
+                        const int32_t id1 = __shfl_sync(0xFFFFFFFFu, page_id, page + 1 - group0);
+                        if (lane == page + 1 - group0) s_scales[warp][put][1] = sc;
+                        if (id1 >= 0) copy_half(((int64_t)id1 * a.c.kv_heads + head) << plog, dst + Sh::kHalfBytes);
+                    }
+                }
+                ptx::cp_async_commit();                   // (empty groups keep the count)
+            };
+            issue(s0);
+
+            float rowf[NT][2], m[NT][2], l[NT][2];        // rows 8 n + 2 t and the next
+            uint32_t qb[kTerms][NT][4 * HF][2];           // row 8 n + g
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int r = min(8 * n + g, n_rows - 1);
+                const int token = token_of(r), qh = head * group + (tile_row + r - token * group);
                 float x[HF][16], amax = 0.f;
-                const T* q = static_cast<const T*>(a.q) + out_row[i] * a.ldq + (int64_t)qh * D;
+                const T* q = static_cast<const T*>(a.q) + ((int64_t)sq.row0 + token) * a.ldq + (int64_t)qh * D;
 #pragma unroll
                 for (int f = 0; f < HF; ++f) {
                     load16(q + f * 64 + t * 16, x[f]);
@@ -191,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? kCtasPerSm : 2)
                 // the row's largest element to [2^14, 2^15)
                 const int e = amax > 0.f ? min(100, 14 - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
                 const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-                rowf[i] = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
+                const float down = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
                 for (int f = 0; f < HF; ++f)
 #pragma unroll
@@ -200,347 +302,381 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? kCtasPerSm : 2)
                         for (int z = 0; z < 2; ++z) {
                             const float p0 = x[f][4 * c + 2 * z] * up, p1 = x[f][4 * c + 2 * z + 1] * up;
                             const uint32_t top = pack_f16(p0, p1);
-                            qa[0][4 * f + c][2 * z + i] = top;
-                            if constexpr (kTwo) qa[kTerms - 1][4 * f + c][2 * z + i] = pack_f16_rest(p0, p1, top);
+                            qb[0][n][4 * f + c][z] = top;
+                            if constexpr (kTerms == 2) qb[kTerms - 1][n][4 * f + c][z] = pack_f16_rest(p0, p1, top);
                         }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    rowf[n][i] = __shfl_sync(0xFFFFFFFFu, down, (2 * t + i) * 4);
+                    m[n][i] = kNone, l[n][i] = 0.f;
+                }
             }
-            float o[D / 8][4];
+            float o[NT][kMT][4];
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < kMT; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
 
-            // ---- its steps that some row sees
-            const int s0 = max(first, (lo_min - sp.lo) / kStepKeys);
-            const int s1 = min(last, hi_max > sp.lo ? (hi_max - sp.lo + kStepKeys - 1) / kStepKeys : 0);
-            const int32_t* table = a.c.table + (int64_t)b * a.c.ld_table;
-            int group0 = -1;                              // first of the 32 pages whose ids and scales the lanes hold
-            int32_t page_id = -1;
-            float page_ks = 0.f, page_vs = 0.f;
-            auto issue = [&](int s) {
-                if (s < s1) {
-                    const int key = sp.lo + s * kStepKeys, page = key >> plog;
-                    if (group0 < 0 || page >= group0 + 32) {
-                        group0 = page;
-                        page_id = -1;
-                        if (((int64_t)(page + lane) << plog) < hi_max) {
-                            page_id = ptx::ld_dependent(table + page + lane);
-                            if (page_id < 0 || page_id >= a.c.n_pages) {
-                                page_id = -1;
-                                if (a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
-                            } else {
-                                const int64_t block = (int64_t)page_id * a.c.kv_heads + head;
-                                page_ks = ptx::ld_dependent(a.c.k_scale + block);
-                                page_vs = fminf(fmaxf(ptx::ld_dependent(a.c.v_scale + block), 7.8886090522e-31f), 1.2676506002e30f);      // 2^-100, 2^100
-                            }
+            // SUBS halves from key0 on, in ring position `at_step` from half `half` on
+            auto work = [&](int key0, int at_step, int half, auto subs) {
+                constexpr int SUBS = decltype(subs)::value;
+                float4 sc[SUBS];
+                float x[SUBS][NT][4];                     // keys g (0, 1) and g + 8 (2, 3), rows 2 t and 2 t + 1
+#pragma unroll
+                for (int u = 0; u < SUBS; ++u) {
+                    const uint8_t* stage = ring + (2 * at_step + half + u) * Sh::kHalfBytes;
+                    sc[u] = s_scales[warp][at_step][half + u];
+                    uint32_t kw[2][HF][4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int f = 0; f < HF; ++f) {
+                            const uint4 w4 = *reinterpret_cast<const uint4*>(stage + ((j * HF + f) * 32 + lane) * 16);
+                            kw[j][f][0] = w4.x, kw[j][f][1] = w4.y, kw[j][f][2] = w4.z, kw[j][f][3] = w4.w;
                         }
-                    }
-                    const int32_t id = __shfl_sync(0xFFFFFFFFu, page_id, page - group0);
-                    const float ks = __shfl_sync(0xFFFFFFFFu, page_ks, page - group0), vs = __shfl_sync(0xFFFFFFFFu, page_vs, page - group0);
-                    if (lane == 0) s_scales[warp][s % kStages] = make_float2(ks, id >= 0 ? vs : -1.f);
-                    if (id >= 0) {
-                        const int64_t row = (((int64_t)id * a.c.kv_heads + head) << plog) + (key & ((1 << plog) - 1));
-                        const uint32_t dst = ring + (uint32_t)((s % kStages) * kStageBytes);
-                        const uint8_t* k = a.c.k + (row + g) * D + t * 16;
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-#pragma unroll
-                            for (int f = 0; f < HF; ++f)
-                                ptx::cp_async_16(dst + (uint32_t)(((j * HF + f) * 32 + lane) * 16), k + j * 8 * D + f * 64);
-                        const uint8_t* v = a.c.v + row * D + g * kVBytes;
-                        const uint32_t vdst = dst + 2 * HF * 512;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint8_t* src = v + (2 * t + (j & 1) + 8 * (j >> 1)) * D;
-                            if constexpr (kVBytes == 16) ptx::cp_async_16(vdst + (uint32_t)((j * 32 + lane) * 16), src);
-                            else cp_async_8(vdst + (uint32_t)((j * 32 + lane) * 8), src);
-                        }
-                    }
-                }
-                ptx::cp_async_commit();                   // (empty groups keep the count)
-            };
-            __syncwarp();
-            for (int s = s0; s < s0 + kStages - 1; ++s) issue(s);
-            for (int s = s0; s < s1; ++s) {
-                issue(s + kStages - 1);
-                ptx::cp_async_wait<kStages - 1>();
-                __syncwarp();                             // (the scales)
-                const float2 sc = s_scales[warp][s % kStages];
-                if (sc.y < 0.f) continue;                 // a page outside the pool
-                const uint8_t* stage = ring_all + (warp * kStages + s % kStages) * kStageBytes;
-                uint32_t kw[2][HF][4], vw[4][kVBytes / 4];
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int f = 0; f < HF; ++f) {
-                        const uint4 x = *reinterpret_cast<const uint4*>(stage + ((j * HF + f) * 32 + lane) * 16);
-                        kw[j][f][0] = x.x, kw[j][f][1] = x.y, kw[j][f][2] = x.z, kw[j][f][3] = x.w;
-                    }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if constexpr (kVBytes == 16) {
-                        const uint4 x = *reinterpret_cast<const uint4*>(stage + 2 * HF * 512 + (j * 32 + lane) * 16);
-                        vw[j][0] = x.x, vw[j][1] = x.y, vw[j][2] = x.z, vw[j][3] = x.w;
-                    } else {
-                        const uint2 x = *reinterpret_cast<const uint2*>(stage + 2 * HF * 512 + (j * 32 + lane) * 8);
-                        vw[j][0] = x.x, vw[j][1] = x.y;
-                    }
-                }
-                float x[2][4];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    x[j][0] = x[j][1] = x[j][2] = x[j][3] = 0.f;
+                    float part[HF][NT][4];                // (a chain of sums per half: each waits for its predecessor)
 #pragma unroll
                     for (int f = 0; f < HF; ++f)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const uint32_t b0 = e4m3x2_to_f16x2(kw[j][f][c]), b1 = e4m3x2_to_f16x2_high(kw[j][f][c]);
+                        for (int n = 0; n < NT; ++n) part[f][n][0] = part[f][n][1] = part[f][n][2] = part[f][n][3] = 0.f;
 #pragma unroll
-                            for (int z = 0; z < kTerms; ++z) mma_f16(x[j], qa[z][4 * f + c], b0, b1);
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int f = 0; f < HF; ++f) {
+                            const uint32_t a0 = e4m3x2_to_f16x2(kw[0][f][c]), a2 = e4m3x2_to_f16x2_high(kw[0][f][c]);
+                            const uint32_t a1 = e4m3x2_to_f16x2(kw[1][f][c]), a3 = e4m3x2_to_f16x2_high(kw[1][f][c]);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int z = 0; z < kTerms; ++z) mma_f16(part[f][n], a0, a1, a2, a3, qb[z][n][4 * f + c][0], qb[z][n][4 * f + c][1]);
                         }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[u][n][e] = HF == 2 ? part[0][n][e] + part[HF - 1][n][e] : part[0][n][e];
                 }
-                const int key0 = sp.lo + s * kStepKeys;
-                if (key0 + kStepKeys > hi_min || key0 < lo_max) {
-                    // Some row does not see some key of this step.  Values that no row sees count as zero; a NaN among the codes of a value
+                const bool border = key0 + SUBS * kHalfKeys > hi_min || key0 < lo_max;
+                uint32_t vw[SUBS][4][kVBytes / 4];
+#pragma unroll
+                for (int u = 0; u < SUBS; ++u) {
+                    const uint8_t* stage = ring + (2 * at_step + half + u) * Sh::kHalfBytes + 2 * HF * 512;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if constexpr (kVBytes == 16) {
+                            const uint4 w4 = *reinterpret_cast<const uint4*>(stage + (j * 32 + lane) * 16);
+                            vw[u][j][0] = w4.x, vw[u][j][1] = w4.y, vw[u][j][2] = w4.z, vw[u][j][3] = w4.w;
+                        } else {
+                            const uint2 w2 = *reinterpret_cast<const uint2*>(stage + (j * 32 + lane) * 8);
+                            vw[u][j][0] = w2.x, vw[u][j][1] = w2.y;
+                        }
+                    }
+                }
+                if (border) {
+                    // Some row does not see some key of these steps.  Values that no row sees count as zero; a NaN among the codes of a value
                     // becomes a NaN in the scores of the rows that see it and a zero here, so that it cannot reach the others through
                     // their weight of zero.
                     unsigned nan = 0;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int key = key0 + 2 * t + (j & 1) + 8 * (j >> 1);
-                        const bool none = key >= hi_max || key < lo_min;
+                    for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-                        for (int i = 0; i < kVBytes / 4; ++i) {
-                            const uint32_t bits = e4m3x4_nan_bits(vw[j][i]);
-                            if (bits != 0 && !none) nan |= 1u << j;
-                            vw[j][i] = none ? 0u : vw[j][i] & ~((bits >> 7) * 0xFFu);
+                        for (int j = 0; j < 4; ++j) {
+                            const int k16 = 16 * u + 2 * t + (j & 1) + 8 * (j >> 1), key = key0 + k16;
+                            const bool none = key >= hi_max || key < lo_min;
+#pragma unroll
+                            for (int i = 0; i < kVBytes / 4; ++i) {
+                                const uint32_t bits = e4m3x4_nan_bits(vw[u][j][i]);
+                                if (bits != 0 && !none) nan |= 1u << k16;
+                                vw[u][j][i] = none ? 0u : vw[u][j][i] & ~((bits >> 7) * 0xFFu);
+                            }
                         }
-                    }
-                    nan |= __shfl_xor_sync(0xFFFFFFFFu, nan, 4);
-                    nan |= __shfl_xor_sync(0xFFFFFFFFu, nan, 8);
-                    nan |= __shfl_xor_sync(0xFFFFFFFFu, nan, 16);
+                    nan = __reduce_or_sync(0xFFFFFFFFu, nan);
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const int key = key0 + 8 * j + 2 * t + (c & 1), i = c >> 1;
-                            const bool poisoned = (nan >> (2 * j + (c & 1))) & 1u;
-                            x[j][c] = key >= hi_row[i] || key < lo_row[i] ? -INFINITY : poisoned ? __int_as_float(0x7FC00000) : x[j][c];
+                        for (int i = 0; i < 2; ++i) {
+                            const int token = token_of(8 * n + 2 * t + i), hi_row = upper(token), lo_row = lower(token);
+#pragma unroll
+                            for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    const int k16 = 16 * u + g + 8 * j, key = key0 + k16;
+                                    float& v = x[u][n][2 * j + i];
+                                    v = key >= hi_row || key < lo_row ? -INFINITY : (nan >> k16) & 1u ? __int_as_float(0x7FC00000) : v;
+                                }
                         }
                 }
-                const float lvs = __log2f(sc.y), inv_vs = 1.f / sc.y;
-                float c[2], off[2];
+                // sc: scale of K, logarithm of V's, its reciprocal
+                float c[SUBS][NT][2], top = -INFINITY, y[SUBS][NT][4];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) c[i] = fmaxf(rowf[i] * sc.x, 1.17549435e-38f), off[i] = lvs - m[i];      // (never 0: a hidden score is -infinity times it)
-                float y[2][4];
-                float top = -INFINITY;
+                for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        y[j][e] = fmaf(x[j][e], c[e >> 1], off[e >> 1]);
-                        top = fmaxf(top, y[j][e]);
-                    }
+                        for (int i = 0; i < 2; ++i) {
+                            c[u][n][i] = fmaxf(rowf[n][i] * sc[u].x, 1.17549435e-38f);      // (never 0: a hidden score is -infinity times it)
+                            const float off = sc[u].y - m[n][i];
+                            y[u][n][i] = fmaf(x[u][n][i], c[u][n][i], off);
+                            y[u][n][2 + i] = fmaf(x[u][n][2 + i], c[u][n][i], off);
+                            top = fmaxf(top, fmaxf(y[u][n][i], y[u][n][2 + i]));
+                        }
                 if (__any_sync(0xFFFFFFFFu, top > kTop + 8.f)) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float r = fmaxf(fmaxf(y[0][2 * i], y[0][2 * i + 1]), fmaxf(y[1][2 * i], y[1][2 * i + 1]));
-                        r = fmaxf(r, __shfl_xor_sync(0xFFFFFFFFu, r, 1));
-                        r = fmaxf(r, __shfl_xor_sync(0xFFFFFFFFu, r, 2));
-                        // (against the new reference from the scores themselves: m may be the one of a row that has seen nothing)
-                        float raw = fmaxf(fmaxf(x[0][2 * i] * c[i], x[0][2 * i + 1] * c[i]), fmaxf(x[1][2 * i] * c[i], x[1][2 * i + 1] * c[i]));
-                        raw = fmaxf(raw, __shfl_xor_sync(0xFFFFFFFFu, raw, 1));
-                        raw = fmaxf(raw, __shfl_xor_sync(0xFFFFFFFFu, raw, 2));
-                        const float next = r > kTop ? raw + lvs - kTop : m[i];
-                        const float shrink = ex2(m[i] - next);
-                        m[i] = next;
-                        off[i] = lvs - next;
-                        l[i] *= shrink;
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int d = 0; d < D / 8; ++d) o[d][2 * i] *= shrink, o[d][2 * i + 1] *= shrink;
+                        for (int i = 0; i < 2; ++i) {
+                            float raw = -INFINITY;
+#pragma unroll
+                            for (int u = 0; u < SUBS; ++u) raw = fmaxf(raw, fmaxf(x[u][n][i] * c[u][n][i], x[u][n][2 + i] * c[u][n][i]) + sc[u].y);
+#pragma unroll
+                            for (int z = 4; z < 32; z <<= 1) raw = fmaxf(raw, __shfl_xor_sync(0xFFFFFFFFu, raw, z));
+                            const float next = raw - m[n][i] > kTop ? raw - kTop : m[n][i];
+                            const float shrink = ex2(m[n][i] - next);
+                            m[n][i] = next;
+                            l[n][i] *= shrink;
+#pragma unroll
+                            for (int d = 0; d < kMT; ++d) o[n][d][i] *= shrink, o[n][d][2 + i] *= shrink;
+#pragma unroll
+                            for (int u = 0; u < SUBS; ++u) {
+                                y[u][n][i] = fmaf(x[u][n][i], c[u][n][i], sc[u].y - next);
+                                y[u][n][2 + i] = fmaf(x[u][n][2 + i], c[u][n][i], sc[u].y - next);
+                            }
+                        }
+                }
+                uint32_t pb[SUBS][kTerms][NT][2];
+#pragma unroll
+                for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[u][n][e] = ex2(y[u][n][e]);
+                        l[n][0] = fmaf(y[u][n][0] + y[u][n][2], sc[u].z, l[n][0]);
+                        l[n][1] = fmaf(y[u][n][1] + y[u][n][3], sc[u].z, l[n][1]);
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            y[j][2 * i] = fmaf(x[j][2 * i], c[i], off[i]);
-                            y[j][2 * i + 1] = fmaf(x[j][2 * i + 1], c[i], off[i]);
+                            const uint32_t p = pack_f16(y[u][n][2 * j], y[u][n][2 * j + 1]);
+                            pb[u][0][n][j] = transposed(p);
+                            if constexpr (kTerms == 2) pb[u][kTerms - 1][n][j] = transposed(pack_f16_rest(y[u][n][2 * j], y[u][n][2 * j + 1], p));
                         }
                     }
+#pragma unroll
+                for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                    for (int i = 0; i < kVBytes / 4; ++i)
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {                    // elements 4 i + 2 z and the next of each key
+                            const uint32_t sel = z == 0 ? 0x5140u : 0x7362u;
+                            const uint32_t p0 = __byte_perm(vw[u][0][i], vw[u][1][i], sel), p1 = __byte_perm(vw[u][2][i], vw[u][3][i], sel);
+                            const uint32_t a0 = e4m3x2_to_f16x2(p0), a1 = e4m3x2_to_f16x2_high(p0);
+                            const uint32_t a2 = e4m3x2_to_f16x2(p1), a3 = e4m3x2_to_f16x2_high(p1);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int y2 = 0; y2 < kTerms; ++y2) mma_f16(o[n][2 * i + z], a0, a1, a2, a3, pb[u][y2][n][0], pb[u][y2][n][1]);
+                        }
+            };
+            // both halves at a time: their chains of dependent instructions overlap
+            for (int s = s0; s < s1; ++s) {
+                issue(s + 1);
+                ptx::cp_async_wait<1>();
+                __syncwarp();                             // (the scales)
+                const int get = (s - s0) & (kStages - 1), key0 = sp.lo + s * kStepKeys;
+                const bool one = s_scales[warp][get][0].w != 0.f, two = s_scales[warp][get][1].w != 0.f;
+                if (kPairs && one && two) {
+                    work(key0, get, 0, std::integral_constant<int, kPairs ? 2 : 1>{});
+                } else {
+                    if (one) work(key0, get, 0, std::integral_constant<int, 1>{});
+                    if (two) work(key0 + kHalfKeys, get, 1, std::integral_constant<int, 1>{});
                 }
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[j][e] = ex2(y[j][e]);
-                l[0] = fmaf((y[0][0] + y[0][1]) + (y[1][0] + y[1][1]), inv_vs, l[0]);
-                l[1] = fmaf((y[0][2] + y[0][3]) + (y[1][2] + y[1][3]), inv_vs, l[1]);
-                uint32_t pa[kTerms][4];
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        pa[0][2 * j + i] = pack_f16(y[j][2 * i], y[j][2 * i + 1]);
-                        if constexpr (kTwo) pa[kTerms - 1][2 * j + i] = pack_f16_rest(y[j][2 * i], y[j][2 * i + 1], pa[0][2 * j + i]);
-                    }
-#pragma unroll
-                for (int i = 0; i < kVBytes / 4; ++i)
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {                    // elements 4 i + 2 z and the next of each key
-                        const uint32_t sel = z == 0 ? 0x5140u : 0x7362u;
-                        const uint32_t p0 = __byte_perm(vw[0][i], vw[1][i], sel), p1 = __byte_perm(vw[2][i], vw[3][i], sel);
-                        const uint32_t a0 = e4m3x2_to_f16x2(p0), a1 = e4m3x2_to_f16x2(p1);
-                        const uint32_t b0 = e4m3x2_to_f16x2_high(p0), b1 = e4m3x2_to_f16x2_high(p1);
-#pragma unroll
-                        for (int y2 = 0; y2 < kTerms; ++y2) {
-                            mma_f16(o[4 * i + 2 * z], pa[y2], a0, a1);
-                            mma_f16(o[4 * i + 2 * z + 1], pa[y2], b0, b1);
-                        }
-                    }
+                __syncwarp();
             }
             ptx::cp_async_wait<0>();
 
-            // ---- the result, or a piece of it
+            // ---- the four warps' parts become one: everybody's values by the largest reference, through the ring
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], 1);
-                l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], 2);
-            }
-            const bool begins = first == 0, ends = last == sp.steps;
-            if (begins && ends) {
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    if (g + 8 * i >= n_rows) continue;
-                    const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
-                    float r[D / 4];
 #pragma unroll
-                    for (int d = 0; d < D / 8; ++d) r[d] = o[d][2 * i] * inv, r[D / 8 + d] = o[d][2 * i + 1] * inv;
-                    store_run<T, D>(static_cast<T*>(a.out) + out_row[i] * a.ldo + (int64_t)out_head[i] * D + t * (D / 4), r);
-                    if (a.lse != nullptr && t == 0)
-                        a.lse[out_row[i] * a.heads + out_head[i]] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.69314718056f;
+                    for (int z = 4; z < 32; z <<= 1) l[n][i] += __shfl_xor_sync(0xFFFFFFFFu, l[n][i], z);
+                    if (g == 0) s_m[warp][8 * n + 2 * t + i] = m[n][i], s_l[warp][8 * n + 2 * t + i] = l[n][i];
                 }
-            } else {
-                float* slot = slots + (2 * w + (begins ? 1 : 0)) * (int64_t)slot_floats(D);
-                if (begins) {
-                    cut.b = b, cut.row_tile = tile, cut.head = head;
-                    cut.pieces = (int32_t)((unit_at + sp.steps - 1) / share - w + 1);
-                }
+            __syncthreads();
+            float* const rows = reinterpret_cast<float*>(ring);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int row = g + 8 * i;
+                    const int row = 8 * n + 2 * t + i;
                     if (row >= n_rows) continue;
-                    float r[D / 4];
+                    float top = s_m[0][row];
 #pragma unroll
-                    for (int d = 0; d < D / 8; ++d) r[d] = o[d][2 * i], r[D / 8 + d] = o[d][2 * i + 1];
-                    store_run<float, D>(slot + 2 * kRows + row * D + t * (D / 4), r);
-                    if (t == 0) slot[row] = m[i], slot[kRows + row] = l[i];
+                    for (int z = 1; z < kWarpsPerCta; ++z) top = fmaxf(top, s_m[z][row]);
+                    const float f = ex2(m[n][i] - top);
+                    float r[kVBytes];
+#pragma unroll
+                    for (int d = 0; d < kMT; ++d) r[2 * d] = o[n][d][i] * f, r[2 * d + 1] = o[n][d][2 + i] * f;
+                    store_run<float, kVBytes>(rows + row * D + g * kVBytes, r);
+                }
+            __syncthreads();
+            const bool begins = first == 0, ends = last == sp.steps, whole = begins && ends;
+            float* slot = slots + (2 * w + (begins ? 1 : 0)) * (int64_t)slot_floats(kRows, D);
+            if (begins && !ends) {
+                cut.b = b, cut.row_tile = tile, cut.head = head;
+                cut.pieces = (int32_t)((unit_at + sp.steps - 1) / share - w + 1);
+            }
+            for (int i = tid; i < n_rows * (D / 4); i += kThreads) {
+                const int row = i / (D / 4), d = i % (D / 4) * 4;
+                float top = s_m[0][row], sum = 0.f;
+#pragma unroll
+                for (int z = 1; z < kWarpsPerCta; ++z) top = fmaxf(top, s_m[z][row]);
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int z = 0; z < kWarpsPerCta; ++z) {
+                    sum = fmaf(s_l[z][row], ex2(s_m[z][row] - top), sum);
+                    const float4 x = *reinterpret_cast<const float4*>(ring_all + z * kStages * 2 * Sh::kHalfBytes + (row * D + d) * 4);
+                    v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+                }
+                if (whole) {
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    const int token = token_of(row), qh = head * group + (tile_row + row - token * group);
+                    const int64_t orow = (int64_t)sq.row0 + token;
+                    store4(static_cast<T*>(a.out) + orow * a.ldo + (int64_t)qh * D + d, v, inv);
+                    if (a.lse != nullptr && d == 0) a.lse[orow * a.heads + qh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718056f;
+                } else {
+                    *reinterpret_cast<float4*>(slot + 2 * kRows + row * D + d) = v;
+                    if (d == 0) slot[row] = top, slot[kRows + row] = sum;
                 }
             }
+            __syncthreads();
         }
     }
-    if (lane == 0) cuts[w] = cut;
+    if (tid == 0) cuts[w] = cut;
 }
 
-// Joins the pieces of the unit that begins in share blockIdx.x and goes on behind it: with M the largest reference, the sum of
-// 2^(m - M) (values, sum) over the pieces.  A warp takes a row, or a row's every k-th piece where there are fewer rows than warps.
+// Joins the pieces of the units that are cut: with M the largest reference, the sum of 2^(m - M) (values, sum) over the pieces,
+// in the order of the keys.  A CTA looks after 8 rows of the unit that begins in share blockIdx.x and goes on behind it: a warp per row,
+// or several that split the pieces among them.
 constexpr int kJoinWarps = 8;
-template <typename T, int D>
+template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __grid_constant__ AttendArgs a, const CutUnit* __restrict__ cuts,
                                                                      const float* __restrict__ slots)
 {
-    constexpr int E = D / 32;                              // elements per lane
-    __shared__ float part[kJoinWarps][D];
+    constexpr int kRows = 8 * NT, kLanes = D / 4;          // lanes of four elements
+    __shared__ float4 part[kJoinWarps][kLanes];
     ptx::grid_dependency_sync();
-    const int4 c4 = __ldcg(reinterpret_cast<const int4*>(cuts + blockIdx.x));
-    const CutUnit cut{c4.x, c4.y, c4.z, c4.w};
-    if (cut.pieces == 0) return;
+    const int4 cut = __ldcg(reinterpret_cast<const int4*>(cuts + blockIdx.x));          // sequence, row tile, head, pieces
+    if (cut.w == 0) return;
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const int group = a.heads / a.c.kv_heads;
-    const Sequence sq = sequence_of(a.c, cut.b, a.N);
-    const int rows = (int)min((int64_t)kRows, (int64_t)sq.n * group - (int64_t)cut.row_tile * kRows);
-    const int split = rows >= kJoinWarps ? 1 : kJoinWarps / rows;              // warps per row
+    const Sequence sq = sequence_of(a.c, cut.x, a.N);
+    const int rows = (int)min((int64_t)kRows, (int64_t)sq.n * group - (int64_t)cut.y * kRows) - 8 * (int)blockIdx.y;
+    if (rows <= 0) return;
+    const int split = rows >= kJoinWarps ? 1 : kJoinWarps / rows;                       // warps per row
+    const int row = 8 * (int)blockIdx.y + warp / split, sub = warp % split;
+    const bool on = warp / split < min(rows, kJoinWarps);
     const int64_t w0 = blockIdx.x;
-    auto slot = [&](int p) { return slots + (p == 0 ? 2 * w0 + 1 : 2 * (w0 + p)) * (int64_t)slot_floats(D); };
-    for (int r0 = 0; r0 < rows; r0 += kJoinWarps / split) {
-        const int row = r0 + warp / split, sub = warp % split;
-        const bool on = row < rows && warp < kJoinWarps / split * split;
-        float M = kNone, L = 0.f, acc[E];
+    auto slot = [&](int p) { return slots + (p == 0 ? 2 * w0 + 1 : 2 * (w0 + p)) * (int64_t)slot_floats(kRows, D); };
+    float M = kNone, L = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (on) {
+        for (int p = lane; p < cut.w; p += 32) M = fmaxf(M, __ldcg(slot(p) + row));
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = 0.f;
-        if (on) {
-            for (int p = lane; p < cut.pieces; p += 32) M = fmaxf(M, __ldcg(slot(p) + row));
+        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
+        for (int p = lane; p < cut.w; p += 32) L += __ldcg(slot(p) + kRows + row) * ex2(__ldcg(slot(p) + row) - M);
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
-            for (int p = lane; p < cut.pieces; p += 32) L += __ldcg(slot(p) + kRows + row) * ex2(__ldcg(slot(p) + row) - M);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
+        for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
+        if (lane < kLanes) {
 #pragma unroll 8
-            for (int p = sub; p < cut.pieces; p += split) {
+            for (int p = sub; p < cut.w; p += split) {
                 const float f = ex2(__ldcg(slot(p) + row) - M);
-                const float* v = slot(p) + 2 * kRows + row * D + lane * E;
-                if constexpr (E == 4) {
-                    const float4 x = __ldcg(reinterpret_cast<const float4*>(v));
-                    acc[0] = fmaf(x.x, f, acc[0]), acc[1] = fmaf(x.y, f, acc[1]), acc[2] = fmaf(x.z, f, acc[2]), acc[3] = fmaf(x.w, f, acc[3]);
-                } else {
-                    const float2 x = __ldcg(reinterpret_cast<const float2*>(v));
-                    acc[0] = fmaf(x.x, f, acc[0]), acc[1] = fmaf(x.y, f, acc[1]);
-                }
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(slot(p) + 2 * kRows + row * D + lane * 4));
+                acc.x = fmaf(x.x, f, acc.x), acc.y = fmaf(x.y, f, acc.y), acc.z = fmaf(x.z, f, acc.z), acc.w = fmaf(x.w, f, acc.w);
             }
-        }
-        if (split > 1) {
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < E; ++e) part[warp][lane * E + e] = acc[e];
-            __syncthreads();
-            if (on && sub == 0)
-                for (int z = 1; z < split; ++z)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) acc[e] += part[warp + z][lane * E + e];
-        }
-        if (on && sub == 0) {
-            const int64_t r = (int64_t)cut.row_tile * kRows + row, token = r / group;
-            const int64_t orow = sq.row0 + token;
-            const int oh = cut.head * group + (int)(r - token * group);
-            const float inv = L == 0.f ? 0.f : 1.f / L;
-            T* out = static_cast<T*>(a.out) + orow * a.ldo + (int64_t)oh * D + lane * E;
-            if constexpr (sizeof(T) == 4) {
-                if constexpr (E == 4) *reinterpret_cast<float4*>(out) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-                else *reinterpret_cast<float2*>(out) = make_float2(acc[0] * inv, acc[1] * inv);
-            } else {
-                if constexpr (E == 4)
-                    *reinterpret_cast<uint2*>(out) = make_uint2(f32x2_to_bf16x2(acc[0] * inv, acc[1] * inv), f32x2_to_bf16x2(acc[2] * inv, acc[3] * inv));
-                else *reinterpret_cast<uint32_t*>(out) = f32x2_to_bf16x2(acc[0] * inv, acc[1] * inv);
-            }
-            if (a.lse != nullptr && lane == 0) a.lse[orow * a.heads + oh] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718056f;
         }
     }
+    if (split > 1) {                                       // (the same in all threads)
+        if (lane < kLanes) part[warp][lane] = acc;
+        __syncthreads();
+    }
+    if (!on || sub != 0 || lane >= kLanes) return;
+    for (int z = 1; z < split; ++z) {
+        const float4 x = part[warp + z][lane];
+        acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
+    }
+    const int r = cut.y * kRows + row, token = r / group;
+    const int64_t orow = (int64_t)sq.row0 + token;
+    const int oh = cut.z * group + (r - token * group);
+    store4(static_cast<T*>(a.out) + orow * a.ldo + (int64_t)oh * D + lane * 4, acc, L == 0.f ? 0.f : 1.f / L);
+    if (a.lse != nullptr && lane == 0) a.lse[orow * a.heads + oh] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718056f;
 }
 
-int64_t worker_count() { return (int64_t)sm_count() * kCtasPerSm * kWarpsPerCta; }
+template <typename T, int D, int NT>
+int64_t worker_count() { return (int64_t)sm_count() * Shape<T, D, NT>::kCtas * kWaves; }
 
-template <typename T, int D>
+template <typename T, int D, int NT>
+size_t bytes_needed()
+{
+    const int64_t n = worker_count<T, D, NT>();
+    return cut_bytes(n) + (size_t)(2 * n * slot_floats(8 * NT, D)) * sizeof(float);
+}
+
+template <typename T, int D, int NT>
 molora_status_t launch(const AttendArgs& a, void* ws, cudaStream_t s)
 {
-    constexpr int kStageBytes = 32 * (2 * (D / 64) * 16 + 4 * (D / 8));
-    constexpr size_t smem = (size_t)kWarpsPerCta * kStages * kStageBytes;
+    using Sh = Shape<T, D, NT>;
     static bool ready[kMaxDevices] = {};
     bool& done = ready[device_slot()];
     if (!done) {
-        if (cudaFuncSetAttribute(attend_rows_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return MOLORA_ERR_CUDA;
+        if (cudaFuncSetAttribute(attend_rows_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Sh::kSmem) != cudaSuccess) return MOLORA_ERR_CUDA;
         done = true;
     }
-    const int ctas = sm_count() * (sizeof(T) == 2 ? kCtasPerSm : 2);
-    const int workers = ctas * kWarpsPerCta;
+    const int workers = (int)worker_count<T, D, NT>();
     CutUnit* cuts = static_cast<CutUnit*>(ws);
-    float* slots = reinterpret_cast<float*>(static_cast<char*>(ws) + cut_bytes(worker_count()));
-    cudaError_t e = launch_kernel(attend_rows_kernel<T, D>, dim3((unsigned)ctas), dim3(kThreads), smem, s, 1, true, a, cuts, slots);
-    if (e != cudaSuccess) return MOLORA_ERR_CUDA;
-    return cuda_ok(launch_kernel(attend_join_kernel<T, D>, dim3((unsigned)workers), dim3(kJoinWarps * 32), 0, s, 1, true, a,
+    float* slots = reinterpret_cast<float*>(static_cast<char*>(ws) + cut_bytes(workers));
+    if (launch_kernel(attend_rows_kernel<T, D, NT>, dim3((unsigned)workers), dim3(kThreads), Sh::kSmem, s, 1, true, a, cuts, slots) != cudaSuccess)
+        return MOLORA_ERR_CUDA;
+    return cuda_ok(launch_kernel(attend_join_kernel<T, D, NT>, dim3((unsigned)workers, NT), dim3(kJoinWarps * 32), 0, s, 1, true, a,
                                  static_cast<const CutUnit*>(cuts), static_cast<const float*>(slots)));
 }
 
+// f<T, D, NT>() of the variant for these rows: as few 8-row tiles as hold the rows that share a key / value head in the longest sequence, at most 4
+// (2 for fp32, whose terms take the registers)
+template <typename T, int D, typename F>
+auto for_tiles(int64_t rows, F f)
+{
+    if (rows <= 8) return f.template operator()<T, D, 1>();
+    if (rows <= 16 || sizeof(T) == 4) return f.template operator()<T, D, 2>();
+    if constexpr (sizeof(T) == 2) {
+        if (rows <= 24) return f.template operator()<T, D, 3>();
+        return f.template operator()<T, D, kMaxTiles>();
+    }
+    return f.template operator()<T, D, 2>();
+}
+template <typename F>
+auto for_variant(molora_dtype_t dt, int32_t dim, int64_t rows, F f)
+{
+    if (dt == MOLORA_F32) return dim == 64 ? for_tiles<float, 64>(rows, f) : for_tiles<float, 128>(rows, f);
+    return dim == 64 ? for_tiles<__nv_bfloat16, 64>(rows, f) : for_tiles<__nv_bfloat16, 128>(rows, f);
+}
+struct BytesNeeded {
+    template <typename T, int D, int NT>
+    size_t operator()() const { return bytes_needed<T, D, NT>(); }
+};
+struct Launch {
+    const AttendArgs& a;
+    void* ws;
+    cudaStream_t s;
+    template <typename T, int D, int NT>
+    molora_status_t operator()() const { return launch<T, D, NT>(a, ws, s); }
+};
+
 }  // namespace
 
-size_t attend_rows_workspace_bytes(int32_t dim) { return cut_bytes(worker_count()) + (size_t)(2 * worker_count() * slot_floats(dim)) * sizeof(float); }
+size_t attend_rows_workspace_bytes(molora_dtype_t dt, int32_t dim, int64_t rows) { return for_variant(dt, dim, rows, BytesNeeded{}); }
 
-molora_status_t launch_attend_rows(const AttendArgs& a, molora_dtype_t dt, void* ws, cudaStream_t s)
+molora_status_t launch_attend_rows(const AttendArgs& a, molora_dtype_t dt, int64_t rows, void* ws, cudaStream_t s)
 {
-    if (a.c.dim == 64) return dt == MOLORA_F32 ? launch<float, 64>(a, ws, s) : launch<__nv_bfloat16, 64>(a, ws, s);
-    return dt == MOLORA_F32 ? launch<float, 128>(a, ws, s) : launch<__nv_bfloat16, 128>(a, ws, s);
+    return for_variant(dt, a.c.dim, rows, Launch{a, ws, s});
 }
 
 }  // namespace molora
