@@ -1,4 +1,5 @@
 // C ABI of the paged cache and of draft verification: argument validation on the host, then enqueue.
+#include <algorithm>
 #include <cmath>
 
 #include "kv_cache.cuh"
@@ -74,7 +75,10 @@ molora_status_t molora_kv_append(const molora_kv_cache_t* cache, const molora_se
 size_t molora_kv_attend_workspace_bytes(molora_dtype_t dt, int32_t heads, int32_t kv_heads, int32_t dim, int64_t max_tokens)
 {
     if ((dim != 64 && dim != 128) || kv_heads < 1 || heads < 1 || heads % kv_heads != 0 || max_tokens < 1 || (dt != MOLORA_F32 && dt != MOLORA_BF16)) return 0;
-    return attend_rows_workspace_bytes(dt, dim, max_tokens * (heads / kv_heads));
+    // (the choice of kernel depends on the pool too, which is not known here)
+    const int64_t rows = max_tokens * (heads / kv_heads);
+    const size_t stream = dt == MOLORA_BF16 && dim == 128 && rows <= 32 ? attend_stream_workspace_bytes(rows) : 0;
+    return std::max(stream, attend_rows_workspace_bytes(dt, dim, rows));
 }
 
 molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_sequences_t* seqs, molora_dtype_t dt, int64_t N, const void* q,
@@ -97,7 +101,9 @@ molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_se
     a.heads = heads, a.causal = causal != 0, a.window = window;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.dev_status = dev_status;
-    return launch_attend_rows(a, dt, max_tokens * (heads / cache->kv_heads), ws, static_cast<cudaStream_t>(stream));
+    const int64_t rows = max_tokens * (heads / cache->kv_heads);
+    if (attend_stream_eligible(a.c, dt, rows)) return launch_attend_stream(a, rows, ws, static_cast<cudaStream_t>(stream));
+    return launch_attend_rows(a, dt, rows, ws, static_cast<cudaStream_t>(stream));
 }
 
 molora_status_t molora_verify_drafts(const void* target, int64_t target_ld_seq, int64_t target_ld, const void* draft, int64_t draft_ld_seq,

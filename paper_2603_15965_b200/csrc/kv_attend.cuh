@@ -1,0 +1,210 @@
+// What the attention kernels over the paged cache share: units, their equal shares, what a cut unit leaves behind, the join.
+//
+// A row of a sequence is (new token, query head of the group that shares a key / value head); ROWS consecutive rows, one key /
+// value head and the keys that they see are a UNIT.  The units' keys, cut into steps of KEYS, form one long list; every CTA of the
+// grid takes an equal, contiguous share of it, whatever the lengths of the sequences.  A unit that lies inside one share is written at
+// once; one that is cut leaves its pieces (sum, reference, weighted values, all fp32) in the workspace, and a second kernel joins
+// them in the order of the keys: results do not depend on timing.
+#pragma once
+#include "kv_cache.cuh"
+
+namespace molora {
+namespace {
+
+constexpr float kNone = -1e30f;              // reference of a row that has seen nothing
+
+// What a cut unit leaves behind.
+struct CutUnit {
+    int32_t b, row_tile, head, pieces;       // pieces 0: no unit begins in this share and goes on in the next
+};
+__host__ __device__ constexpr int slot_floats(int rows, int dim) { return 2 * rows + rows * dim; }
+__host__ __device__ inline size_t cut_bytes(int64_t workers) { return (size_t)((workers * (int64_t)sizeof(CutUnit) + 255) / 256 * 256); }
+
+// steps of every unit of a sequence, and where its keys begin
+struct Span {
+    int32_t lo;        // first key, a multiple of KEYS
+    int32_t steps;     // per unit
+    int32_t tiles;     // of rows
+};
+template <int ROWS, int KEYS>
+__device__ __forceinline__ Span span_of(const Sequence& s, int group, int window)
+{
+    Span r{0, 0, 0};
+    if (s.n == 0) return r;
+    r.lo = window > 0 ? max(0, s.first_pos() - window + 1) & ~(KEYS - 1) : 0;
+    r.steps = max(1, (s.len - r.lo + KEYS - 1) / KEYS);
+    r.tiles = (int32_t)(((int64_t)s.n * group + ROWS - 1) / ROWS);
+    return r;
+}
+
+// A unit, and what of its keys lies in this share.
+struct Unit {
+    Sequence sq;
+    Span sp;
+    int64_t at;                             // its first step in the list
+    int32_t b, head, tile, first, last;     // its steps [first, last) are in this share
+    int32_t n_rows, tile_row;
+    int32_t hi_min, hi_max, lo_min, lo_max; // keys below hi_min and from lo_max on are seen by every row, [lo_min, hi_max) by some
+    int32_t u0, u1;                         // the steps of the share that some row sees
+};
+__device__ __forceinline__ int upper_key(const AttendArgs& a, const Sequence& sq, int token)
+{
+    return a.causal ? max(0, min(sq.first_pos() + token + 1, sq.len)) : sq.len;
+}
+__device__ __forceinline__ int lower_key(const AttendArgs& a, const Sequence& sq, int token)
+{
+    return a.window > 0 ? max(0, sq.first_pos() + token - a.window + 1) : 0;
+}
+
+// The units of a share, in order; every thread (or warp) that asks gets the same.
+template <int ROWS, int KEYS>
+struct Walk {
+    const AttendArgs& a;
+    int64_t at, stop, base;                 // next step, end of the share, first step of sequence b
+    int64_t share;
+    int b, group;
+    Sequence sq;
+    Span sp;
+    __device__ explicit Walk(const AttendArgs& args) : a(args), at(0), stop(0), base(0), share(1), b(0), group(args.heads / args.c.kv_heads) {}
+
+    __device__ void load()
+    {
+        sq = sequence_of(a.c, b, a.N);
+        sp = span_of<ROWS, KEYS>(sq, group, a.window);
+    }
+    __device__ bool next(Unit& u)
+    {
+        if (at >= stop) return false;
+        while (base + (int64_t)sp.steps * sp.tiles * a.c.kv_heads <= at) {
+            base += (int64_t)sp.steps * sp.tiles * a.c.kv_heads;
+            ++b;
+            load();
+        }
+        const int64_t unit = (at - base) / sp.steps;
+        u.sq = sq, u.sp = sp, u.b = b;
+        u.at = base + unit * sp.steps;
+        u.first = (int)(at - u.at), u.last = (int)min((int64_t)sp.steps, stop - u.at);
+        u.head = (int)(unit % a.c.kv_heads), u.tile = (int)(unit / a.c.kv_heads);
+        u.tile_row = u.tile * ROWS;
+        u.n_rows = (int)min((int64_t)ROWS, (int64_t)sq.n * group - u.tile_row);
+        at = u.at + u.last;
+        const int t0 = u.tile_row / group, t1 = (u.tile_row + u.n_rows - 1) / group;
+        u.hi_min = upper_key(a, sq, t0), u.hi_max = upper_key(a, sq, t1);
+        u.lo_min = lower_key(a, sq, t0), u.lo_max = lower_key(a, sq, t1);
+        u.u0 = max(u.first, (u.lo_min - sp.lo) / KEYS);
+        u.u1 = min(u.last, u.hi_max > sp.lo ? (u.hi_max - sp.lo + KEYS - 1) / KEYS : 0);
+        return true;
+    }
+    // the shares in which the unit lies, from this one (w), where it begins, on
+    __device__ int32_t pieces(const Unit& u, int64_t w) const { return (int32_t)((u.at + u.sp.steps - 1) / share - w + 1); }
+};
+
+// Puts `walk` at the beginning of share w of `shares`.  All THREADS threads of the CTA call it; s_upto: THREADS words.
+template <int THREADS, int ROWS, int KEYS>
+__device__ __forceinline__ void begin_share(Walk<ROWS, KEYS>& walk, int64_t w, int64_t shares, int min_share, int64_t* s_upto)
+{
+    const AttendArgs& a = walk.a;
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int part = (a.c.B + THREADS - 1) / THREADS;
+    int64_t incl = 0;
+    for (int b = tid * part; b < min(a.c.B, (tid + 1) * part); ++b) {
+        const Sequence sq = sequence_of(a.c, b, a.N);
+        const Span sp = span_of<ROWS, KEYS>(sq, walk.group, a.window);
+        incl += (int64_t)sp.steps * sp.tiles * a.c.kv_heads;
+        if (sq.bad && w == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += up;
+    }
+    if (lane == 31) s_upto[tid] = incl;
+    __syncthreads();
+    for (int z = 0; z < warp; ++z) incl += s_upto[32 * z + 31];
+    __syncthreads();
+    s_upto[tid] = incl;                     // steps of the sequences up to the end of this thread's part
+    __syncthreads();
+    const int64_t total = s_upto[THREADS - 1];
+    walk.share = max((total + shares - 1) / shares, (int64_t)min_share);
+    walk.at = w * walk.share;
+    walk.stop = min(total, walk.at + walk.share);
+    if (walk.at >= walk.stop) return;
+    int lo = 0, hi = THREADS - 1;           // the part in which the share begins
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (s_upto[mid] > walk.at) hi = mid;
+        else lo = mid + 1;
+    }
+    walk.b = lo * part;
+    walk.base = lo > 0 ? s_upto[lo - 1] : 0;
+    walk.load();
+}
+
+// scales of v outside [2^-100, 2^100] are read as its ends
+__device__ __forceinline__ float clamped_scale(float v) { return fminf(fmaxf(v, 7.8886090522e-31f), 1.2676506002e30f); }
+
+__device__ __forceinline__ void store4(float* p, float4 v, float f) { *reinterpret_cast<float4*>(p) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f); }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v, float f)
+{
+    *reinterpret_cast<uint2*>(p) = make_uint2(f32x2_to_bf16x2(v.x * f, v.y * f), f32x2_to_bf16x2(v.z * f, v.w * f));
+}
+
+// Joins the pieces of the units that are cut: with M the largest reference, the sum of 2^(m - M) (values, sum) over the pieces,
+// in the order of the keys.  A CTA looks after 8 rows of the unit that begins in share blockIdx.x and goes on behind it: a warp per row,
+// or several that split the pieces among them.
+constexpr int kJoinWarps = 8;
+template <typename T, int D, int ROWS>
+__global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __grid_constant__ AttendArgs a, const CutUnit* __restrict__ cuts,
+                                                                     const float* __restrict__ slots)
+{
+    constexpr int kRows = ROWS, kLanes = D / 4;          // lanes of four elements
+    __shared__ float4 part[kJoinWarps][kLanes];
+    ptx::grid_dependency_sync();
+    const int4 cut = __ldcg(reinterpret_cast<const int4*>(cuts + blockIdx.x));          // sequence, row tile, head, pieces
+    if (cut.w == 0) return;
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+    const int group = a.heads / a.c.kv_heads;
+    const Sequence sq = sequence_of(a.c, cut.x, a.N);
+    const int rows = (int)min((int64_t)kRows, (int64_t)sq.n * group - (int64_t)cut.y * kRows) - 8 * (int)blockIdx.y;
+    if (rows <= 0) return;
+    const int split = rows >= kJoinWarps ? 1 : kJoinWarps / rows;                       // warps per row
+    const int row = 8 * (int)blockIdx.y + warp / split, sub = warp % split;
+    const bool on = warp / split < min(rows, kJoinWarps);
+    const int64_t w0 = blockIdx.x;
+    auto slot = [&](int p) { return slots + (p == 0 ? 2 * w0 + 1 : 2 * (w0 + p)) * (int64_t)slot_floats(kRows, D); };
+    float M = kNone, L = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (on) {
+        for (int p = lane; p < cut.w; p += 32) M = fmaxf(M, __ldcg(slot(p) + row));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
+        for (int p = lane; p < cut.w; p += 32) L += __ldcg(slot(p) + kRows + row) * ex2(__ldcg(slot(p) + row) - M);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
+        if (lane < kLanes) {
+#pragma unroll 8
+            for (int p = sub; p < cut.w; p += split) {
+                const float f = ex2(__ldcg(slot(p) + row) - M);
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(slot(p) + 2 * kRows + row * D + lane * 4));
+                acc.x = fmaf(x.x, f, acc.x), acc.y = fmaf(x.y, f, acc.y), acc.z = fmaf(x.z, f, acc.z), acc.w = fmaf(x.w, f, acc.w);
+            }
+        }
+    }
+    if (split > 1) {                                       // (the same in all threads)
+        if (lane < kLanes) part[warp][lane] = acc;
+        __syncthreads();
+    }
+    if (!on || sub != 0 || lane >= kLanes) return;
+    for (int z = 1; z < split; ++z) {
+        const float4 x = part[warp + z][lane];
+        acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
+    }
+    const int r = cut.y * kRows + row, token = r / group;
+    const int64_t orow = (int64_t)sq.row0 + token;
+    const int oh = cut.z * group + (r - token * group);
+    store4(static_cast<T*>(a.out) + orow * a.ldo + (int64_t)oh * D + lane * 4, acc, L == 0.f ? 0.f : 1.f / L);
+    if (a.lse != nullptr && lane == 0) a.lse[orow * a.heads + oh] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718056f;
+}
+
+}  // namespace
+}  // namespace molora

@@ -24,7 +24,7 @@
 // What bounds it: the codes, 2 D bytes per (key, key / value head), from HBM.
 #include <type_traits>
 
-#include "kv_cache.cuh"
+#include "kv_attend.cuh"
 
 namespace molora {
 namespace {
@@ -34,7 +34,6 @@ constexpr int kHalfKeys = 16, kStepKeys = 32;  // keys of a tensor instruction, 
 constexpr int kMinShare = 4;                 // steps of a CTA: shorter shares cost more in joining than they save
 constexpr int kWaves = 2;                    // shares per resident CTA
 constexpr int kMaxTiles = 4;                 // 8-row tiles of a unit
-constexpr float kNone = -1e30f;              // reference of a row that has seen nothing
 constexpr float kTop = 7.f;                  // weight of a row's largest score when the reference is set: 2^7
 
 // CTAs per SM by what a thread holds (accumulators D / 4 NT, fragments of q D / 8 NT per term), and copies in flight per warp
@@ -49,13 +48,6 @@ struct Shape {
     static constexpr size_t kSmem = (size_t)kWarpsPerCta * kStages * 2 * kHalfBytes;      // (and 8 NT rows of fp32 values per warp fit it)
     static_assert(kStages * 2 * kHalfBytes >= 8 * NT * D * 4, "a warp's share of the ring holds its rows");
 };
-
-// What a cut unit leaves behind.
-struct CutUnit {
-    int32_t b, row_tile, head, pieces;       // pieces 0: no unit begins in this share and goes on in the next
-};
-__host__ __device__ constexpr int slot_floats(int rows, int dim) { return 2 * rows + rows * dim; }
-__host__ __device__ inline size_t cut_bytes(int64_t workers) { return (size_t)((workers * (int64_t)sizeof(CutUnit) + 255) / 256 * 256); }
 
 __device__ __forceinline__ void mma_f16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -88,23 +80,6 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src)
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// steps of every unit of a sequence, and where its keys begin
-struct Span {
-    int32_t lo;        // first key, a multiple of 32
-    int32_t steps;     // of 32 keys, per unit
-    int32_t tiles;     // row tiles
-};
-template <int ROWS>
-__device__ __forceinline__ Span span_of(const Sequence& s, int group, int window)
-{
-    Span r{0, 0, 0};
-    if (s.n == 0) return r;
-    r.lo = window > 0 ? max(0, s.first_pos() - window + 1) & ~(kStepKeys - 1) : 0;
-    r.steps = max(1, (s.len - r.lo + kStepKeys - 1) / kStepKeys);
-    r.tiles = (int32_t)(((int64_t)s.n * group + ROWS - 1) / ROWS);
-    return r;
-}
-
 template <typename T>
 __device__ __forceinline__ void load16(const T* p, float* x)
 {
@@ -119,12 +94,6 @@ __device__ __forceinline__ void store_run(T* p, const float* x)          // N ne
     constexpr int E = VecTraits<T>::kElems;
 #pragma unroll
     for (int i = 0; i < N / E; ++i) stg128(p + i * E, pack<T>(x + i * E));
-}
-
-__device__ __forceinline__ void store4(float* p, float4 v, float f) { *reinterpret_cast<float4*>(p) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f); }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v, float f)
-{
-    *reinterpret_cast<uint2*>(p) = make_uint2(f32x2_to_bf16x2(v.x * f, v.y * f), f32x2_to_bf16x2(v.z * f, v.w * f));
 }
 
 template <typename T, int D, int NT>
@@ -151,74 +120,23 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
     uint8_t* const ring = ring_all + warp * kStages * 2 * Sh::kHalfBytes;
     const uint32_t ring_at = ptx::smem_u32(ring);
 
-    // ---- the shares
-    const int part = (a.c.B + kThreads - 1) / kThreads;
-    int64_t mine = 0;
-    for (int b = tid * part; b < min(a.c.B, (tid + 1) * part); ++b) {
-        const Sequence sq = sequence_of(a.c, b, a.N);
-        const Span sp = span_of<kRows>(sq, group, a.window);
-        mine += (int64_t)sp.steps * sp.tiles * a.c.kv_heads;
-        if (sq.bad && blockIdx.x == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
-    }
-    {
-        int64_t incl = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-            if (lane >= o) incl += up;
-        }
-        if (lane == 31) s_upto[tid] = incl;
-        __syncthreads();
-        for (int w = 0; w < warp; ++w) incl += s_upto[32 * w + 31];
-        __syncthreads();
-        s_upto[tid] = incl;
-        __syncthreads();
-    }
-    const int64_t total = s_upto[kThreads - 1];
-    const int64_t workers = gridDim.x, w = blockIdx.x;
-    const int64_t share = max((total + workers - 1) / workers, (int64_t)kMinShare);
-    int64_t at = w * share;
-    const int64_t stop = min(total, at + share);
+    const int64_t w = blockIdx.x;
+    Walk<kRows, kStepKeys> walk(a);
+    begin_share<kThreads>(walk, w, gridDim.x, kMinShare, s_upto);
     CutUnit cut{0, 0, 0, 0};
-    if (at < stop) {
-        // the sequence in which the share begins
-        int lo = 0, hi = kThreads - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (s_upto[mid] > at) hi = mid;
-            else lo = mid + 1;
-        }
-        int b = lo * part;
-        int64_t base = lo > 0 ? s_upto[lo - 1] : 0;      // first step of sequence b
-        Sequence sq = sequence_of(a.c, b, a.N);
-        Span sp = span_of<kRows>(sq, group, a.window);
-        while (at < stop) {
-            while (base + (int64_t)sp.steps * sp.tiles * a.c.kv_heads <= at) {
-                base += (int64_t)sp.steps * sp.tiles * a.c.kv_heads;
-                sq = sequence_of(a.c, ++b, a.N);
-                sp = span_of<kRows>(sq, group, a.window);
-            }
-            const int64_t unit = (at - base) / sp.steps;
-            const int64_t unit_at = base + unit * sp.steps;                 // its first step
-            const int first = (int)(at - unit_at), last = (int)min((int64_t)sp.steps, stop - unit_at);
-            const int head = (int)(unit % a.c.kv_heads), tile = (int)(unit / a.c.kv_heads);
-            at = unit_at + last;
-
-            // ---- the rows of the unit
-            const int n_rows = (int)min((int64_t)kRows, (int64_t)sq.n * group - (int64_t)tile * kRows);
-            const int tile_row = tile * kRows;
+    Unit un;
+    while (walk.next(un)) {
+        {
+            const Sequence& sq = un.sq;
+            const int lo0 = un.sp.lo, head = un.head, n_rows = un.n_rows, tile_row = un.tile_row;
+            const int hi_min = un.hi_min, hi_max = un.hi_max, lo_min = un.lo_min, lo_max = un.lo_max;
             auto token_of = [&](int r) { return (tile_row + min(r, n_rows - 1)) / group; };
-            auto upper = [&](int token) { return a.causal ? max(0, min(sq.first_pos() + token + 1, sq.len)) : sq.len; };
-            auto lower = [&](int token) { return a.window > 0 ? max(0, sq.first_pos() + token - a.window + 1) : 0; };
-            const int tok_lo = token_of(0), tok_hi = token_of(n_rows - 1);
-            const int hi_min = upper(tok_lo), hi_max = upper(tok_hi), lo_min = lower(tok_lo), lo_max = lower(tok_hi);
 
             // ---- its steps that some row sees, a contiguous part of them for each warp; the first come in while q does
-            const int u0 = max(first, (lo_min - sp.lo) / kStepKeys);
-            const int u1 = min(last, hi_max > sp.lo ? (hi_max - sp.lo + kStepKeys - 1) / kStepKeys : 0);
+            const int u0 = un.u0, u1 = un.u1;
             const int per_warp = (max(u1 - u0, 0) + kWarpsPerCta - 1) / kWarpsPerCta;
             const int s0 = u0 + warp * per_warp, s1 = min(u1, s0 + per_warp);
-            const int32_t* table = a.c.table + (int64_t)b * a.c.ld_table;
+            const int32_t* table = a.c.table + (int64_t)un.b * a.c.ld_table;
             int group0 = -1;                              // first of the 32 pages whose ids and scales the lanes hold
             int32_t page_id = -1;
             float page_ks = 0.f, page_lvs = 0.f, page_inv = 0.f;
@@ -233,7 +151,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
                     } else {
                         const int64_t block = (int64_t)page_id * a.c.kv_heads + head;
                         page_ks = ptx::ld_dependent(a.c.k_scale + block);
-                        const float vs = fminf(fmaxf(ptx::ld_dependent(a.c.v_scale + block), 7.8886090522e-31f), 1.2676506002e30f);      // 2^-100, 2^100
+                        const float vs = clamped_scale(ptx::ld_dependent(a.c.v_scale + block));
                         page_lvs = log2f(vs), page_inv = 1.f / vs;
                     }
                 }
@@ -253,7 +171,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
             };
             auto issue = [&](int s) {
                 if (s < s1) {
-                    const int key = sp.lo + s * kStepKeys, page = key >> plog, put = (s - s0) & (kStages - 1);
+                    const int key = lo0 + s * kStepKeys, page = key >> plog, put = (s - s0) & (kStages - 1);
                     if (group0 < 0 || page >= group0 + 32 || (plog == 4 && page + 1 >= group0 + 32)) load_pages(page);
                     const uint32_t dst = ring_at + (uint32_t)(put * 2 * Sh::kHalfBytes);
                     const int32_t id = __shfl_sync(0xFFFFFFFFu, page_id, page - group0);
@@ -394,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const int token = token_of(8 * n + 2 * t + i), hi_row = upper(token), lo_row = lower(token);
+                            const int token = token_of(8 * n + 2 * t + i), hi_row = upper_key(a, sq, token), lo_row = lower_key(a, sq, token);
 #pragma unroll
                             for (int u = 0; u < SUBS; ++u)
 #pragma unroll
@@ -479,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
                 issue(s + 1);
                 ptx::cp_async_wait<1>();
                 __syncwarp();                             // (the scales)
-                const int get = (s - s0) & (kStages - 1), key0 = sp.lo + s * kStepKeys;
+                const int get = (s - s0) & (kStages - 1), key0 = lo0 + s * kStepKeys;
                 const bool one = s_scales[warp][get][0].w != 0.f, two = s_scales[warp][get][1].w != 0.f;
                 if (kPairs && one && two) {
                     work(key0, get, 0, std::integral_constant<int, kPairs ? 2 : 1>{});
@@ -518,11 +436,11 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
                     store_run<float, kVBytes>(rows + row * D + g * kVBytes, r);
                 }
             __syncthreads();
-            const bool begins = first == 0, ends = last == sp.steps, whole = begins && ends;
+            const bool begins = un.first == 0, ends = un.last == un.sp.steps, whole = begins && ends;
             float* slot = slots + (2 * w + (begins ? 1 : 0)) * (int64_t)slot_floats(kRows, D);
             if (begins && !ends) {
-                cut.b = b, cut.row_tile = tile, cut.head = head;
-                cut.pieces = (int32_t)((unit_at + sp.steps - 1) / share - w + 1);
+                cut.b = un.b, cut.row_tile = un.tile, cut.head = head;
+                cut.pieces = walk.pieces(un, w);
             }
             for (int i = tid; i < n_rows * (D / 4); i += kThreads) {
                 const int row = i / (D / 4), d = i % (D / 4) * 4;
@@ -553,63 +471,6 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
     if (tid == 0) cuts[w] = cut;
 }
 
-// Joins the pieces of the units that are cut: with M the largest reference, the sum of 2^(m - M) (values, sum) over the pieces,
-// in the order of the keys.  A CTA looks after 8 rows of the unit that begins in share blockIdx.x and goes on behind it: a warp per row,
-// or several that split the pieces among them.
-constexpr int kJoinWarps = 8;
-template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __grid_constant__ AttendArgs a, const CutUnit* __restrict__ cuts,
-                                                                     const float* __restrict__ slots)
-{
-    constexpr int kRows = 8 * NT, kLanes = D / 4;          // lanes of four elements
-    __shared__ float4 part[kJoinWarps][kLanes];
-    ptx::grid_dependency_sync();
-    const int4 cut = __ldcg(reinterpret_cast<const int4*>(cuts + blockIdx.x));          // sequence, row tile, head, pieces
-    if (cut.w == 0) return;
-    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
-    const int group = a.heads / a.c.kv_heads;
-    const Sequence sq = sequence_of(a.c, cut.x, a.N);
-    const int rows = (int)min((int64_t)kRows, (int64_t)sq.n * group - (int64_t)cut.y * kRows) - 8 * (int)blockIdx.y;
-    if (rows <= 0) return;
-    const int split = rows >= kJoinWarps ? 1 : kJoinWarps / rows;                       // warps per row
-    const int row = 8 * (int)blockIdx.y + warp / split, sub = warp % split;
-    const bool on = warp / split < min(rows, kJoinWarps);
-    const int64_t w0 = blockIdx.x;
-    auto slot = [&](int p) { return slots + (p == 0 ? 2 * w0 + 1 : 2 * (w0 + p)) * (int64_t)slot_floats(kRows, D); };
-    float M = kNone, L = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (on) {
-        for (int p = lane; p < cut.w; p += 32) M = fmaxf(M, __ldcg(slot(p) + row));
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
-        for (int p = lane; p < cut.w; p += 32) L += __ldcg(slot(p) + kRows + row) * ex2(__ldcg(slot(p) + row) - M);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
-        if (lane < kLanes) {
-#pragma unroll 8
-            for (int p = sub; p < cut.w; p += split) {
-                const float f = ex2(__ldcg(slot(p) + row) - M);
-                const float4 x = __ldcg(reinterpret_cast<const float4*>(slot(p) + 2 * kRows + row * D + lane * 4));
-                acc.x = fmaf(x.x, f, acc.x), acc.y = fmaf(x.y, f, acc.y), acc.z = fmaf(x.z, f, acc.z), acc.w = fmaf(x.w, f, acc.w);
-            }
-        }
-    }
-    if (split > 1) {                                       // (the same in all threads)
-        if (lane < kLanes) part[warp][lane] = acc;
-        __syncthreads();
-    }
-    if (!on || sub != 0 || lane >= kLanes) return;
-    for (int z = 1; z < split; ++z) {
-        const float4 x = part[warp + z][lane];
-        acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
-    }
-    const int r = cut.y * kRows + row, token = r / group;
-    const int64_t orow = (int64_t)sq.row0 + token;
-    const int oh = cut.z * group + (r - token * group);
-    store4(static_cast<T*>(a.out) + orow * a.ldo + (int64_t)oh * D + lane * 4, acc, L == 0.f ? 0.f : 1.f / L);
-    if (a.lse != nullptr && lane == 0) a.lse[orow * a.heads + oh] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718056f;
-}
-
 template <typename T, int D, int NT>
 int64_t worker_count() { return (int64_t)sm_count() * Shape<T, D, NT>::kCtas * kWaves; }
 
@@ -635,7 +496,7 @@ molora_status_t launch(const AttendArgs& a, void* ws, cudaStream_t s)
     float* slots = reinterpret_cast<float*>(static_cast<char*>(ws) + cut_bytes(workers));
     if (launch_kernel(attend_rows_kernel<T, D, NT>, dim3((unsigned)workers), dim3(kThreads), Sh::kSmem, s, 1, true, a, cuts, slots) != cudaSuccess)
         return MOLORA_ERR_CUDA;
-    return cuda_ok(launch_kernel(attend_join_kernel<T, D, NT>, dim3((unsigned)workers, NT), dim3(kJoinWarps * 32), 0, s, 1, true, a,
+    return cuda_ok(launch_kernel(attend_join_kernel<T, D, 8 * NT>, dim3((unsigned)workers, NT), dim3(kJoinWarps * 32), 0, s, 1, true, a,
                                  static_cast<const CutUnit*>(cuts), static_cast<const float*>(slots)));
 }
 

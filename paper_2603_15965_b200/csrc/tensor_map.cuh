@@ -38,6 +38,20 @@ static inline bool make_tensor_map_bf16_2d(CUtensorMap* m, const void* ptr, uint
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// 2-D map of bytes: `cols` contiguous bytes per row, `rows` dense rows.
+static inline bool make_tensor_map_bytes_2d(CUtensorMap* m, const void* ptr, uint64_t cols, uint64_t rows, uint32_t box_cols, uint32_t box_rows,
+                                            CUtensorMapSwizzle swz)
+{
+    EncodeTiledFn fn = tensor_map_encode_fn();
+    if (fn == nullptr) return false;
+    const cuuint64_t dims[2] = {cols, rows};
+    const cuuint64_t strides[1] = {cols};
+    const cuuint32_t box[2] = {box_cols, box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swz,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Row blocks of a bf16 matrix [rows, cols] of pitch `cols` for loads of many columns at once: dimensions (block columns, rows,
 // cols / block), so that one box of all blocks lands as one [rows][block] tile per block.  `block` divides cols.
 static inline bool make_tensor_map_bf16_blocks(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, uint32_t block,
