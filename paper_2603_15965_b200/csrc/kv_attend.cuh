@@ -20,19 +20,20 @@ struct CutUnit {
 __host__ __device__ constexpr int slot_floats(int rows, int dim) { return 2 * rows + rows * dim; }
 __host__ __device__ inline size_t cut_bytes(int64_t workers) { return (size_t)((workers * (int64_t)sizeof(CutUnit) + 255) / 256 * 256); }
 
-// steps of every unit of a sequence, and where its keys begin
+// steps of every unit of a sequence, and where its keys begin.  In front of its keys a unit has COST steps without any, so that shares are
+// equal in time where short sequences come with their units' fixed costs.
 struct Span {
     int32_t lo;        // first key, a multiple of KEYS
     int32_t steps;     // per unit
     int32_t tiles;     // of rows
 };
-template <int ROWS, int KEYS>
+template <int ROWS, int KEYS, int COST>
 __device__ __forceinline__ Span span_of(const Sequence& s, int group, int window)
 {
     Span r{0, 0, 0};
     if (s.n == 0) return r;
     r.lo = window > 0 ? max(0, s.first_pos() - window + 1) & ~(KEYS - 1) : 0;
-    r.steps = max(1, (s.len - r.lo + KEYS - 1) / KEYS);
+    r.steps = COST + max(1, (s.len - r.lo + KEYS - 1) / KEYS);
     r.tiles = (int32_t)(((int64_t)s.n * group + ROWS - 1) / ROWS);
     return r;
 }
@@ -45,7 +46,7 @@ struct Unit {
     int32_t b, head, tile, first, last;     // its steps [first, last) are in this share
     int32_t n_rows, tile_row;
     int32_t hi_min, hi_max, lo_min, lo_max; // keys below hi_min and from lo_max on are seen by every row, [lo_min, hi_max) by some
-    int32_t u0, u1;                         // the steps of the share that some row sees
+    int32_t u0, u1;                         // its steps of keys, counted from lo, that some row sees
 };
 __device__ __forceinline__ int upper_key(const AttendArgs& a, const Sequence& sq, int token)
 {
@@ -57,20 +58,21 @@ __device__ __forceinline__ int lower_key(const AttendArgs& a, const Sequence& sq
 }
 
 // The units of a share, in order; every thread (or warp) that asks gets the same.
-template <int ROWS, int KEYS>
+template <int ROWS, int KEYS, int COST>
 struct Walk {
     const AttendArgs& a;
     int64_t at, stop, base;                 // next step, end of the share, first step of sequence b
-    int64_t share;
+    const int64_t* s_upto = nullptr;
+    int64_t total = 0, share = 1;           // steps of all units, and of a share
     int b, group;
     Sequence sq;
     Span sp;
-    __device__ explicit Walk(const AttendArgs& args) : a(args), at(0), stop(0), base(0), share(1), b(0), group(args.heads / args.c.kv_heads) {}
+    __device__ explicit Walk(const AttendArgs& args) : a(args), at(0), stop(0), base(0), b(0), group(args.heads / args.c.kv_heads) {}
 
     __device__ void load()
     {
         sq = sequence_of(a.c, b, a.N);
-        sp = span_of<ROWS, KEYS>(sq, group, a.window);
+        sp = span_of<ROWS, KEYS, COST>(sq, group, a.window);
     }
     __device__ bool next(Unit& u)
     {
@@ -91,27 +93,42 @@ struct Walk {
         const int t0 = u.tile_row / group, t1 = (u.tile_row + u.n_rows - 1) / group;
         u.hi_min = upper_key(a, sq, t0), u.hi_max = upper_key(a, sq, t1);
         u.lo_min = lower_key(a, sq, t0), u.lo_max = lower_key(a, sq, t1);
-        u.u0 = max(u.first, (u.lo_min - sp.lo) / KEYS);
-        u.u1 = min(u.last, u.hi_max > sp.lo ? (u.hi_max - sp.lo + KEYS - 1) / KEYS : 0);
+        u.u0 = max(u.first - COST, (u.lo_min - sp.lo) / KEYS);
+        u.u1 = min(u.last - COST, u.hi_max > sp.lo ? (u.hi_max - sp.lo + KEYS - 1) / KEYS : 0);
         return true;
     }
     // the shares in which the unit lies, from this one (w), where it begins, on
     __device__ int32_t pieces(const Unit& u, int64_t w) const { return (int32_t)((u.at + u.sp.steps - 1) / share - w + 1); }
+    // Puts the walk at the beginning of share w; `parts`: how many parts of the sequences s_upto counts.
+    __device__ void begin(int64_t w, int parts)
+    {
+        at = w * share;
+        stop = min(total, at + share);
+        if (at >= stop) return;
+        int lo = 0, hi = parts - 1;         // the part in which the share begins
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (s_upto[mid] > at) hi = mid;
+            else lo = mid + 1;
+        }
+        b = lo * ((a.c.B + parts - 1) / parts);
+        base = lo > 0 ? s_upto[lo - 1] : 0;
+        load();
+    }
 };
 
-// Puts `walk` at the beginning of share w of `shares`.  All THREADS threads of the CTA call it; s_upto: THREADS words.
-template <int THREADS, int ROWS, int KEYS>
-__device__ __forceinline__ void begin_share(Walk<ROWS, KEYS>& walk, int64_t w, int64_t shares, int min_share, int64_t* s_upto)
+// Steps of the sequences up to the end of each thread's part of them, into s_upto (THREADS words); all THREADS threads of the CTA.
+template <int THREADS, int ROWS, int KEYS, int COST>
+__device__ __forceinline__ void count_steps(const AttendArgs& a, int64_t* s_upto)
 {
-    const AttendArgs& a = walk.a;
-    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, group = a.heads / a.c.kv_heads;
     const int part = (a.c.B + THREADS - 1) / THREADS;
     int64_t incl = 0;
     for (int b = tid * part; b < min(a.c.B, (tid + 1) * part); ++b) {
         const Sequence sq = sequence_of(a.c, b, a.N);
-        const Span sp = span_of<ROWS, KEYS>(sq, walk.group, a.window);
+        const Span sp = span_of<ROWS, KEYS, COST>(sq, group, a.window);
         incl += (int64_t)sp.steps * sp.tiles * a.c.kv_heads;
-        if (sq.bad && w == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
+        if (sq.bad && blockIdx.x == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
     }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -122,22 +139,16 @@ __device__ __forceinline__ void begin_share(Walk<ROWS, KEYS>& walk, int64_t w, i
     __syncthreads();
     for (int z = 0; z < warp; ++z) incl += s_upto[32 * z + 31];
     __syncthreads();
-    s_upto[tid] = incl;                     // steps of the sequences up to the end of this thread's part
+    s_upto[tid] = incl;
     __syncthreads();
-    const int64_t total = s_upto[THREADS - 1];
-    walk.share = max((total + shares - 1) / shares, (int64_t)min_share);
-    walk.at = w * walk.share;
-    walk.stop = min(total, walk.at + walk.share);
-    if (walk.at >= walk.stop) return;
-    int lo = 0, hi = THREADS - 1;           // the part in which the share begins
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (s_upto[mid] > walk.at) hi = mid;
-        else lo = mid + 1;
-    }
-    walk.b = lo * part;
-    walk.base = lo > 0 ? s_upto[lo - 1] : 0;
-    walk.load();
+}
+// Equal shares of all steps, none shorter than min_share.
+template <int ROWS, int KEYS, int COST>
+__device__ __forceinline__ void cut_shares(Walk<ROWS, KEYS, COST>& walk, const int64_t* s_upto, int parts, int64_t shares, int min_share)
+{
+    walk.s_upto = s_upto;
+    walk.total = s_upto[parts - 1];
+    walk.share = max((walk.total + shares - 1) / shares, (int64_t)min_share);
 }
 
 // scales of v outside [2^-100, 2^100] are read as its ends
@@ -150,60 +161,74 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v, float f)
 }
 
 // Joins the pieces of the units that are cut: with M the largest reference, the sum of 2^(m - M) (values, sum) over the pieces,
-// in the order of the keys.  A CTA looks after 8 rows of the unit that begins in share blockIdx.x and goes on behind it: a warp per row,
-// or several that split the pieces among them.
-constexpr int kJoinWarps = 8;
+// always in the same order.  A CTA looks after 4 rows of the unit that begins in share blockIdx.x and goes on behind it; its four warps take every
+// fourth piece each, four rows at a time, and are added up in order.  (Asked for row by row, the pieces of a unit cut into 55 took 32 us.)
+constexpr int kJoinWarps = 4, kJoinRows = 4;
 template <typename T, int D, int ROWS>
 __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __grid_constant__ AttendArgs a, const CutUnit* __restrict__ cuts,
                                                                      const float* __restrict__ slots)
 {
-    constexpr int kRows = ROWS, kLanes = D / 4;          // lanes of four elements
-    __shared__ float4 part[kJoinWarps][kLanes];
+    constexpr int kLanes = D / 4;                          // lanes of four elements
+    __shared__ float4 part[kJoinWarps][kJoinRows][kLanes];
+    __shared__ float part_l[kJoinWarps][kJoinRows];
     ptx::grid_dependency_sync();
     const int4 cut = __ldcg(reinterpret_cast<const int4*>(cuts + blockIdx.x));          // sequence, row tile, head, pieces
     if (cut.w == 0) return;
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
-    const int group = a.heads / a.c.kv_heads;
+    const int group = a.heads / a.c.kv_heads, r0 = kJoinRows * (int)blockIdx.y;
     const Sequence sq = sequence_of(a.c, cut.x, a.N);
-    const int rows = (int)min((int64_t)kRows, (int64_t)sq.n * group - (int64_t)cut.y * kRows) - 8 * (int)blockIdx.y;
+    const int rows = (int)min((int64_t)ROWS, (int64_t)sq.n * group - (int64_t)cut.y * ROWS) - r0;
     if (rows <= 0) return;
-    const int split = rows >= kJoinWarps ? 1 : kJoinWarps / rows;                       // warps per row
-    const int row = 8 * (int)blockIdx.y + warp / split, sub = warp % split;
-    const bool on = warp / split < min(rows, kJoinWarps);
     const int64_t w0 = blockIdx.x;
-    auto slot = [&](int p) { return slots + (p == 0 ? 2 * w0 + 1 : 2 * (w0 + p)) * (int64_t)slot_floats(kRows, D); };
-    float M = kNone, L = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (on) {
-        for (int p = lane; p < cut.w; p += 32) M = fmaxf(M, __ldcg(slot(p) + row));
+    auto slot = [&](int p) { return slots + (p == 0 ? 2 * w0 + 1 : 2 * (w0 + p)) * (int64_t)slot_floats(ROWS, D) + r0; };
+    float M[kJoinRows], L[kJoinRows] = {};
+    float4 acc[kJoinRows] = {};
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
-        for (int p = lane; p < cut.w; p += 32) L += __ldcg(slot(p) + kRows + row) * ex2(__ldcg(slot(p) + row) - M);
+    for (int r = 0; r < kJoinRows; ++r) M[r] = kNone;
+    for (int p = lane; p < cut.w; p += 32) {
+        const float4 m = __ldcg(reinterpret_cast<const float4*>(slot(p)));
+        M[0] = fmaxf(M[0], m.x), M[1] = fmaxf(M[1], m.y), M[2] = fmaxf(M[2], m.z), M[3] = fmaxf(M[3], m.w);
+    }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
-        if (lane < kLanes) {
-#pragma unroll 8
-            for (int p = sub; p < cut.w; p += split) {
-                const float f = ex2(__ldcg(slot(p) + row) - M);
-                const float4 x = __ldcg(reinterpret_cast<const float4*>(slot(p) + 2 * kRows + row * D + lane * 4));
-                acc.x = fmaf(x.x, f, acc.x), acc.y = fmaf(x.y, f, acc.y), acc.z = fmaf(x.z, f, acc.z), acc.w = fmaf(x.w, f, acc.w);
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int r = 0; r < kJoinRows; ++r) M[r] = fmaxf(M[r], __shfl_xor_sync(0xFFFFFFFFu, M[r], o));
+    // (rows behind the last hold whatever was there: their M, sums and values are not used)
+#pragma unroll 4
+    for (int p = warp; p < cut.w; p += kJoinWarps) {
+        const float* s = slot(p);
+        const float4 m = __ldcg(reinterpret_cast<const float4*>(s)), l = __ldcg(reinterpret_cast<const float4*>(s + ROWS));
+        const float f[kJoinRows] = {ex2(m.x - M[0]), ex2(m.y - M[1]), ex2(m.z - M[2]), ex2(m.w - M[3])};
+        L[0] = fmaf(l.x, f[0], L[0]), L[1] = fmaf(l.y, f[1], L[1]), L[2] = fmaf(l.z, f[2], L[2]), L[3] = fmaf(l.w, f[3], L[3]);
+#pragma unroll
+        for (int r = 0; r < kJoinRows; ++r)
+            if (r < rows && lane < kLanes) {
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(s + 2 * ROWS - r0 + (r0 + r) * D + lane * 4));
+                acc[r].x = fmaf(x.x, f[r], acc[r].x), acc[r].y = fmaf(x.y, f[r], acc[r].y);
+                acc[r].z = fmaf(x.z, f[r], acc[r].z), acc[r].w = fmaf(x.w, f[r], acc[r].w);
             }
-        }
     }
-    if (split > 1) {                                       // (the same in all threads)
-        if (lane < kLanes) part[warp][lane] = acc;
-        __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kJoinRows; ++r) {
+        if (lane < kLanes) part[warp][r][lane] = acc[r];
+        if (lane == 0) part_l[warp][r] = L[r];
     }
-    if (!on || sub != 0 || lane >= kLanes) return;
-    for (int z = 1; z < split; ++z) {
-        const float4 x = part[warp + z][lane];
-        acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
+    __syncthreads();
+    if (warp >= rows || lane >= kLanes) return;            // a row per warp from here on
+    const int row = r0 + warp;
+    float sum = 0.f, top = warp == 0 ? M[0] : warp == 1 ? M[1] : warp == 2 ? M[2] : M[3];
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int z = 0; z < kJoinWarps; ++z) {
+        const float4 x = part[z][warp][lane];
+        v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+        sum += part_l[z][warp];
     }
-    const int r = cut.y * kRows + row, token = r / group;
+    const int r = cut.y * ROWS + row, token = r / group;
     const int64_t orow = (int64_t)sq.row0 + token;
     const int oh = cut.z * group + (r - token * group);
-    store4(static_cast<T*>(a.out) + orow * a.ldo + (int64_t)oh * D + lane * 4, acc, L == 0.f ? 0.f : 1.f / L);
-    if (a.lse != nullptr && lane == 0) a.lse[orow * a.heads + oh] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718056f;
+    store4(static_cast<T*>(a.out) + orow * a.ldo + (int64_t)oh * D + lane * 4, v, sum == 0.f ? 0.f : 1.f / sum);
+    if (a.lse != nullptr && lane == 0) a.lse[orow * a.heads + oh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718056f;
 }
 
 }  // namespace

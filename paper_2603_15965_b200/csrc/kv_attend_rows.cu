@@ -31,6 +31,7 @@ namespace {
 
 constexpr int kWarpsPerCta = 4, kThreads = kWarpsPerCta * 32;
 constexpr int kHalfKeys = 16, kStepKeys = 32;  // keys of a tensor instruction, and of a step: two of them, in one page or in two of 16
+constexpr int kUnitCost = 4;                 // steps that a unit's rows and results cost
 constexpr int kMinShare = 4;                 // steps of a CTA: shorter shares cost more in joining than they save
 constexpr int kWaves = 2;                    // shares per resident CTA
 constexpr int kMaxTiles = 4;                 // 8-row tiles of a unit
@@ -121,8 +122,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
     const uint32_t ring_at = ptx::smem_u32(ring);
 
     const int64_t w = blockIdx.x;
-    Walk<kRows, kStepKeys> walk(a);
-    begin_share<kThreads>(walk, w, gridDim.x, kMinShare, s_upto);
+    Walk<kRows, kStepKeys, kUnitCost> walk(a);
+    count_steps<kThreads, kRows, kStepKeys, kUnitCost>(a, s_upto);
+    cut_shares(walk, s_upto, kThreads, gridDim.x, kMinShare);
+    walk.begin(w, kThreads);
     CutUnit cut{0, 0, 0, 0};
     Unit un;
     while (walk.next(un)) {
@@ -496,7 +499,7 @@ molora_status_t launch(const AttendArgs& a, void* ws, cudaStream_t s)
     float* slots = reinterpret_cast<float*>(static_cast<char*>(ws) + cut_bytes(workers));
     if (launch_kernel(attend_rows_kernel<T, D, NT>, dim3((unsigned)workers), dim3(kThreads), Sh::kSmem, s, 1, true, a, cuts, slots) != cudaSuccess)
         return MOLORA_ERR_CUDA;
-    return cuda_ok(launch_kernel(attend_join_kernel<T, D, 8 * NT>, dim3((unsigned)workers, NT), dim3(kJoinWarps * 32), 0, s, 1, true, a,
+    return cuda_ok(launch_kernel(attend_join_kernel<T, D, 8 * NT>, dim3((unsigned)workers, 8 * NT / kJoinRows), dim3(kJoinWarps * 32), 0, s, 1, true, a,
                                  static_cast<const CutUnit*>(cuts), static_cast<const float*>(slots)));
 }
 

@@ -5,17 +5,22 @@
 // written as a sum of e4m3 terms, each in columns of its own:
 //   q (8 significant bits) = t1 + t2 / 32, exactly: the rest that rounding to 4 bits leaves of 8 fits 4; a power of two per row brings the largest
 //       element to [2^7, 2^8), so elements below 2^-14 of it are off by at most 2^-23 of it
-//   a weight = t1 + t2 / 32 + t3 / 1024, to 2^-12 of it (and 2^-20 where a row's largest is 2^4 or more)
+//   a weight, rounded to fp16 (11 bits), = t1 + t2 / 32 + t3 / 1024, exactly (to 2^-20 where a row's largest is 2 or more)
 //   S^T [128 keys x 2 rows]   = K Q^T     A = K tile, keys the 128 lanes of TMEM; B = q's terms
 //   O^T [128 elements x 3 rows] += V^T P^T  A = V tile read across (MN-major); B = the weights' terms
 // with the key as the lane a thread owns one key: the scales of its block, its mask and its weights are its own, and reductions
 // over keys are needed only when a row's reference moves (a score 2^4 over the reference) and at the end of a unit.
-//   warp 0    page table, scales, TMA (kStages tiles of 128 keys = 32 KB each in flight)
-//   warp 1    the MMAs of S one tile ahead of those of O
-//   warps 2-5 a key per thread: weights and their terms into shared memory; at the end of a unit an element per thread
+//   warp 0    pages, scales and TMA (5 or 6 tiles of 128 keys, 32 KB each, in flight or in use)
+//   warp 1    the MMAs, those of S one tile ahead of those of O
+//   warp 2    the units and their rows, one or two units ahead: q's terms, factors, bounds, places of the results
+//   warps 4.. groups of four warps, each with 4 or 8 of the rows: a key per thread, weights and their terms into shared memory; at the end
+//             of a unit an element per thread.  The rows are divided because a warp works through its tile (S, weights, terms) at the latencies
+//             of one chain of instructions; up to 16 rows there are two sets of groups for alternate units, so that the end of one unit and the
+//             beginning of the next overlap.  Code that runs once a unit is kept short and the state of a unit in shared memory:
+//             instructions that are not in the cache cost more than what they do.
 // Weights are at most 2^8; the scale of a block of K multiplies its scores, that of V is added to the exponent as a logarithm and taken off
 // the sum again, so that weights have the size of what they contribute.
-// What bounds it: 32 KB a tile from HBM; the chain of a tile (S, weights, O) takes about half of what the bytes do.
+// What bounds it: 32 KB a tile from HBM.
 #include "kv_attend.cuh"
 #include "pipeline.cuh"
 #include "tensor_map.cuh"
@@ -24,40 +29,73 @@ namespace molora {
 namespace {
 
 constexpr int kDim = 128, kKeys = 128;
-constexpr int kThreads = 192, kKeyThreads = 128;
-constexpr int kStages = 5;
-constexpr int kTileBytes = kKeys * kDim, kStageBytes = 2 * kTileBytes;
+constexpr int kFirstGroupWarp = 4;
+constexpr int kMaxStages = 6;                // tiles in flight or in use
+constexpr int kTileBytes = kKeys * kDim, kStageBytes = 2 * kTileBytes;      // K, then V
 constexpr int kMinShare = 2;                 // tiles
-constexpr int kWaves = 1;
 constexpr int kTermsQ = 2, kTermsP = 3;
 constexpr float kTermStep = 32.f;            // a term's weight against the next
-constexpr float kTop = 4.f, kSlack = 4.f;    // a row's largest weight when its reference is set: 2^4; it may grow by 2^4 before the reference moves
+constexpr float kTop = 1.f, kSlack = 7.f;    // a row's largest weight when its reference is set: 2; it may grow by 2^7 before the reference moves
 constexpr float kNan = __builtin_nanf("");
 
 template <int ROWS>
 struct Cfg {
-    static constexpr int kNS = kTermsQ * ROWS;                            // columns of S: a multiple of 16
-    static constexpr int kNP = (kTermsP * ROWS + 15) / 16 * 16;           // columns of O, the last ones unused
-    static constexpr int kQBytes = (kNS + 7) / 8 * 1024, kPBytes = (kNP + 7) / 8 * 1024;
-    static constexpr uint32_t kSCol0 = 0, kSCol1 = 64, kOCol = 128, kTmemCols = 256;
-    static_assert(kNS <= 64 && kNP <= 128, "TMEM columns");
-    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kQBytes + 2 * kPBytes;
+    static constexpr int kRowsPerGroup = ROWS == 16 || ROWS == 32 ? 8 : 4, kGroups = ROWS / kRowsPerGroup;
+    static constexpr int kSets = ROWS <= 16 ? 2 : 1;                      // units in hand at a time
+    static constexpr int kUnitCost = kSets == 2 ? 2 : 4;                  // tiles that a unit's rows and results cost
+    static constexpr int kKeyThreads = 128 * kGroups, kThreads = 32 * kFirstGroupWarp + kSets * kKeyThreads;      // (kKeyThreads: of a set)
+    static_assert(kThreads <= 1024, "threads");
+    static constexpr int kNS = (kTermsQ * ROWS + 15) / 16 * 16;           // columns of S and of O: multiples of 16, the last ones unused
+    static constexpr int kNP = (kTermsP * ROWS + 15) / 16 * 16;
+    static constexpr int kQBytes = kNS / 8 * 1024, kPBytes = kNP / 8 * 1024;
+    static constexpr uint32_t kSCol1 = 64, kOCol = 128, kOSet = 64, kTmemCols = 256;  // S of odd tiles, O of each set
+    static_assert(kNS <= 64 && kNP <= (kSets == 2 ? 64 : 128), "TMEM columns");
+    static constexpr int kStages = ROWS <= 16 ? 6 : 5;
+    static constexpr int kQAt = kStages * kStageBytes, kPAt = kQAt + 2 * kQBytes;
+    static constexpr size_t kSmem = 1024 + (size_t)kPAt + 2 * kPBytes;
+    static_assert(kStages <= kMaxStages, "stages");
 };
 
+// A thread that waits for a phase by its parity must have seen the phase before it.  Hence barriers of their own where a role does not look
+// at every phase: s_full for the tiles of each set, q_ready (for the MMAs) beside q_full, since units without tiles pass the MMAs by.
 struct Control {
-    uint64_t full[kStages], empty[kStages], s_full[2], s_empty[2], p_full[2], p_empty[2], q_full, o_empty, drained;
+    uint64_t full[kMaxStages], empty[kMaxStages];
+    uint64_t s_full[2][2], s_empty[2], p_full[2], p_empty[2], o_empty[2];
+    uint64_t q_full[2], q_ready[2], q_empty[2];
+    uint64_t drained;
     uint32_t tmem_base;
     int abort_flag;
 };
+// A tile in the ring: the scales of every 16 keys (of K, logarithm and reciprocal of V's, whether their page can be used), and where in its unit it
+// stands.
+struct Tile {
+    float4 scale[8];
+    int32_t kind;                             // kFirst: begins a unit, kOdd: of an odd one; kLast: no tile, there are no more
+};
+enum : int32_t { kFirst = 1, kOdd = 2, kLast = 4 };
+// A unit and its rows.
+template <int ROWS>
+struct Rows {
+    float factor[ROWS];                       // of a score: scale, powers of two
+    int32_t lower[ROWS], upper[ROWS];         // keys that the row sees
+    int64_t out[ROWS], lse[ROWS];             // places in out and lse
+    int32_t tile0, tiles;                     // its tiles; -1: there are no more units
+    int32_t key0, n_rows;                     // first key of the first tile
+    int32_t hi_min, hi_max, lo_min, lo_max;
+    int32_t slot;                             // where a piece goes; -1: the unit is whole
+};
 
-__device__ __forceinline__ void key_threads_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
-__device__ __forceinline__ bool key_threads_any(bool v)
+// barriers of a group (1 + group) and of a set (14 + set)
+template <int THREADS>
+__device__ __forceinline__ void sync_threads_of(int id) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "n"(THREADS) : "memory"); }
+template <int THREADS>
+__device__ __forceinline__ bool threads_any(int id, bool v)
 {
     uint32_t r;
     asm volatile(
-        "{\n\t.reg .pred P, Q;\n\tsetp.ne.b32 P, %1, 0;\n\tbarrier.cta.red.or.pred Q, 1, 128, P;\n\tselp.u32 %0, 1, 0, Q;\n\t}"
+        "{\n\t.reg .pred P, Q;\n\tsetp.ne.b32 P, %1, 0;\n\tbarrier.cta.red.or.pred Q, %2, %3, P;\n\tselp.u32 %0, 1, 0, Q;\n\t}"
         : "=r"(r)
-        : "r"((uint32_t)v)
+        : "r"((uint32_t)v), "r"(id), "n"(THREADS)
         : "memory");
     return r != 0;
 }
@@ -78,31 +116,32 @@ __device__ __forceinline__ uint32_t split_pair(float& a, float& b)
 // byte `b` of line `line` of a K-major operand of 128-byte lines, 128-byte swizzle
 __device__ __forceinline__ uint32_t line_offset(int line, int b) { return (uint32_t)(line * 128 + ((((b >> 4) ^ line) & 7) << 4) + (b & 15)); }
 
+// N = 4 or 8 neighbouring columns
 template <int N>
-__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t* v)          // N columns, a multiple of 8
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t* v)
 {
-#pragma unroll
-    for (int i = 0; i + 16 <= N; i += 16) ptx::tmem_ld_x16(addr + i, v + i);
-    if constexpr (N % 16 != 0) ptx::tmem_ld_x8(addr + N / 16 * 16, v + N / 16 * 16);
-    ptx::tmem_wait_ld();
+    if constexpr (N == 4) ptx::tmem_ld_x4(addr, v);
+    else ptx::tmem_ld_x8(addr, v);
 }
 
 template <int ROWS>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
     attend_stream_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                          CutUnit* __restrict__ cuts, float* __restrict__ slots)
 {
     using C = Cfg<ROWS>;
+    constexpr int RPG = C::kRowsPerGroup;
     using namespace ptx;
     __shared__ Control ctrl;
-    __shared__ int64_t s_upto[kThreads];
-    __shared__ float4 s_scales[kStages][8];          // of 16 keys: scale of K, logarithm and reciprocal of V's, whether their page can be used
-    __shared__ float s_row[ROWS], s_part[4][ROWS];
+    __shared__ int64_t s_upto[C::kThreads];
+    __shared__ Tile s_tiles[C::kStages];
+    __shared__ Rows<ROWS> s_rows[2];
+    __shared__ float s_part[C::kSets * C::kGroups][4][RPG];
     extern __shared__ uint8_t smem_raw[];
     const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base - raw);
-    const uint32_t q_at = base + kStages * kStageBytes, p_at = q_at + C::kQBytes;
+    const uint32_t q_at = base + C::kQAt, p_at = base + C::kPAt;
     volatile int* abort_flag = &ctrl.abort_flag;
     auto bar = [](const uint64_t* b) { return smem_u32(b); };
 
@@ -110,13 +149,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (tid == 0) {
         prefetch_tensormap(&tm_k);
         prefetch_tensormap(&tm_v);
-        for (int s = 0; s < kStages; ++s) mbar_init(bar(&ctrl.full[s]), 1), mbar_init(bar(&ctrl.empty[s]), 1);
+        for (int s = 0; s < C::kStages; ++s) mbar_init(bar(&ctrl.full[s]), 1), mbar_init(bar(&ctrl.empty[s]), 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(&ctrl.s_full[i]), 1), mbar_init(bar(&ctrl.s_empty[i]), kKeyThreads);
-            mbar_init(bar(&ctrl.p_full[i]), kKeyThreads), mbar_init(bar(&ctrl.p_empty[i]), 1);
+            mbar_init(bar(&ctrl.s_full[0][i]), 1), mbar_init(bar(&ctrl.s_full[1][i]), 1), mbar_init(bar(&ctrl.s_empty[i]), C::kKeyThreads);
+            mbar_init(bar(&ctrl.p_full[i]), C::kKeyThreads), mbar_init(bar(&ctrl.p_empty[i]), 1);
+            mbar_init(bar(&ctrl.q_full[i]), 1), mbar_init(bar(&ctrl.q_ready[i]), 1), mbar_init(bar(&ctrl.q_empty[i]), C::kKeyThreads);
+            mbar_init(bar(&ctrl.o_empty[i]), C::kKeyThreads);
         }
-        mbar_init(bar(&ctrl.q_full), kKeyThreads);
-        mbar_init(bar(&ctrl.o_empty), kKeyThreads);
         mbar_init(bar(&ctrl.drained), 1);
         ctrl.abort_flag = 0;
         fence_mbar_init();
@@ -126,37 +165,44 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_relinquish();
     }
     // operand lines of no row are zero for good
-    for (int i = tid; i < (C::kQBytes + 2 * C::kPBytes) / 16; i += kThreads) *reinterpret_cast<uint4*>(smem + kStages * kStageBytes + i * 16) = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < (2 * C::kQBytes + 2 * C::kPBytes) / 16; i += C::kThreads) *reinterpret_cast<uint4*>(smem + C::kQAt + i * 16) = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
-    Walk<ROWS, kKeys> walk(a);
-    begin_share<kThreads>(walk, blockIdx.x, gridDim.x, kMinShare, s_upto);
+    count_steps<C::kThreads, ROWS, kKeys, C::kUnitCost>(a, s_upto);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     grid_dependency_trigger();                        // (not before TMEM is mine)
     const uint32_t tmem = ctrl.tmem_base;
-    const int group = walk.group, plog = a.c.page_log2;
-    Unit u;
+    const int group = a.heads / a.c.kv_heads, plog = a.c.page_log2;
+    Walk<ROWS, kKeys, C::kUnitCost> walk(a);
+    cut_shares(walk, s_upto, C::kThreads, (int64_t)gridDim.x, kMinShare);
+    walk.begin((int64_t)blockIdx.x, C::kThreads);
 
     if (warp == 0) {
         // ============================================================ pages, scales, copies
-        const int box_log2 = min(plog, 7), boxes = kKeys >> box_log2;      // copies of a tile, each of one page (or of a part of 128)
-        const uint32_t box_bytes = (uint32_t)kDim << box_log2;
-        int s = 0, tiles = 0;
-        uint32_t ph = 1;
-        while (walk.next(u)) {
-            const int32_t* table = a.c.table + (int64_t)u.b * a.c.ld_table;
-            int group0 = -1;
+        const uint32_t page_bytes = (uint32_t)kDim << plog;
+        const int step = kKeys >> plog;                       // pages of a tile, a copy of K and one of V each
+        int tiles = 0, units = 0;
+        Unit u;
+        // the place of the next tile, when it is free
+        auto claim = [&]() {
+            const int s = tiles % C::kStages;
+            if (tiles >= C::kStages) wait_bar(bar(&ctrl.empty[s]), ((uint32_t)(tiles / C::kStages) & 1u) ^ 1u, abort_flag, a.dev_status);
+            __syncwarp();
+            return s;
+        };
+        for (; *abort_flag == 0 && walk.next(u); ++units) {
+            int group0 = 0;                                   // first of the 32 pages whose ids and scales the lanes hold
             int32_t page_id = -1;
             float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int i = u.u0; i < u.u1; ++i) {
                 const int key0 = u.sp.lo + i * kKeys, page = key0 >> plog;
-                if (group0 < 0 || page + boxes > group0 + 32) {
+                if (i == u.u0 || page + step > group0 + 32) {
                     group0 = page;
                     page_id = -1;
                     sc = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (((int64_t)(page + lane) << plog) < u.hi_max) {
-                        page_id = ld_dependent(table + page + lane);
+                        page_id = ld_dependent(a.c.table + (int64_t)u.b * a.c.ld_table + page + lane);
                         if (page_id < 0 || page_id >= a.c.n_pages) {
                             page_id = -1;
                             if (a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
@@ -166,39 +212,45 @@ __global__ void __launch_bounds__(kThreads, 1)
                             sc = make_float4(ld_dependent(a.c.k_scale + block), log2f(vs), 1.f / vs, 1.f);
                         }
                     }
+                    __syncwarp();
                 }
-                if (tiles >= kStages) wait_bar(bar(&ctrl.empty[s]), ph, abort_flag, a.dev_status);
-                if (*abort_flag) break;
-                const int mine = page - group0 + (((lane & 7) * 16) >> plog);           // the page of 16 keys
+                const int mine = (page - group0 + (((lane & 7) * 16) >> plog)) & 31;           // the page of 16 keys
                 float4 g;
-                g.x = __shfl_sync(0xFFFFFFFFu, sc.x, mine & 31), g.y = __shfl_sync(0xFFFFFFFFu, sc.y, mine & 31);
-                g.z = __shfl_sync(0xFFFFFFFFu, sc.z, mine & 31), g.w = __shfl_sync(0xFFFFFFFFu, sc.w, mine & 31);
-                if (lane < 8) s_scales[s][lane] = g;
+                g.x = __shfl_sync(0xFFFFFFFFu, sc.x, mine), g.y = __shfl_sync(0xFFFFFFFFu, sc.y, mine);
+                g.z = __shfl_sync(0xFFFFFFFFu, sc.z, mine), g.w = __shfl_sync(0xFFFFFFFFu, sc.w, mine);
                 const int32_t id = __shfl_sync(0xFFFFFFFFu, page_id, (page - group0 + lane) & 31);
-                const bool copies = lane < boxes && id >= 0;
-                const uint32_t bytes = 2u * box_bytes * (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, copies));
-                const uint32_t fb = bar(&ctrl.full[s]);
-                if (lane == 0) mbar_arrive_expect_tx(fb, bytes);
+                const bool copies = lane < step && id >= 0;
+                const uint32_t bytes = 2u * page_bytes * (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, copies));
+                const int row = (int)((((int64_t)id * a.c.kv_heads + u.head) << plog) + (key0 & ((1 << plog) - 1)));
+                const int s = claim();
+                if (*abort_flag) break;
+                if (lane < 8) s_tiles[s].scale[lane] = g;
+                if (lane == 0) s_tiles[s].kind = (i == u.u0 ? kFirst : 0) | ((units & 1) ? kOdd : 0);
+                __syncwarp();
+                if (lane == 0) mbar_arrive_expect_tx(bar(&ctrl.full[s]), bytes);
                 __syncwarp();
                 if (copies) {
-                    const int row = (int)((((int64_t)id * a.c.kv_heads + u.head) << plog) + (key0 & ((1 << plog) - 1)));
-                    const uint32_t dst = base + (uint32_t)(s * kStageBytes) + (uint32_t)lane * box_bytes;
-                    tma_load_2d(dst, &tm_k, 0, row, fb);
-                    tma_load_2d(dst + kTileBytes, &tm_v, 0, row, fb);
+                    const uint32_t dst = base + (uint32_t)(s * kStageBytes) + (uint32_t)lane * page_bytes;
+                    tma_load_2d(dst, &tm_k, 0, row, bar(&ctrl.full[s]));
+                    tma_load_2d(dst + kTileBytes, &tm_v, 0, row, bar(&ctrl.full[s]));
                 }
-                __syncwarp();
                 ++tiles;
-                if (++s == kStages) s = 0, ph ^= 1u;
             }
-            if (*abort_flag) break;
         }
-        // every copy has landed before the memory is given up (an abort may come with copies in flight; this wait has its own limit)
-        for (int i = 0; i < min(tiles, kStages); ++i) {
-            const int t = tiles - 1 - i;
-            const long long t0 = clock64();
-            while (!mbar_try_wait(bar(&ctrl.full[t % kStages]), (uint32_t)(t / kStages) & 1u))
-                if (clock64() - t0 > kTimeoutCycles) break;
+        const int last = claim();
+        if (*abort_flag == 0 && lane == 0) {
+            s_tiles[last].kind = kLast;
+            mbar_arrive(bar(&ctrl.full[last]));
         }
+        // every copy has landed before the memory is given up: otherwise they have been worked on, but an abort may come with some in flight
+        // (this wait has its own limit)
+        if (*abort_flag)
+            for (int i = 0; i < min(tiles, C::kStages); ++i) {
+                const int z = tiles - 1 - i;
+                const long long t0 = clock64();
+                while (!mbar_try_wait(bar(&ctrl.full[z % C::kStages]), (uint32_t)(z / C::kStages) & 1u))
+                    if (clock64() - t0 > kTimeoutCycles) break;
+            }
     } else if (warp == 1) {
         // ============================================================ MMAs
         const bool leader = elect_one();
@@ -208,206 +260,280 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t k_desc = smem_desc(base, 16, 1024, kL128), v_desc = smem_desc(base + kTileBytes, 0, 1024, kL128);
         const uint64_t q_desc = smem_desc(q_at, 16, 1024, kL128), p_desc = smem_desc(p_at, 16, 1024, kL128);
         bool live = true;
-        int tiles = 0, units = 0;                     // tiles whose S has been asked for, units with tiles begun
-        auto issue_s = [&](bool first) {              // S of tile `tiles`
-            const int s = tiles % kStages, b = tiles & 1;
-            if (first) live = wait_bar(bar(&ctrl.q_full), (uint32_t)units & 1u, abort_flag, a.dev_status) && live, ++units;
-            live = wait_bar(bar(&ctrl.full[s]), (uint32_t)(tiles / kStages) & 1u, abort_flag, a.dev_status) && live;
-            if (tiles >= 2) live = wait_bar(bar(&ctrl.s_empty[b]), ((uint32_t)(tiles >> 1) & 1u) ^ 1u, abort_flag, a.dev_status) && live;
-            tc_fence_after();
-            if (leader && live) {
-                const uint64_t at = (uint64_t)(s * (kStageBytes >> 4));
-                const uint32_t d = tm + (b ? C::kSCol1 : C::kSCol0);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) umma_f8(d, k_desc + at + j * 2, q_desc + j * 2, idesc_s, j > 0);      // 32 elements a step
-                umma_commit(bar(&ctrl.s_full[b]));
-            }
-            ++tiles;
+        int ahead = 0, begun0 = 0, begun1 = 0, asked0 = 0, asked1 = 0;      // tiles whose S has been asked for; of each set: units begun, tiles asked for
+        int ready0 = 0, ready1 = 0;                   // units with tiles whose rows have been waited for, per buffer
+        // S of a tile goes out before O of the one before it, but nothing that is not there yet is waited for while an O is due: the next unit's
+        // rows may be waiting in turn for whoever waits for that O.
+        int done = 0;                                 // tiles whose O has been asked for
+        bool end = false;                             // no more tiles
+        bool first_a = false, first_b = false;        // of the tiles in between, in order: whether they begin a unit, and their sets
+        int set_a = 0, set_b = 0;
+        auto there = [&](const uint64_t* b, uint32_t parity, bool wait) {
+            if (wait) return live = wait_bar(bar(b), parity, abort_flag, a.dev_status) && live;
+            return __shfl_sync(0xFFFFFFFFu, (int)mbar_test_wait(bar(b), parity), 0) != 0;
         };
-        auto issue_o = [&](int t, bool first, int unit) {
-            const int s = t % kStages, b = t & 1;
-            live = wait_bar(bar(&ctrl.p_full[b]), (uint32_t)(t >> 1) & 1u, abort_flag, a.dev_status) && live;
-            if (first && unit > 0) live = wait_bar(bar(&ctrl.o_empty), ((uint32_t)unit & 1u) ^ 1u, abort_flag, a.dev_status) && live;
+        while (live) {
+            const bool due = ahead != done;
+            const int s = ahead % C::kStages;
+            bool go = !end && ahead - done < 2 && there(&ctrl.full[s], (uint32_t)(ahead / C::kStages) & 1u, !due);
+            const int kind = go ? *const_cast<volatile int32_t*>(&s_tiles[s].kind) : 0, qb = (kind & kOdd) ? 1 : 0;
+            if (kind & kLast) end = true, go = false;
+            if (go && (kind & kFirst) && !there(&ctrl.q_ready[qb], (uint32_t)(qb == 0 ? ready0 : ready1) & 1u, !due)) go = false;
+            if (go && live) {
+                const int b = ahead & 1, set = C::kSets == 2 ? qb : 0;
+                const int mine = set == 0 ? asked0++ : asked1++;
+                if (kind & kFirst) ++(qb == 0 ? ready0 : ready1);
+                if (ahead >= 2) live = wait_bar(bar(&ctrl.s_empty[b]), ((uint32_t)(ahead >> 1) & 1u) ^ 1u, abort_flag, a.dev_status) && live;
+                tc_fence_after();
+                if (leader && live) {
+                    const uint64_t at = (uint64_t)(s * (kStageBytes >> 4)), qa = (uint64_t)(qb * (C::kQBytes >> 4));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) umma_f8(tm + (b ? C::kSCol1 : 0u), k_desc + at + j * 2, q_desc + qa + j * 2, idesc_s, j > 0);      // 32 elements a step
+                    umma_commit(bar(&ctrl.s_full[set][mine & 1]));
+                }
+                __syncwarp();
+                if (ahead == done) first_a = (kind & kFirst) != 0, set_a = set;
+                else first_b = (kind & kFirst) != 0, set_b = set;
+                ++ahead;
+                if (ahead - done < 2) continue;
+            }
+            if (ahead == done) {
+                if (end) break;
+                continue;
+            }
+            const int so = done % C::kStages, bo = done & 1;
+            live = wait_bar(bar(&ctrl.p_full[bo]), (uint32_t)(done >> 1) & 1u, abort_flag, a.dev_status) && live;
+            if (first_a) {
+                const int n = set_a == 0 ? begun0++ : begun1++;
+                if (n > 0) live = wait_bar(bar(&ctrl.o_empty[set_a]), ((uint32_t)n & 1u) ^ 1u, abort_flag, a.dev_status) && live;
+            }
             tc_fence_after();
             if (leader && live) {
-                const uint64_t at = (uint64_t)(s * (kStageBytes >> 4)), pa = (uint64_t)(b * (C::kPBytes >> 4));
+                const uint64_t at = (uint64_t)(so * (kStageBytes >> 4)), pa = (uint64_t)(bo * (C::kPBytes >> 4));
 #pragma unroll
                 for (int j = 0; j < 4; ++j)           // 32 keys a step: 4 groups of 8 lines of V
-                    umma_f8(tm + C::kOCol, v_desc + at + j * (4096 >> 4), p_desc + pa + j * 2, idesc_o, !first || j > 0);
-                umma_commit(bar(&ctrl.p_empty[b]));
-                umma_commit(bar(&ctrl.empty[s]));
+                    umma_f8(tm + C::kOCol + set_a * C::kOSet, v_desc + at + j * (4096 >> 4), p_desc + pa + j * 2, idesc_o, !first_a || j > 0);
+                umma_commit(bar(&ctrl.p_empty[bo]));
+                umma_commit(bar(&ctrl.empty[so]));
             }
-        };
-        while (live && walk.next(u)) {
-            const int n = u.u1 - u.u0;
-            if (n <= 0) continue;
-            const int t0 = tiles, unit = units;
-            issue_s(true);
-            for (int i = 0; i < n && live; ++i) {
-                if (i + 1 < n) issue_s(false);        // one ahead, but not into the next unit: its rows are made ready when this one is done
-                issue_o(t0 + i, i == 0, unit);
-            }
+            __syncwarp();
+            ++done;
+            first_a = first_b, set_a = set_b;
         }
         if (leader) umma_commit(bar(&ctrl.drained));  // nothing of the tensor cores' is in flight when TMEM and shared memory are given up
         const long long c0 = clock64();
         while (!mbar_try_wait(bar(&ctrl.drained), 0))
             if (clock64() - c0 > kTimeoutCycles) break;
         __syncwarp();
-    } else {
-        // ============================================================ a key per thread
-        const int q4 = warp & 3, key_lane = q4 * 32 + lane;      // the quarter of TMEM's lanes that this warp may access
-        const int kt = tid - 64;                                 // 0 .. 127
-        const uint32_t lane_addr = (uint32_t)(q4 * 32) << 16;
-        const int64_t w = blockIdx.x;
+    } else if (warp == 2) {
+        // ============================================================ the rows of the units, one unit ahead
+        Unit u;
         CutUnit cut{0, 0, 0, 0};
-        int tiles = 0;
-        // (after an abort the waits fall through and everybody goes on to the end together: nobody is left at a barrier)
-        while (walk.next(u)) {
-            const int n = max(u.u1 - u.u0, 0);
-            auto token_of = [&](int r) { return (u.tile_row + min(r, u.n_rows - 1)) / group; };
-            float m[ROWS], l[ROWS], rowf[ROWS];
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) m[r] = kNone, l[r] = 0.f;
-            if (n > 0) {
-                // ---- q's terms: four threads a row, 32 elements each
-                const int row = kt >> 2, part = kt & 3;
-                const bool have = row < u.n_rows;
-                float x[32], amax = 0.f;
-                if (have) {
-                    const int token = token_of(row), qh = u.head * group + (u.tile_row + row - token * group);
-                    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + ((int64_t)u.sq.row0 + token) * a.ldq + (int64_t)qh * kDim + part * 32;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) unpack<__nv_bfloat16>(ld128_rw_stream(q + i * 8), x + i * 8);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) x[i] = 0.f;
+        const int share = (int)blockIdx.x;
+        int tiles = 0, ends = 0;
+        for (int k = 0; ends < C::kSets; ++k) {
+            if (ends > 0 || !walk.next(u)) ++ends;
+            if (k >= 2) wait_bar(bar(&ctrl.q_empty[k & 1]), ((uint32_t)(k >> 1) & 1u) ^ 1u, abort_flag, a.dev_status);
+            if (*abort_flag) break;
+            __syncwarp();
+            Rows<ROWS>& rows = s_rows[k & 1];
+            if (ends > 0) {                           // for every set: there are no more units
+                if (lane == 0) {
+                    rows.tiles = -1;
+                    mbar_arrive(bar(&ctrl.q_full[k & 1]));
                 }
+                continue;
+            }
+            const bool begins = u.first == 0, whole = begins && u.last == u.sp.steps;
+            if (begins && !whole) cut.b = u.b, cut.row_tile = u.tile, cut.head = u.head, cut.pieces = walk.pieces(u, share);
+            const int n = max(u.u1 - u.u0, 0);
+            if (lane == 0) {
+                rows.tile0 = tiles, rows.tiles = n, rows.key0 = u.sp.lo + u.u0 * kKeys, rows.n_rows = u.n_rows;
+                rows.hi_min = u.hi_min, rows.hi_max = u.hi_max, rows.lo_min = u.lo_min, rows.lo_max = u.lo_max;
+                rows.slot = whole ? -1 : 2 * share + (begins ? 1 : 0);
+            }
+            tiles += n;
+            const int row = min(lane, u.n_rows - 1);
+            const int token = (u.tile_row + row) / group, qh = u.head * group + (u.tile_row + row - token * group);
+            const int64_t in = ((int64_t)u.sq.row0 + token) * a.ldq + (int64_t)qh * kDim;
+            if (lane < ROWS) {
+                rows.lower[lane] = lower_key(a, u.sq, token);
+                rows.upper[lane] = upper_key(a, u.sq, token);
+                rows.out[lane] = ((int64_t)u.sq.row0 + token) * a.ldo + (int64_t)qh * kDim;
+                rows.lse[lane] = ((int64_t)u.sq.row0 + token) * a.heads + qh;
+            }
+            uint4 q[ROWS / 2];                        // half a warp a row, eight elements a lane; asked for together
 #pragma unroll
-                for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(x[i]));
-                amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-                amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+            for (int i = 0; i < ROWS / 2; ++i) {
+                const int r = 2 * i + (lane >> 4);
+                const int64_t from = __shfl_sync(0xFFFFFFFFu, in, r);
+                q[i] = r < u.n_rows ? ld128_rw_stream(static_cast<const __nv_bfloat16*>(a.q) + from + (lane & 15) * 8) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < ROWS / 2; ++i) {
+                const int r = 2 * i + (lane >> 4), chunk = lane & 15;
+                float x[8], amax = 0.f;
+                unpack<__nv_bfloat16>(q[i], x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
                 const int e = amax > 0.f ? min(100, 7 - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
                 const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-                if (row < ROWS) {
-                    if (part == 0) s_row[row] = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
+                if (chunk == 0) rows.factor[r] = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) x[i] *= up;
+                for (int z = 0; z < 8; ++z) x[z] *= up;
 #pragma unroll
-                    for (int t = 0; t < kTermsQ; ++t)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint32_t c[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint32_t lo = split_pair(x[16 * h + 4 * i], x[16 * h + 4 * i + 1]);
-                                c[i] = lo | (split_pair(x[16 * h + 4 * i + 2], x[16 * h + 4 * i + 3]) << 16);
-                            }
-                            *reinterpret_cast<uint4*>(smem + (q_at - base) + line_offset(t * ROWS + row, part * 32 + h * 16)) = make_uint4(c[0], c[1], c[2], c[3]);
-                        }
+                for (int z = 0; z < kTermsQ; ++z) {
+                    uint2 c;
+                    c.x = split_pair(x[0], x[1]);
+                    c.x |= split_pair(x[2], x[3]) << 16;
+                    c.y = split_pair(x[4], x[5]);
+                    c.y |= split_pair(x[6], x[7]) << 16;
+                    *reinterpret_cast<uint2*>(smem + (q_at - base) + (k & 1) * C::kQBytes + line_offset(z * ROWS + r, chunk * 8)) = c;
                 }
-                fence_proxy_async_smem();
-                mbar_arrive(bar(&ctrl.q_full));
-                key_threads_sync();
-#pragma unroll
-                for (int r = 0; r < ROWS; ++r) rowf[r] = s_row[r];
             }
-            for (int i = 0; i < n; ++i, ++tiles) {
-                const int s = tiles % kStages, b = tiles & 1;
-                wait_bar(bar(&ctrl.s_full[b]), (uint32_t)(tiles >> 1) & 1u, abort_flag, a.dev_status);
-                wait_bar(bar(&ctrl.full[s]), (uint32_t)(tiles / kStages) & 1u, abort_flag, a.dev_status);      // (long complete: for the scales and V in shared memory)
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(bar(&ctrl.q_full[k & 1]));
+                if (n > 0) mbar_arrive(bar(&ctrl.q_ready[k & 1]));
+            }
+        }
+        if (lane == 0) cuts[blockIdx.x] = *abort_flag == 0 ? cut : CutUnit{0, 0, 0, 0};
+    } else if (warp >= kFirstGroupWarp) {
+        // ============================================================ a key per thread
+        const int q4 = warp & 3, key_lane = q4 * 32 + lane;      // the quarter of TMEM's lanes that this warp may access
+        const int all = (warp - kFirstGroupWarp) >> 2, set = all / C::kGroups, gr = all % C::kGroups, r0 = gr * RPG;
+        const uint32_t o_col = C::kOCol + set * C::kOSet;
+        const uint32_t lane_addr = (uint32_t)(q4 * 32) << 16;
+        uint32_t p_off[RPG];                          // of this key in the lines of the weights
+#pragma unroll
+        for (int r = 0; r < RPG; ++r) p_off[r] = (uint32_t)(((((key_lane >> 4) ^ (r0 + r)) & 7) << 4) + (key_lane & 15));
+        int own = 0;                                  // tiles of this set so far
+        for (int k = set;; k += C::kSets) {
+            wait_bar(bar(&ctrl.q_full[k & 1]), (uint32_t)(k >> 1) & 1u, abort_flag, a.dev_status);
+            // after an abort the waits fall through: a set leaves here together, or goes on to the end of its unit together, so that nobody is left
+            // at a barrier
+            if (threads_any<C::kKeyThreads>(14 + set, *abort_flag != 0)) break;
+            const Rows<ROWS>& rows = s_rows[k & 1];
+            const int n = rows.tiles, n_rows = rows.n_rows, hi_min = rows.hi_min, hi_max = rows.hi_max, lo_min = rows.lo_min, lo_max = rows.lo_max;
+            if (n < 0) break;
+            int tiles = rows.tile0, key0 = rows.key0;
+            float m[RPG], l[RPG], rowf[RPG];
+#pragma unroll
+            for (int r = 0; r < RPG; ++r) m[r] = kNone, l[r] = 0.f, rowf[r] = rows.factor[r0 + r];
+#pragma unroll 1
+            for (int i = 0; i < n; ++i, ++tiles, ++own, key0 += kKeys) {
+                const int b = tiles & 1;
+                wait_bar(bar(&ctrl.s_full[set][own & 1]), (uint32_t)(own >> 1) & 1u, abort_flag, a.dev_status);
+                const int s = tiles % C::kStages;
+                wait_bar(bar(&ctrl.full[s]), (uint32_t)(tiles / C::kStages) & 1u, abort_flag, a.dev_status);      // (long complete: for what was written there)
                 __syncwarp();
                 tc_fence_after();
-                float y[ROWS];
+                const float4 sc = s_tiles[s].scale[key_lane >> 4];
+                float y[RPG];
                 {
-                    uint32_t v[C::kNS];
-                    tmem_load<C::kNS>(tmem + lane_addr + (b ? C::kSCol1 : C::kSCol0), v);
+                    uint32_t v0[RPG], v1[RPG];
+                    const uint32_t at = tmem + lane_addr + (b ? C::kSCol1 : 0u) + r0;
+                    tmem_load<RPG>(at, v0);
+                    tmem_load<RPG>(at + ROWS, v1);
+                    tmem_wait_ld();
 #pragma unroll
-                    for (int r = 0; r < ROWS; ++r) y[r] = fmaf(__uint_as_float(v[ROWS + r]), 1.f / kTermStep, __uint_as_float(v[r]));
+                    for (int r = 0; r < RPG; ++r) y[r] = fmaf(__uint_as_float(v1[r]), 1.f / kTermStep, __uint_as_float(v0[r]));
                 }
                 tc_fence_before();
                 mbar_arrive(bar(&ctrl.s_empty[b]));
-                const float4 sc = s_scales[s][key_lane >> 4];
-                const int key = u.sp.lo + (u.u0 + i) * kKeys + key_lane;
-                // (the bounds of a tile are the same for all threads; whether a page is missing is not known to all, but matters to its keys only)
-                const int key0 = key - key_lane;
-                const bool border = key0 + kKeys > u.hi_min || key0 < u.lo_max;
-                float ks = fmaxf(sc.x, 1.17549435e-38f);
-                bool hidden = false, poisoned = false;
-                if (border || sc.w == 0.f) {
+                const int key = key0 + key_lane;
+                const bool border = key0 + kKeys > hi_min || key0 < lo_max;
+                // y: the logarithm of what the key contributes to the row, over the row's reference
+                float c[RPG], e[RPG], top = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < RPG; ++r) {
+                    c[r] = rowf[r] * sc.x;
+                    e[r] = fmaf(y[r], c[r], sc.y - m[r]);
+                }
+                const bool hidden = sc.w == 0.f || key >= hi_max || key < lo_min;      // no row sees the key, or its page cannot be used
+                if (border || hidden) {
                     // A value that no row sees counts as zero; a NaN among the codes of one becomes a NaN in the scores of the rows that see it and a
                     // zero here, so that it cannot reach the others through their weight of zero.
-                    hidden = sc.w == 0.f || key >= u.hi_max || key < u.lo_min;
                     uint8_t* line = smem + s * kStageBytes + kTileBytes + key_lane * 128;
+                    bool nan = false;
+                    if (!hidden)
+#pragma unroll 2
+                        for (int c = 0; c < 8; ++c) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(line + ((c ^ lane) & 7) * 16);
+                            nan |= (e4m3x4_nan_bits(x.x) | e4m3x4_nan_bits(x.y) | e4m3x4_nan_bits(x.z) | e4m3x4_nan_bits(x.w)) != 0;
+                        }
+                    if (border && C::kGroups > 1) sync_threads_of<C::kKeyThreads>(14 + set);      // every group has looked
+                    if (gr == 0 && (hidden || nan))
+#pragma unroll 2
+                        for (int c = 0; c < 8; ++c) {
+                            uint4 x = *reinterpret_cast<const uint4*>(line + ((c ^ lane) & 7) * 16);
+                            x.x &= hidden ? 0u : ~((e4m3x4_nan_bits(x.x) >> 7) * 0xFFu), x.y &= hidden ? 0u : ~((e4m3x4_nan_bits(x.y) >> 7) * 0xFFu);
+                            x.z &= hidden ? 0u : ~((e4m3x4_nan_bits(x.z) >> 7) * 0xFFu), x.w &= hidden ? 0u : ~((e4m3x4_nan_bits(x.w) >> 7) * 0xFFu);
+                            *reinterpret_cast<uint4*>(line + ((c ^ lane) & 7) * 16) = x;
+                        }
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        uint4* at = reinterpret_cast<uint4*>(line + ((c ^ key_lane) & 7) * 16);
-                        uint4 x = hidden ? make_uint4(0, 0, 0, 0) : *at;
-                        const uint32_t n0 = e4m3x4_nan_bits(x.x), n1 = e4m3x4_nan_bits(x.y), n2 = e4m3x4_nan_bits(x.z), n3 = e4m3x4_nan_bits(x.w);
-                        const bool nan = (n0 | n1 | n2 | n3) != 0;
-                        poisoned |= nan;
-                        if (hidden || nan)
-                            *at = make_uint4(x.x & ~((n0 >> 7) * 0xFFu), x.y & ~((n1 >> 7) * 0xFFu), x.z & ~((n2 >> 7) * 0xFFu), x.w & ~((n3 >> 7) * 0xFFu));
-                    }
-                    if (hidden) ks = 1.f;
-#pragma unroll
-                    for (int r = 0; r < ROWS; ++r) {
-                        const int token = token_of(r);
-                        const bool sees = !hidden && key < upper_key(a, u.sq, token) && key >= lower_key(a, u.sq, token);
-                        y[r] = !sees ? -INFINITY : poisoned ? kNan : y[r];
+                    for (int r = 0; r < RPG; ++r) {
+                        const bool sees = !hidden && key < rows.upper[r0 + r] && key >= rows.lower[r0 + r];
+                        if (!sees || nan) y[r] = e[r] = sees ? kNan : -INFINITY, c[r] = 1.f;
                     }
                 }
-                // y: the weight's exponent over the row's reference
-                bool over = false;
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) {
-                    y[r] = fmaf(y[r], fmaxf(rowf[r] * ks, 1.17549435e-38f), sc.y);
-                    over |= y[r] - m[r] > kTop + kSlack;
-                }
-                if (key_threads_any(over)) {
-                    float shrink[ROWS];
+                for (int r = 0; r < RPG; ++r) top = fmaxf(top, e[r]);
+                if (threads_any<128>(1 + all, top > kTop + kSlack)) {
+                    float shrink[RPG];
 #pragma unroll
-                    for (int r = 0; r < ROWS; ++r) {
-                        const float top = warp_max(y[r]);
-                        if (lane == 0) s_part[q4][r] = top;
+                    for (int r = 0; r < RPG; ++r) {
+                        y[r] = fmaf(y[r], c[r], sc.y);      // (not from e: m may be the reference of a row that has seen nothing)
+                        const float most = warp_max(y[r]);
+                        if (lane == 0) s_part[all][q4][r] = most;
                     }
-                    key_threads_sync();
+                    sync_threads_of<128>(1 + all);
 #pragma unroll
-                    for (int r = 0; r < ROWS; ++r) {
-                        const float top = fmaxf(fmaxf(s_part[0][r], s_part[1][r]), fmaxf(s_part[2][r], s_part[3][r]));
+                    for (int r = 0; r < RPG; ++r) {
+                        const float top = fmaxf(fmaxf(s_part[all][0][r], s_part[all][1][r]), fmaxf(s_part[all][2][r], s_part[all][3][r]));
                         const float next = top - m[r] > kTop ? top - kTop : m[r];
                         shrink[r] = ex2(m[r] - next);
                         m[r] = next;
                         l[r] *= shrink[r];
+                        e[r] = y[r] - next;
                     }
                     if (i > 0) {                      // what is in O already: the MMAs of the tile before are done, those of this one wait for its weights
                         wait_bar(bar(&ctrl.p_empty[b ^ 1]), (uint32_t)((tiles - 1) >> 1) & 1u, abort_flag, a.dev_status);
                         __syncwarp();
                         tc_fence_after();
+#pragma unroll 1
+                        for (int z = 0; z < kTermsP; ++z) {
+                            uint32_t v[RPG];
+                            tmem_load<RPG>(tmem + lane_addr + o_col + z * ROWS + r0, v);
+                            tmem_wait_ld();
 #pragma unroll
-                        for (int t = 0; t < kTermsP; ++t) {
-                            uint32_t v[ROWS];
-                            tmem_load<ROWS>(tmem + lane_addr + C::kOCol + t * ROWS, v);
-#pragma unroll
-                            for (int r = 0; r < ROWS; ++r) v[r] = __float_as_uint(__uint_as_float(v[r]) * shrink[r]);
-#pragma unroll
-                            for (int r = 0; r < ROWS; r += 8) tmem_st<8>(tmem + lane_addr + C::kOCol + t * ROWS + r, v + r);
+                            for (int r = 0; r < RPG; ++r) v[r] = __float_as_uint(__uint_as_float(v[r]) * shrink[r]);
+                            tmem_st<RPG>(tmem + lane_addr + o_col + z * ROWS + r0, v);
                         }
                         tmem_wait_st();
                         tc_fence_before();
                     }
-                    key_threads_sync();               // (s_part is free again)
+                    sync_threads_of<128>(1 + all);     // (s_part is free again)
                 }
                 if (tiles >= 2) wait_bar(bar(&ctrl.p_empty[b]), ((uint32_t)(tiles >> 1) & 1u) ^ 1u, abort_flag, a.dev_status);
-                uint8_t* const p = smem + (p_at - base) + b * C::kPBytes;
+                uint8_t* const p = smem + (p_at - base) + b * C::kPBytes + r0 * 128;
 #pragma unroll
-                for (int r = 0; r < ROWS; r += 2) {
-                    float w0 = ex2(y[r] - m[r]), w1 = ex2(y[r + 1] - m[r + 1]);
+                for (int r = 0; r < RPG; r += 2) {
+                    const float w0 = ex2(e[r]), w1 = ex2(e[r + 1]);
                     l[r] = fmaf(w0, sc.z, l[r]), l[r + 1] = fmaf(w1, sc.z, l[r + 1]);
+                    __half2 rest = __floats2half2_rn(w0, w1);
 #pragma unroll
-                    for (int t = 0; t < kTermsP; ++t) {
-                        const uint32_t c = split_pair(w0, w1);
-                        p[line_offset(t * ROWS + r, key_lane)] = (uint8_t)c;
-                        p[line_offset(t * ROWS + r + 1, key_lane)] = (uint8_t)(c >> 8);
+                    for (int z = 0; z < kTermsP; ++z) {
+                        const uint32_t code = __nv_cvt_halfraw2_to_fp8x2(rest, __NV_SATFINITE, __NV_E4M3);
+                        const uint32_t back = e4m3x2_to_f16x2(code);
+                        rest = __hmul2(__hsub2(rest, *reinterpret_cast<const __half2*>(&back)), __float2half2_rn(kTermStep));
+                        // line z ROWS + r0 + r: r0 is a multiple of 4 (and of 8 where groups have 8 rows)
+                        const uint32_t swz = (uint32_t)((z * ROWS) & 7) << 4;
+                        p[(z * ROWS + r) * 128 + (p_off[r] ^ swz)] = (uint8_t)code;
+                        p[(z * ROWS + r + 1) * 128 + (p_off[r + 1] ^ swz)] = (uint8_t)(code >> 8);
                     }
                 }
                 fence_proxy_async_smem();
@@ -415,14 +541,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mbar_arrive(bar(&ctrl.p_full[b]));
             }
             // ---- the unit's result, or a piece of it: an element per thread
-            const bool begins = u.first == 0, ends = u.last == u.sp.steps, whole = begins && ends;
-            if (begins && !ends) {
-                cut.b = u.b, cut.row_tile = u.tile, cut.head = u.head;
-                cut.pieces = walk.pieces(u, w);
-            }
-            float o[ROWS];
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) o[r] = 0.f;
+            for (int r = 0; r < RPG; ++r) {
+#pragma unroll
+                for (int z = 16; z > 0; z >>= 1) l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], z);
+                if (lane == 0) s_part[all][q4][r] = l[r];
+            }
+            float o[RPG];
+#pragma unroll
+            for (int r = 0; r < RPG; ++r) o[r] = 0.f;
             if (n > 0) {
                 const int t = tiles - 1;
                 wait_bar(bar(&ctrl.p_empty[t & 1]), (uint32_t)(t >> 1) & 1u, abort_flag, a.dev_status);
@@ -431,40 +558,35 @@ __global__ void __launch_bounds__(kThreads, 1)
                 float f = 1.f;
 #pragma unroll
                 for (int z = 0; z < kTermsP; ++z, f /= kTermStep) {
-                    uint32_t v[ROWS];
-                    tmem_load<ROWS>(tmem + lane_addr + C::kOCol + z * ROWS, v);
+                    uint32_t v[RPG];
+                    tmem_load<RPG>(tmem + lane_addr + o_col + z * ROWS + r0, v);
+                    tmem_wait_ld();
 #pragma unroll
-                    for (int r = 0; r < ROWS; ++r) o[r] = fmaf(__uint_as_float(v[r]), f, o[r]);
+                    for (int r = 0; r < RPG; ++r) o[r] = fmaf(__uint_as_float(v[r]), f, o[r]);
                 }
                 tc_fence_before();
-                mbar_arrive(bar(&ctrl.o_empty));
+                mbar_arrive(bar(&ctrl.o_empty[set]));
             }
             const bool live = *abort_flag == 0;       // (nothing of an aborted call is stored)
+            sync_threads_of<128>(1 + all);
+            const int at_slot = rows.slot;
+            float* slot = slots + at_slot * (int64_t)slot_floats(ROWS, kDim);
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-#pragma unroll
-                for (int z = 16; z > 0; z >>= 1) l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], z);
-                if (lane == 0) s_part[q4][r] = l[r];
-            }
-            key_threads_sync();
-            float* slot = slots + (2 * w + (begins ? 1 : 0)) * (int64_t)slot_floats(ROWS, kDim);
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                if (r >= u.n_rows || !live) continue;
-                const float sum = (s_part[0][r] + s_part[1][r]) + (s_part[2][r] + s_part[3][r]);
-                if (whole) {
-                    const int token = token_of(r), qh = u.head * group + (u.tile_row + r - token * group);
-                    const int64_t orow = (int64_t)u.sq.row0 + token;
-                    static_cast<__nv_bfloat16*>(a.out)[orow * a.ldo + (int64_t)qh * kDim + key_lane] = __float2bfloat16(sum == 0.f ? 0.f : o[r] / sum);
-                    if (a.lse != nullptr && kt == 0) a.lse[orow * a.heads + qh] = sum == 0.f ? -INFINITY : (m[r] + log2f(sum)) * 0.69314718056f;
+            for (int r = 0; r < RPG; ++r) {
+                const int row = r0 + r;
+                if (row >= n_rows || !live) continue;
+                const float sum = (s_part[all][0][r] + s_part[all][1][r]) + (s_part[all][2][r] + s_part[all][3][r]);
+                if (at_slot < 0) {
+                    static_cast<__nv_bfloat16*>(a.out)[rows.out[row] + key_lane] = __float2bfloat16(sum == 0.f ? 0.f : __fdividef(o[r], sum));
+                    if (a.lse != nullptr && key_lane == 0) a.lse[rows.lse[row]] = sum == 0.f ? -INFINITY : (m[r] + log2f(sum)) * 0.69314718056f;
                 } else {
-                    slot[2 * ROWS + r * kDim + key_lane] = o[r];
-                    if (kt == 0) slot[r] = m[r], slot[ROWS + r] = sum;
+                    slot[2 * ROWS + row * kDim + key_lane] = o[r];
+                    if (key_lane == 0) slot[row] = m[r], slot[ROWS + row] = sum;
                 }
             }
-            key_threads_sync();                       // (s_part, s_row)
+            mbar_arrive(bar(&ctrl.q_empty[k & 1]));
+            sync_threads_of<128>(1 + all);             // (s_part)
         }
-        if (kt == 0) cuts[w] = *abort_flag == 0 ? cut : CutUnit{0, 0, 0, 0};
     }
     tc_fence_before();
     __syncthreads();
@@ -472,7 +594,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 template <int ROWS>
-int64_t share_count() { return (int64_t)sm_count() * kWaves; }
+int64_t share_count() { return sm_count(); }
 
 template <int ROWS>
 size_t bytes_needed() { return cut_bytes(share_count<ROWS>()) + (size_t)(2 * share_count<ROWS>() * slot_floats(ROWS, kDim)) * sizeof(float); }
@@ -496,9 +618,9 @@ molora_status_t launch(const AttendArgs& a, void* ws, cudaStream_t s)
     const int64_t shares = share_count<ROWS>();
     CutUnit* cuts = static_cast<CutUnit*>(ws);
     float* slots = reinterpret_cast<float*>(static_cast<char*>(ws) + cut_bytes(shares));
-    if (launch_kernel(attend_stream_kernel<ROWS>, dim3((unsigned)shares), dim3(kThreads), C::kSmem, s, 1, true, a, tm_k, tm_v, cuts, slots) != cudaSuccess)
+    if (launch_kernel(attend_stream_kernel<ROWS>, dim3((unsigned)shares), dim3(C::kThreads), C::kSmem, s, 1, true, a, tm_k, tm_v, cuts, slots) != cudaSuccess)
         return MOLORA_ERR_CUDA;
-    return cuda_ok(launch_kernel(attend_join_kernel<__nv_bfloat16, kDim, ROWS>, dim3((unsigned)shares, ROWS / 8), dim3(kJoinWarps * 32), 0, s, 1, true, a,
+    return cuda_ok(launch_kernel(attend_join_kernel<__nv_bfloat16, kDim, ROWS>, dim3((unsigned)shares, ROWS / kJoinRows), dim3(kJoinWarps * 32), 0, s, 1, true, a,
                                  static_cast<const CutUnit*>(cuts), static_cast<const float*>(slots)));
 }
 
@@ -512,12 +634,12 @@ bool attend_stream_eligible(const KvView& c, molora_dtype_t dt, int64_t rows)
 
 size_t attend_stream_workspace_bytes(int64_t rows)
 {
-    return rows <= 8 ? bytes_needed<8>() : rows <= 16 ? bytes_needed<16>() : rows <= 24 ? bytes_needed<24>() : bytes_needed<32>();
+    return rows <= 4 ? bytes_needed<4>() : rows <= 8 ? bytes_needed<8>() : rows <= 16 ? bytes_needed<16>() : rows <= 24 ? bytes_needed<24>() : bytes_needed<32>();
 }
 
 molora_status_t launch_attend_stream(const AttendArgs& a, int64_t rows, void* ws, cudaStream_t s)
 {
-    return rows <= 8 ? launch<8>(a, ws, s) : rows <= 16 ? launch<16>(a, ws, s) : rows <= 24 ? launch<24>(a, ws, s) : launch<32>(a, ws, s);
+    return rows <= 4 ? launch<4>(a, ws, s) : rows <= 8 ? launch<8>(a, ws, s) : rows <= 16 ? launch<16>(a, ws, s) : rows <= 24 ? launch<24>(a, ws, s) : launch<32>(a, ws, s);
 }
 
 }  // namespace molora
