@@ -77,8 +77,8 @@ size_t molora_kv_attend_workspace_bytes(molora_dtype_t dt, int32_t heads, int32_
     if ((dim != 64 && dim != 128) || kv_heads < 1 || heads < 1 || heads % kv_heads != 0 || max_tokens < 1 || (dt != MOLORA_F32 && dt != MOLORA_BF16)) return 0;
     // (the choice of kernel depends on the pool too, which is not known here)
     const int64_t rows = max_tokens * (heads / kv_heads);
-    const size_t stream = dt == MOLORA_BF16 && dim == 128 && rows <= 32 ? attend_stream_workspace_bytes(rows) : 0;
-    return std::max(stream, attend_rows_workspace_bytes(dt, dim, rows));
+    const size_t other = dt != MOLORA_BF16 || dim != 128 ? 0 : rows <= 32 ? attend_stream_workspace_bytes(rows) : attend_tiles_workspace_bytes();
+    return std::max(other, attend_rows_workspace_bytes(dt, dim, rows));
 }
 
 molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_sequences_t* seqs, molora_dtype_t dt, int64_t N, const void* q,
@@ -103,6 +103,7 @@ molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_se
     a.dev_status = dev_status;
     const int64_t rows = max_tokens * (heads / cache->kv_heads);
     if (attend_stream_eligible(a.c, dt, rows)) return launch_attend_stream(a, rows, ws, static_cast<cudaStream_t>(stream));
+    if (rows > 32 && attend_tiles_eligible(a.c, dt)) return launch_attend_tiles(a, ws, static_cast<cudaStream_t>(stream));
     return launch_attend_rows(a, dt, rows, ws, static_cast<cudaStream_t>(stream));
 }
 

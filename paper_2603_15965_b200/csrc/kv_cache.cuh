@@ -96,6 +96,9 @@ molora_status_t launch_attend_rows(const AttendArgs& a, molora_dtype_t dt, int64
 bool attend_stream_eligible(const KvView& c, molora_dtype_t dt, int64_t rows);
 size_t attend_stream_workspace_bytes(int64_t rows);
 molora_status_t launch_attend_stream(const AttendArgs& a, int64_t rows, void* ws, cudaStream_t s);
+bool attend_tiles_eligible(const KvView& c, molora_dtype_t dt);
+size_t attend_tiles_workspace_bytes();
+molora_status_t launch_attend_tiles(const AttendArgs& a, void* ws, cudaStream_t s);
 molora_status_t launch_verify_drafts(const void* target, int64_t tls, int64_t tl, const void* draft, int64_t dls, int64_t dl, molora_dtype_t dt,
                                      const int32_t* drafted, const int32_t* n_drafted, const float* uniform, int32_t B, int32_t S, int32_t V,
                                      int32_t* tokens, int32_t* accepted, uint32_t* dev_status, cudaStream_t s);
