@@ -7,8 +7,9 @@
 //   warps 0-3, 4-7  a row per thread of tile 0 and 1: q to fp16 by a power of two, weights of a tile (S_t -> P_t), the sum, the result.  Nothing
 //                   is shared between rows, so nothing is synchronised; the reference of a row moves when a score is 2^8 over the weight that its
 //                   largest was given, and then O_t is rescaled (by warps: TMEM is read and written by whole warps)
-//   warps 8-11      codes -> fp16, two tiles of 128 keys of K and of V ahead
+//   warps 8-11      codes -> fp16, two tiles of 128 keys of K and of V ahead, the codes of the next tile on their way in registers
 //   warp 12         the MMAs: O_0 S_0 O_1 S_1 ... -- while the weights of one tile are worked out, the other has the tensor cores
+//   warp 13         units, pages and scales, into queues: what depends on one another there is waited for long before it is needed
 // S_t of the next keys is asked for right behind O_t of the last, which is the last to read P_t: the tensor cores work in the order of issue.
 // TMEM: S_0 S_1 O_0 O_1, 128 columns each.  Shared memory: Q 64 KB, K and V 2 x 32 KB each.
 // Shares, pieces and the join as in kv_attend.cuh, but with the steps that each tile of rows really sees.
@@ -20,20 +21,38 @@ namespace molora {
 namespace {
 
 constexpr int kDim = 128, kKeys = 128, kTileRows = 128, kUnitRows = 256;
-constexpr int kThreads = 416;
+constexpr int kThreads = 448;
 constexpr int kConvWarp0 = 8, kMmaWarp = 12;
 constexpr int kOperandBytes = 128 * kDim * 2;                 // of a Q tile, of a tile of K or of V, in fp16
 constexpr int kQAt = 0, kKAt = 2 * kOperandBytes, kVAt = 4 * kOperandBytes;
 constexpr size_t kSmem = 1024 + 6 * (size_t)kOperandBytes;
 constexpr uint32_t kTmemCols = 512, kOCol = 256;
-constexpr int kScaleRing = 4;
+constexpr int kTileQueue = 8, kUnitQueue = 4;
 constexpr int kUnitCost = 1, kMinShare = 2;                   // tiles of keys
 constexpr float kTop = 7.f, kSlack = 8.f;                     // a row's largest weight when its reference is set, and by how much it may grow: fp16
 
 struct Control {
-    uint64_t q_full[2], s_full[2], p_full[2], o_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
+    uint64_t q_full[2], s_full[2], p_full[2], o_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2];
+    uint64_t tile_full[kTileQueue], tile_empty[kTileQueue], unit_full[kUnitQueue], unit_empty[kUnitQueue], drained;
     uint32_t tmem_base;
     int abort_flag;
+};
+constexpr int kUnitReaders = kConvWarp0 + 1;                  // the warps of rows, the MMAs'
+
+// A tile of keys in the queue.
+struct KeyTile {
+    float4 scale[8];                           // of 16 keys: scale of K, logarithm and reciprocal of V's, whether their page can be used
+    int64_t line[8];                           // of 16 keys: the first one's line in the pool, -1: none
+    uint32_t nan[4];                           // keys with a NaN among the codes of V, where not every row sees every key
+    int32_t key0, hi_max, lo_min;
+    int32_t kind;                              // 0: every row sees every key, 1: not so, 2: no tile, there are no more
+};
+// A unit in the queue.
+struct UnitInfo {
+    int32_t row0, first_pos, len;              // of its sequence
+    int32_t tile_row, n_rows, head;
+    int32_t key0, n;                           // first key, tiles of keys; n -1: there are no more units
+    int32_t slot;                              // where its piece goes, -1: it is whole
 };
 
 // A unit's key range belongs to its tile of rows.
@@ -125,8 +144,6 @@ struct TileWalk {
     __device__ int32_t pieces(const TileUnit& u, int64_t w) const { return (int32_t)((u.at + u.steps - 1) / share - w + 1); }
 };
 
-__device__ __forceinline__ void umma_f16(uint32_t d, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, bool accumulate) { ptx::umma_bf16(d, a_desc, b_desc, idesc, accumulate); }
-
 // fp16 operands of kind::f16, fp32 accumulation
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, int b_mn_major)
 {
@@ -140,8 +157,10 @@ __device__ __forceinline__ void store_codes_f16(uint8_t* operand, int r, int c, 
     const int x = (2 * c) & 7;
     const uint4 lo = make_uint4(e4m3x2_to_f16x2(w.x), e4m3x2_to_f16x2_high(w.x), e4m3x2_to_f16x2(w.y), e4m3x2_to_f16x2_high(w.y));
     const uint4 hi = make_uint4(e4m3x2_to_f16x2(w.z), e4m3x2_to_f16x2_high(w.z), e4m3x2_to_f16x2(w.w), e4m3x2_to_f16x2_high(w.w));
-    *reinterpret_cast<uint4*>(line + ((x ^ (r & 7)) << 4)) = lo;
-    *reinterpret_cast<uint4*>(line + (((x + 1) ^ (r & 7)) << 4)) = hi;
+    // (the two parts of a line lie in the same banks: half of the lanes begin with the second of their pieces)
+    const int odd = c >> 2;
+    *reinterpret_cast<uint4*>(line + (((x + odd) ^ (r & 7)) << 4)) = odd ? hi : lo;
+    *reinterpret_cast<uint4*>(line + (((x + 1 - odd) ^ (r & 7)) << 4)) = odd ? lo : hi;
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -150,9 +169,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     using namespace ptx;
     __shared__ Control ctrl;
     __shared__ int64_t s_upto[kThreads];
-    __shared__ float4 s_scales[kScaleRing][8];        // of 16 keys: scale of K, logarithm and reciprocal of V's, whether their page can be used
-    __shared__ int32_t s_pages[kScaleRing][8];
-    __shared__ uint32_t s_nan[kScaleRing][4];         // keys with a NaN among the codes of V that not every row sees
+    __shared__ KeyTile s_tiles[kTileQueue];
+    __shared__ UnitInfo s_units[kUnitQueue];
     extern __shared__ uint8_t smem_raw[];
     const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -164,11 +182,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     grid_dependency_wait();
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(&ctrl.q_full[i]), kTileRows), mbar_init(bar(&ctrl.s_full[i]), 1);
+            mbar_init(bar(&ctrl.q_full[i]), 4), mbar_init(bar(&ctrl.s_full[i]), 1);
             mbar_init(bar(&ctrl.p_full[i]), kTileRows), mbar_init(bar(&ctrl.o_full[i]), 1);
             mbar_init(bar(&ctrl.k_full[i]), 128), mbar_init(bar(&ctrl.k_empty[i]), 1);
             mbar_init(bar(&ctrl.v_full[i]), 128), mbar_init(bar(&ctrl.v_empty[i]), 1);
         }
+        for (int i = 0; i < kTileQueue; ++i) mbar_init(bar(&ctrl.tile_full[i]), 1), mbar_init(bar(&ctrl.tile_empty[i]), 1);
+        for (int i = 0; i < kUnitQueue; ++i) mbar_init(bar(&ctrl.unit_full[i]), 1), mbar_init(bar(&ctrl.unit_empty[i]), kUnitReaders);
         mbar_init(bar(&ctrl.drained), 1);
         ctrl.abort_flag = 0;
         fence_mbar_init();
@@ -202,9 +222,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     grid_dependency_trigger();                        // (not before TMEM is mine)
     const uint32_t tmem = ctrl.tmem_base;
-    TileWalk walk(a);
-    walk.begin(s_upto, blockIdx.x);
-    TileUnit u{};
+    // unit k of the share, for a warp that reads them all in turn; given back by done_with
+    auto unit = [&](int k) {
+        wait_bar(bar(&ctrl.unit_full[k % kUnitQueue]), (uint32_t)(k / kUnitQueue) & 1u, abort_flag, a.dev_status);
+        UnitInfo u = s_units[k % kUnitQueue];
+        if (*abort_flag) u.n = -1;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(&ctrl.unit_empty[k % kUnitQueue]));
+        return u;
+    };
 
     if (warp < kConvWarp0) {
         // ============================================================ a row per thread
@@ -212,104 +238,107 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + lane_addr + (uint32_t)(t * 128), o_at = tmem + lane_addr + kOCol + (uint32_t)(t * 128);
         uint8_t* const q_tile = smem + kQAt + t * kOperandBytes;
-        int tiles = 0, units = 0;                     // key tiles of the share so far, and of this tile of rows units with any
-        int own = 0;                                  // key tiles that this tile of rows took part in
+        int tiles = 0, own = 0, finished = 0;         // key tiles of the share so far; of them, those that this tile of rows took part in; its Os
         float rowf = 0.f;
-        int token = 0, qh = 0;
-        // q of this row of unit u, as the A operand; the MMAs of S that read the last one are done
-        auto load_q = [&]() {
-            const int r = min(u.tile_row + t * kTileRows + row, u.tile_row + u.n_rows - 1);
-            token = r / group, qh = u.head * group + (r - token * group);
-            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + ((int64_t)u.sq.row0 + token) * a.ldq + (int64_t)qh * kDim;
-            uint4 w[16];
+        int64_t out_at = 0, lse_at = 0;
+        int hi_row = 0, lo_row = 0;
+        bool real = false;
+        auto takes_part = [&](const UnitInfo& u) { return t * kTileRows < u.n_rows; };
+        // This thread's row of unit u, and q of the warp's 32 rows as lines of the A operand (the MMAs of S that read the last ones are done):
+        // half a warp a row, eight elements a lane.
+        auto begin_unit = [&](const UnitInfo& u) {
+            const int mine = t * kTileRows + row, r = u.tile_row + min(mine, u.n_rows - 1);
+            const int token = r / group, qh = u.head * group + (r - token * group);
+            real = mine < u.n_rows;
+            hi_row = a.causal ? max(0, min(u.first_pos + token + 1, u.len)) : u.len;
+            lo_row = a.window > 0 ? max(0, u.first_pos + token - a.window + 1) : 0;
+            const int64_t at = (int64_t)u.row0 + token, in = at * a.ldq + (int64_t)qh * kDim;
+            out_at = at * a.ldo + (int64_t)qh * kDim, lse_at = at * a.heads + qh;
+            if (u.n <= 0) return;
+#pragma unroll 1
+            for (int i0 = 0; i0 < 16; i0 += 4) {
+                uint4 w[4];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = ld128_rw_stream(q + 8 * i);
-            float amax = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float x[8];
-                unpack<__nv_bfloat16>(w[i], x);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
-            }
-            // the row's largest element to [2^14, 2^15)
-            const int e = amax > 0.f ? min(100, 14 - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
-            const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-            rowf = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float x[8];
-                unpack<__nv_bfloat16>(w[i], x);
-                uint32_t h[4];
-#pragma unroll
-                for (int z = 0; z < 4; ++z) {
-                    const __half2 p = __floats2half2_rn(x[2 * z] * up, x[2 * z + 1] * up);
-                    h[z] = *reinterpret_cast<const uint32_t*>(&p);
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t from = __shfl_sync(0xFFFFFFFFu, in, 2 * (i0 + i) + (lane >> 4));
+                    w[i] = ld128_rw_stream(static_cast<const __nv_bfloat16*>(a.q) + from + (lane & 15) * 8);
                 }
-                *reinterpret_cast<uint4*>(q_tile + (i >> 3) * (kOperandBytes / 2) + row * 128 + (((i & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x[8], amax = 0.f;
+                    unpack<__nv_bfloat16>(w[i], x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
+#pragma unroll
+                    for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
+                    // the row's largest element to [2^14, 2^15)
+                    const int e = amax > 0.f ? min(100, 14 - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
+                    const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+                    const float down = __shfl_sync(0xFFFFFFFFu, a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23), (lane & 1) * 16);
+                    if (lane >> 1 == i0 + i) rowf = down;
+                    uint32_t h[4];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        const __half2 p = __floats2half2_rn(x[2 * z] * up, x[2 * z + 1] * up);
+                        h[z] = *reinterpret_cast<const uint32_t*>(&p);
+                    }
+                    const int line = (warp & 3) * 32 + 2 * (i0 + i) + (lane >> 4), chunk = lane & 15;
+                    *reinterpret_cast<uint4*>(q_tile + (chunk >> 3) * (kOperandBytes / 2) + line * 128 + (((chunk ^ line) & 7) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                }
             }
             fence_proxy_async_smem();
-            mbar_arrive(bar(&ctrl.q_full[t]));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(&ctrl.q_full[t]));
         };
-        bool more = walk.next(u);
-        auto takes_part = [&]() { return u.u0 < u.u1 && t * kTileRows < u.n_rows; };
-        if (more && takes_part()) load_q();
-        while (more) {
-            const TileUnit c = u;                     // the unit in hand; u becomes the next one before it is finished
-            const int n = max(c.u1 - c.u0, 0);
-            const bool part = t * kTileRows < c.n_rows;
-            const int row_at = c.tile_row + t * kTileRows + row;
-            const bool real = t * kTileRows + row < c.n_rows;
-            const int my_token = part && n > 0 ? token : min(row_at, c.tile_row + c.n_rows - 1) / group;
-            const int my_head = part && n > 0 ? qh : c.head * group + (min(row_at, c.tile_row + c.n_rows - 1) - my_token * group);
-            const int hi_row = upper_key(a, c.sq, my_token), lo_row = lower_key(a, c.sq, my_token);
+        UnitInfo u = unit(0);
+        if (u.n >= 0 && takes_part(u)) begin_unit(u);
+        for (int k = 1; u.n >= 0; ++k) {
+            const int n = u.n, slot_at = u.slot, mine = t * kTileRows + row;
+            const bool part = takes_part(u);
             float m = kNone, l = 0.f;
             if (part) {
+#pragma unroll 1
                 for (int i = 0; i < n; ++i, ++own) {
-                    const int key0 = c.lo + (c.u0 + i) * kKeys, kt = tiles + i;
+                    const int kt = tiles + i;
                     wait_bar(bar(&ctrl.s_full[t]), (uint32_t)own & 1u, abort_flag, a.dev_status);
                     // for the scales and what is known of V (its place is not filled again before this thread has handed over its weights, so that this
                     // phase cannot be missed)
                     wait_bar(bar(&ctrl.v_full[kt & 1]), (uint32_t)(kt >> 1) & 1u, abort_flag, a.dev_status);
-                    const float4* scales = s_scales[kt % kScaleRing];
-                    bool border = key0 + kKeys > c.hi_min || key0 < c.lo_max;
-                    uint32_t nan[4] = {0, 0, 0, 0};
-#pragma unroll
-                    for (int g = 0; g < 8; ++g) border |= scales[g].w == 0.f;
-                    if (border) {
-#pragma unroll
-                        for (int z = 0; z < 4; ++z) nan[z] = s_nan[kt % kScaleRing][z];
-                    }
                     __syncwarp();
                     tc_fence_after();
-                    // 32 scores, with what hides them; y: the raw score
-                    auto scores = [&](int c32, float* y) {
-                        uint32_t v[32];
-                        tmem_ld_x16(s_at + c32 * 32, v);
-                        tmem_ld_x16(s_at + c32 * 32 + 16, v + 16);
-                        tmem_wait_ld();
+                    const KeyTile& tile = s_tiles[kt % kTileQueue];
+                    const bool border = tile.kind != 0;
+                    const int first = lo_row - tile.key0, behind = hi_row - tile.key0;      // the row sees keys [first, behind) of the tile
+                    uint32_t v[2][32];                // scores, the next 32 on their way
+                    // what hides scores 32 c .. 32 c + 31
+                    auto hide = [&](int c, uint32_t* w) {
+                        // bits of the keys that the row sees, and of those that are a NaN for it
+                        const int lo = min(max(first - 32 * c, 0), 32), hi = min(max(behind - 32 * c, 0), 32);
+                        uint32_t sees = (hi == 32 ? 0xFFFFFFFFu : (1u << hi) - 1u) & ~(lo == 32 ? 0xFFFFFFFFu : (1u << lo) - 1u);
+                        if (tile.scale[2 * c].w == 0.f) sees &= 0xFFFF0000u;
+                        if (tile.scale[2 * c + 1].w == 0.f) sees &= 0xFFFFu;
+                        const uint32_t nan = tile.nan[c];
 #pragma unroll
-                        for (int z = 0; z < 32; ++z) y[z] = __uint_as_float(v[z]);
-                        if (border) {
-#pragma unroll
-                            for (int z = 0; z < 32; ++z) {
-                                const int key = key0 + c32 * 32 + z;
-                                const bool sees = key < hi_row && key >= lo_row && scales[2 * c32 + (z >> 4)].w != 0.f;
-                                y[z] = !sees ? -INFINITY : (nan[c32] >> z) & 1u ? __int_as_float(0x7FC00000) : y[z];
-                            }
-                        }
+                        for (int z = 0; z < 32; ++z) w[z] = !((sees >> z) & 1u) ? 0xFF800000u : (nan >> z) & 1u ? 0x7FC00000u : w[z];
                     };
+                    // ---- the largest exponent
                     float top = -INFINITY;
-#pragma unroll 1
-                    for (int c32 = 0; c32 < 4; ++c32) {
-                        float y[32];
-                        scores(c32, y);
+                    tmem_ld_x32(s_at, v[0]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t* w = v[c & 1];
+                        tmem_wait_ld();
+                        if (c < 3) tmem_ld_x32(s_at + (c + 1) * 32, v[(c + 1) & 1]);
+                        if (border) hide(c, w);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            float raw = y[16 * h];
+                            const float4 sc = tile.scale[2 * c + h];
+                            float tops[4];
 #pragma unroll
-                            for (int z = 1; z < 16; ++z) raw = fmaxf(raw, y[16 * h + z]);
-                            const float4 sc = scales[2 * c32 + h];
+                            for (int z = 0; z < 4; ++z)
+                                tops[z] = fmaxf(fmaxf(__uint_as_float(w[16 * h + z]), __uint_as_float(w[16 * h + z + 4])),
+                                                fmaxf(__uint_as_float(w[16 * h + z + 8]), __uint_as_float(w[16 * h + z + 12])));
+                            const float raw = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                             top = fmaxf(top, fmaf(raw, fmaxf(rowf * sc.x, 1.17549435e-38f), sc.y));      // (never 0: a hidden score is -infinity times it)
                         }
                     }
@@ -321,35 +350,42 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (i > 0) {                  // (S of this tile was asked for behind O of the last, which is therefore done)
 #pragma unroll 1
                             for (int c16 = 0; c16 < 8; ++c16) {
-                                uint32_t v[16];
-                                tmem_ld_x16(o_at + c16 * 16, v);
+                                uint32_t o[16];
+                                tmem_ld_x16(o_at + c16 * 16, o);
                                 tmem_wait_ld();
 #pragma unroll
-                                for (int z = 0; z < 16; ++z) v[z] = __float_as_uint(__uint_as_float(v[z]) * shrink);
-                                tmem_st<16>(o_at + c16 * 16, v);
+                                for (int z = 0; z < 16; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * shrink);
+                                tmem_st<16>(o_at + c16 * 16, o);
                             }
                         }
                     }
-#pragma unroll 1
-                    for (int c32 = 0; c32 < 4; ++c32) {
-                        float y[32];
-                        scores(c32, y);
+                    // ---- the weights, two to a column, over scores that have been read
+                    tmem_ld_x32(s_at, v[0]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t* w = v[c & 1];
+                        tmem_wait_ld();
+                        if (c < 3) tmem_ld_x32(s_at + (c + 1) * 32, v[(c + 1) & 1]);
+                        if (border) hide(c, w);
                         uint32_t p[16];
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const float4 sc = scales[2 * c32 + h];
+                            const float4 sc = tile.scale[2 * c + h];
                             const float f = fmaxf(rowf * sc.x, 1.17549435e-38f), off = sc.y - m;
-                            float sum = 0.f;
+                            float e[16];
 #pragma unroll
-                            for (int z = 0; z < 16; z += 2) {
-                                const float w0 = ex2(fmaf(y[16 * h + z], f, off)), w1 = ex2(fmaf(y[16 * h + z + 1], f, off));
-                                sum += w0 + w1;
-                                const __half2 w = __floats2half2_rn(w0, w1);
-                                p[8 * h + z / 2] = *reinterpret_cast<const uint32_t*>(&w);
+                            for (int z = 0; z < 16; ++z) e[z] = ex2(fmaf(__uint_as_float(w[16 * h + z]), f, off));
+                            float sums[4];
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) sums[z] = (e[z] + e[z + 4]) + (e[z + 8] + e[z + 12]);
+                            l = fmaf((sums[0] + sums[1]) + (sums[2] + sums[3]), sc.z, l);
+#pragma unroll
+                            for (int z = 0; z < 8; ++z) {
+                                const __half2 w2 = __floats2half2_rn(e[2 * z], e[2 * z + 1]);
+                                p[8 * h + z] = *reinterpret_cast<const uint32_t*>(&w2);
                             }
-                            l = fmaf(sum, sc.z, l);
                         }
-                        tmem_st<16>(s_at + c32 * 16, p);
+                        tmem_st<16>(s_at + c * 16, p);
                     }
                     tmem_wait_st();
                     tc_fence_before();
@@ -357,28 +393,28 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             tiles += n;
+            const int64_t out_was = out_at, lse_was = lse_at;
+            const bool real_was = real;
             // ---- the next unit's q while the last O is on its way
-            more = walk.next(u);
-            if (more && takes_part()) load_q();
+            u = unit(k);
+            if (u.n >= 0 && takes_part(u)) begin_unit(u);
             if (!part) continue;
-            const bool begins = c.first == 0, whole = begins && c.last == c.steps;
-            float* slot = slots + (2 * (int64_t)blockIdx.x + (begins ? 1 : 0)) * (int64_t)slot_floats(kUnitRows, kDim);
-            const int r = t * kTileRows + row;
             if (n > 0) {
-                wait_bar(bar(&ctrl.o_full[t]), (uint32_t)units & 1u, abort_flag, a.dev_status);
-                ++units;
+                wait_bar(bar(&ctrl.o_full[t]), (uint32_t)finished & 1u, abort_flag, a.dev_status);
+                ++finished;
                 __syncwarp();
                 tc_fence_after();
             }
-            const bool store = real && *abort_flag == 0;       // (nothing of an aborted call is stored)
+            const bool whole = slot_at < 0, store = real_was && *abort_flag == 0;       // (nothing of an aborted call is stored)
             const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
-            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + ((int64_t)c.sq.row0 + my_token) * a.ldo + (int64_t)my_head * kDim;
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + out_was;
+            float* slot = slots + max(slot_at, 0) * (int64_t)slot_floats(kUnitRows, kDim);
 #pragma unroll 1
-            for (int c32 = 0; c32 < 4; ++c32) {
+            for (int c = 0; c < 4; ++c) {
                 uint32_t v[32];
                 if (n > 0) {
-                    tmem_ld_x16(o_at + c32 * 32, v);
-                    tmem_ld_x16(o_at + c32 * 32 + 16, v + 16);
+                    tmem_ld_x16(o_at + c * 32, v);
+                    tmem_ld_x16(o_at + c * 32 + 16, v + 16);
                     tmem_wait_ld();
                 } else {
 #pragma unroll
@@ -390,101 +426,75 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!store) continue;
                 if (whole) {
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) stg128(out + c32 * 32 + z * 8, pack<__nv_bfloat16>(x + 8 * z));
+                    for (int z = 0; z < 4; ++z) stg128(out + c * 32 + z * 8, pack<__nv_bfloat16>(x + 8 * z));
                 } else {
 #pragma unroll
-                    for (int z = 0; z < 8; ++z) stg128(slot + 2 * kUnitRows + r * kDim + c32 * 32 + z * 4, pack<float>(x + 4 * z));
+                    for (int z = 0; z < 8; ++z) stg128(slot + 2 * kUnitRows + mine * kDim + c * 32 + z * 4, pack<float>(x + 4 * z));
                 }
             }
             tc_fence_before();                        // (the next O begins behind this thread's next weights)
             if (store) {
-                if (!whole) slot[r] = m, slot[kUnitRows + r] = l;
-                else if (a.lse != nullptr) a.lse[((int64_t)c.sq.row0 + my_token) * a.heads + my_head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718056f;
+                if (!whole) slot[mine] = m, slot[kUnitRows + mine] = l;
+                else if (a.lse != nullptr) a.lse[lse_was] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718056f;
             }
         }
     } else if (warp < kMmaWarp) {
         // ============================================================ codes -> fp16
-        const int ct = tid - kConvWarp0 * 32, chunk = ct & 7, r0 = ct >> 3;      // chunk of 16 elements, lines r0 + 16 i
-        const int plog = a.c.page_log2;
-        CutUnit cut{0, 0, 0, 0};
-        int tiles = 0;
-        auto sync = [] { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); };
-        while (walk.next(u)) {
-            if (u.first == 0 && u.last < u.steps) cut.b = u.b, cut.row_tile = u.tile, cut.head = u.head, cut.pieces = walk.pieces(u, blockIdx.x);
-            const int32_t* table = a.c.table + (int64_t)u.b * a.c.ld_table;
-            // page and scales of the ct-th 16 keys of tile i, ct < 8: asked for one tile ahead
-            int32_t id = -1;
-            float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);
-            auto look_up = [&](int i) {
-                if (ct >= 8) return;
-                id = -1;
-                sc = make_float4(0.f, 0.f, 0.f, 0.f);
-                const int key = u.lo + i * kKeys + ct * 16;
-                if (i < u.u1 && ((key >> plog) << plog) < u.hi_max) {
-                    id = ld_dependent(table + (key >> plog));
-                    if (id < 0 || id >= a.c.n_pages) {
-                        id = -1;
-                        if (a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
-                    } else {
-                        const int64_t block = (int64_t)id * a.c.kv_heads + u.head;
-                        const float vs = clamped_scale(ld_dependent(a.c.v_scale + block));
-                        sc = make_float4(ld_dependent(a.c.k_scale + block), log2f(vs), 1.f / vs, 1.f);
-                    }
-                }
-            };
-            look_up(u.u0);
-            for (int i = u.u0; i < u.u1; ++i, ++tiles) {
-                const int slot = tiles % kScaleRing, st = tiles & 1;
-                const uint32_t again = ((uint32_t)(tiles >> 1) & 1u) ^ 1u;
-                const int key0 = u.lo + i * kKeys;
-                // (the slot's last tile was four tiles ago: its weights went into an O before the place of V two tiles ago was given back)
-                if (ct < 8) s_scales[slot][ct] = sc, s_pages[slot][ct] = id;
-                if (ct < 4) s_nan[slot][ct] = 0;
-                sync();
-                uint4 k[8], v[8];
-                auto load = [&](const uint8_t* codes, uint4* w) {
+        const int ct = tid - kConvWarp0 * 32, chunk = ct & 7, r0 = ct >> 3;      // chunk of 16 elements, lines r0 + 16 j
+        const int64_t lane_at = (int64_t)r0 * kDim + chunk * 16;
+        uint4 k[8], v[8];
+        auto load = [&](const KeyTile& tile, const uint8_t* codes, uint4* w) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int32_t page = s_pages[slot][j];
-                        const int64_t line = (((int64_t)page * a.c.kv_heads + u.head) << plog) + ((key0 + 16 * j + r0) & ((1 << plog) - 1));
-                        w[j] = page >= 0 ? ld128_rw_stream(codes + line * kDim + chunk * 16) : make_uint4(0, 0, 0, 0);
-                    }
-                };
-                load(a.c.k, k);
-                load(a.c.v, v);
-                look_up(i + 1);
-                if (tiles >= 2) wait_bar(bar(&ctrl.k_empty[st]), again, abort_flag, a.dev_status);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) store_codes_f16(smem + kKAt + st * kOperandBytes, 16 * j + r0, chunk, k[j]);
-                fence_proxy_async_smem();
-                mbar_arrive(bar(&ctrl.k_full[st]));
-                if (key0 + kKeys > u.hi_min || key0 < u.lo_max) {
-                    // Some row does not see some key: values that no row sees count as zero; a NaN among the codes of one becomes a NaN in the scores of
-                    // the rows that see it and a zero here, so that it cannot reach the others through their weight of zero.
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int key = key0 + 16 * j + r0;
-                        const bool none = key >= u.hi_max || key < u.lo_min;
-                        uint32_t* w[4] = {&v[j].x, &v[j].y, &v[j].z, &v[j].w};
-                        bool nan = false;
-#pragma unroll
-                        for (int z = 0; z < 4; ++z) {
-                            const uint32_t bits = e4m3x4_nan_bits(*w[z]);
-                            nan |= bits != 0;
-                            *w[z] = none ? 0u : *w[z] & ~((bits >> 7) * 0xFFu);
-                        }
-                        if (nan && !none) atomicOr(&s_nan[slot][(16 * j + r0) >> 5], 1u << ((16 * j + r0) & 31));
-                    }
-                }
-                if (tiles >= 2) wait_bar(bar(&ctrl.v_empty[st]), again, abort_flag, a.dev_status);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) store_codes_f16(smem + kVAt + st * kOperandBytes, 16 * j + r0, chunk, v[j]);
-                fence_proxy_async_smem();
-                mbar_arrive(bar(&ctrl.v_full[st]));
+            for (int j = 0; j < 8; ++j) {
+                const int64_t line = tile.line[j];
+                w[j] = line >= 0 ? ld128_rw_stream(codes + line * kDim + lane_at) : make_uint4(0, 0, 0, 0);
             }
+        };
+        // (after an abort the queue is not looked at any more)
+        auto there = [&](int kt) {
+            const bool ok = wait_bar(bar(&ctrl.tile_full[kt % kTileQueue]), (uint32_t)(kt / kTileQueue) & 1u, abort_flag, a.dev_status);
+            return ok && *const_cast<volatile int32_t*>(&s_tiles[kt % kTileQueue].kind) != 2;
+        };
+        bool more = there(0);
+        if (more) load(s_tiles[0], a.c.k, k), load(s_tiles[0], a.c.v, v);
+        for (int kt = 0; more; ++kt) {
+            KeyTile& tile = s_tiles[kt % kTileQueue];
+            const KeyTile& next = s_tiles[(kt + 1) % kTileQueue];
+            const int st = kt & 1;
+            const uint32_t again = ((uint32_t)(kt >> 1) & 1u) ^ 1u;
+            if (kt >= 2) wait_bar(bar(&ctrl.k_empty[st]), again, abort_flag, a.dev_status);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) store_codes_f16(smem + kKAt + st * kOperandBytes, 16 * j + r0, chunk, k[j]);
+            fence_proxy_async_smem();
+            mbar_arrive(bar(&ctrl.k_full[st]));
+            more = there(kt + 1);
+            if (more) load(next, a.c.k, k);
+            if (tile.kind == 1) {
+                // Some row does not see some key: values that no row sees count as zero; a NaN among the codes of one becomes a NaN in the scores of
+                // the rows that see it and a zero here, so that it cannot reach the others through their weight of zero.
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int at = 16 * j + r0, key = tile.key0 + at;
+                    const bool none = key >= tile.hi_max || key < tile.lo_min;
+                    uint32_t* w[4] = {&v[j].x, &v[j].y, &v[j].z, &v[j].w};
+                    bool nan = false;
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        const uint32_t bits = e4m3x4_nan_bits(*w[z]);
+                        nan |= bits != 0;
+                        *w[z] = none ? 0u : *w[z] & ~((bits >> 7) * 0xFFu);
+                    }
+                    if (nan && !none) atomicOr(&tile.nan[at >> 5], 1u << (at & 31));
+                }
+            }
+            if (kt >= 2) wait_bar(bar(&ctrl.v_empty[st]), again, abort_flag, a.dev_status);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) store_codes_f16(smem + kVAt + st * kOperandBytes, 16 * j + r0, chunk, v[j]);
+            fence_proxy_async_smem();
+            mbar_arrive(bar(&ctrl.v_full[st]));
+            if (more) load(next, a.c.v, v);
         }
-        if (ct == 0) cuts[blockIdx.x] = *abort_flag == 0 ? cut : CutUnit{0, 0, 0, 0};
-    } else {
+    } else if (warp == kMmaWarp) {
         // ============================================================ MMAs
         const bool leader = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
@@ -493,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t q_desc = smem_desc(base + kQAt, 16, 1024, kL128), k_desc = smem_desc(base + kKAt, 16, 1024, kL128);
         const uint64_t v_desc = smem_desc(base + kVAt, kOperandBytes / 2, 1024, kL128);      // 64 elements a group, 8 keys a group
         bool live = true;
-        int units[2] = {0, 0}, ps[2] = {0, 0};        // of each tile of rows: units with keys, weights waited for
+        int units0 = 0, units1 = 0, weights0 = 0, weights1 = 0;      // of each tile of rows: units with keys, weights waited for
         int tiles = 0;
         auto issue_s = [&](int t, int kt, bool last) {
             if (leader && live) {
@@ -501,7 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {         // 16 elements a step, 64 a part
                     const uint64_t off = (uint64_t)((j >> 2) * (kOperandBytes / 2 >> 4) + (j & 3) * 2);
-                    umma_f16(tm + (uint32_t)(t * 128), q_desc + qa + off, k_desc + ka + off, idesc_s, j > 0);
+                    umma_bf16(tm + (uint32_t)(t * 128), q_desc + qa + off, k_desc + ka + off, idesc_s, j > 0);
                 }
                 umma_commit(bar(&ctrl.s_full[t]));
                 if (last) umma_commit(bar(&ctrl.k_empty[kt & 1]));
@@ -509,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
         };
         auto issue_o = [&](int t, int kt, bool begins, bool ends, bool last) {
-            live = wait_bar(bar(&ctrl.p_full[t]), (uint32_t)(t == 0 ? ps[0]++ : ps[1]++) & 1u, abort_flag, a.dev_status) && live;
+            live = wait_bar(bar(&ctrl.p_full[t]), (uint32_t)(t == 0 ? weights0++ : weights1++) & 1u, abort_flag, a.dev_status) && live;
             live = wait_bar(bar(&ctrl.v_full[kt & 1]), (uint32_t)(kt >> 1) & 1u, abort_flag, a.dev_status) && live;
             tc_fence_after();
             if (leader && live) {
@@ -517,7 +527,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)           // 16 keys a step: two groups of 8 lines
                     umma_bf16_ts(tm + kOCol + (uint32_t)(t * 128), tm + (uint32_t)(t * 128 + j * 8), v_desc + va + j * (2048 >> 4), idesc_o, !begins || j > 0);
-                if (last) umma_commit(bar(&ctrl.v_empty[kt & 1]));
+                if (last) {
+                    umma_commit(bar(&ctrl.v_empty[kt & 1]));
+                    umma_commit(bar(&ctrl.tile_empty[kt % kTileQueue]));
+                }
                 if (ends) umma_commit(bar(&ctrl.o_full[t]));
             }
             __syncwarp();
@@ -526,12 +539,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             live = wait_bar(bar(&ctrl.k_full[kt & 1]), (uint32_t)(kt >> 1) & 1u, abort_flag, a.dev_status) && live;
             tc_fence_after();
         };
-        while (live && walk.next(u)) {
-            const int n = u.u1 - u.u0;
-            if (n <= 0) continue;
+        for (int z = 0; live; ++z) {
+            const UnitInfo u = unit(z);
+            const int n = u.n;
+            if (n < 0) break;
+            if (n == 0) continue;
             const bool two = u.n_rows > kTileRows;
-            for (int t = 0; t < 1 + two; ++t) {
-                live = wait_bar(bar(&ctrl.q_full[t]), (uint32_t)(t == 0 ? units[0]++ : units[1]++) & 1u, abort_flag, a.dev_status) && live;
+            for (int t = 0; t < 1 + (int)two; ++t) {
+                live = wait_bar(bar(&ctrl.q_full[t]), (uint32_t)(t == 0 ? units0++ : units1++) & 1u, abort_flag, a.dev_status) && live;
                 if (t == 0) wait_k(tiles);
                 tc_fence_after();
                 issue_s(t, tiles, t == (int)two);
@@ -553,6 +568,86 @@ __global__ void __launch_bounds__(kThreads, 1)
         while (!mbar_try_wait(bar(&ctrl.drained), 0))
             if (clock64() - c0 > kTimeoutCycles) break;
         __syncwarp();
+    } else {
+        // ============================================================ units, pages, scales
+        const int plog = a.c.page_log2;
+        TileWalk walk(a);
+        walk.begin(s_upto, blockIdx.x);
+        CutUnit cut{0, 0, 0, 0};
+        int tiles = 0, units = 0;
+        auto push_unit = [&](const UnitInfo& info) {
+            const int slot = units % kUnitQueue;
+            if (units >= kUnitQueue) wait_bar(bar(&ctrl.unit_empty[slot]), ((uint32_t)(units / kUnitQueue) & 1u) ^ 1u, abort_flag, a.dev_status);
+            if (lane == 0) {
+                s_units[slot] = info;
+                mbar_arrive(bar(&ctrl.unit_full[slot]));
+            }
+            __syncwarp();
+            ++units;
+        };
+        auto claim_tile = [&]() -> KeyTile& {
+            const int slot = tiles % kTileQueue;
+            if (tiles >= kTileQueue) wait_bar(bar(&ctrl.tile_empty[slot]), ((uint32_t)(tiles / kTileQueue) & 1u) ^ 1u, abort_flag, a.dev_status);
+            __syncwarp();
+            return s_tiles[slot];
+        };
+        auto hand_over = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(&ctrl.tile_full[tiles % kTileQueue]));
+            ++tiles;
+        };
+        TileUnit u{};
+        while (*abort_flag == 0 && walk.next(u)) {
+            const bool begins = u.first == 0, whole = begins && u.last == u.steps;
+            if (begins && !whole) cut.b = u.b, cut.row_tile = u.tile, cut.head = u.head, cut.pieces = walk.pieces(u, blockIdx.x);
+            UnitInfo info;
+            info.row0 = u.sq.row0, info.first_pos = u.sq.first_pos(), info.len = u.sq.len;
+            info.tile_row = u.tile_row, info.n_rows = u.n_rows, info.head = u.head;
+            info.key0 = u.lo + u.u0 * kKeys, info.n = max(u.u1 - u.u0, 0);
+            info.slot = whole ? -1 : 2 * (int)blockIdx.x + (begins ? 1 : 0);
+            push_unit(info);
+            // lanes hold 32 sixteens of keys: four tiles
+            int32_t id = -1;
+            float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);
+            int64_t line = -1;
+            for (int i = u.u0; i < u.u1; ++i) {
+                const int key0 = u.lo + i * kKeys, from = (i - u.u0) & 3;
+                if (from == 0) {
+                    const int key = key0 + lane * 16;
+                    id = -1, line = -1;
+                    sc = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (((key >> plog) << plog) < u.hi_max) {
+                        id = ld_dependent(a.c.table + (int64_t)u.b * a.c.ld_table + (key >> plog));
+                        if (id < 0 || id >= a.c.n_pages) {
+                            if (a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
+                        } else {
+                            const int64_t block = (int64_t)id * a.c.kv_heads + u.head;
+                            const float vs = clamped_scale(ld_dependent(a.c.v_scale + block));
+                            sc = make_float4(ld_dependent(a.c.k_scale + block), log2f(vs), 1.f / vs, 1.f);
+                            line = (block << plog) + (key & ((1 << plog) - 1));
+                        }
+                    }
+                    __syncwarp();
+                }
+                const bool missing = __any_sync(0xFFFFFFFFu, lane >> 3 == from && line < 0);
+                KeyTile& tile = claim_tile();
+                if (*abort_flag) break;
+                if (lane >> 3 == from) tile.scale[lane & 7] = sc, tile.line[lane & 7] = line;
+                if (lane < 4) tile.nan[lane] = 0;
+                if (lane == 0) {
+                    tile.key0 = key0, tile.hi_max = u.hi_max, tile.lo_min = u.lo_min;
+                    tile.kind = missing || key0 + kKeys > u.hi_min || key0 < u.lo_max ? 1 : 0;
+                }
+                hand_over();
+            }
+        }
+        UnitInfo end{};
+        end.n = -1;
+        push_unit(end);
+        KeyTile& tile = claim_tile();
+        if (lane == 0) tile.kind = 2;
+        hand_over();
+        if (lane == 0) cuts[blockIdx.x] = *abort_flag == 0 ? cut : CutUnit{0, 0, 0, 0};
     }
     tc_fence_before();
     __syncthreads();
