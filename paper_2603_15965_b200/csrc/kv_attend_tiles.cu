@@ -4,12 +4,13 @@
 // value head and the keys that they see; here the tensor cores are the bound, so the codes of K and V are brought to fp16 once for both tiles.
 //   S_t = Q_t K^T  [128 rows x 128 keys]       A = Q_t in shared memory, B = K in shared memory
 //   O_t += P_t V   [128 rows x 128 elements]   A = P_t in TMEM (fp16, in the place of S_t), B = V in shared memory, read across (MN-major)
-//   warps 0-3, 4-7  a row per thread of tile 0 and 1: q to fp16 by a power of two, weights of a tile (S_t -> P_t), the sum, the result.  Nothing
-//                   is shared between rows, so nothing is synchronised; the reference of a row moves when a score is 2^8 over the weight that its
-//                   largest was given, and then O_t is rescaled (by warps: TMEM is read and written by whole warps)
-//   warps 8-11      codes -> fp16, two tiles of 128 keys of K and of V ahead, the codes of the next tile on their way in registers
-//   warp 12         the MMAs: O_0 S_0 O_1 S_1 ... -- while the weights of one tile are worked out, the other has the tensor cores
-//   warp 13         units, pages and scales, into queues: what depends on one another there is waited for long before it is needed
+//   warps 0-7, 8-15 two threads per row of tile 0 and 1, each with half of the keys: q to fp16 by a power of two, weights of a tile (S_t -> P_t),
+//                   the sum, the result.  The reference of a row moves when a score is 2^8 over the weight that its largest was given, and then
+//                   O_t is rescaled; whether it does is all that the two ask each other, tile by tile.  (One thread per row, 128 keys one after the other at the
+//                   latencies of one warp per scheduler, took 3500 cycles a tile.)
+//   warps 16-19     codes -> fp16, two tiles of 128 keys of K and of V ahead, the codes of the next tile on their way in registers
+//   warp 20         the MMAs: O_0 S_0 O_1 S_1 ... -- while the weights of one tile are worked out, the other has the tensor cores
+//   warp 21         units, pages and scales, into queues: what depends on one another there is waited for long before it is needed
 // S_t of the next keys is asked for right behind O_t of the last, which is the last to read P_t: the tensor cores work in the order of issue.
 // TMEM: S_0 S_1 O_0 O_1, 128 columns each.  Shared memory: Q 64 KB, K and V 2 x 32 KB each.
 // Shares, pieces and the join as in kv_attend.cuh, but with the steps that each tile of rows really sees.
@@ -21,8 +22,11 @@ namespace molora {
 namespace {
 
 constexpr int kDim = 128, kKeys = 128, kTileRows = 128, kUnitRows = 256;
-constexpr int kThreads = 448;
-constexpr int kConvWarp0 = 8, kMmaWarp = 12;
+constexpr int kThreads = 768;                                 // (the last two warps only make a warpgroup of four)
+constexpr int kConvWarp0 = 16, kMmaWarp = 20, kWalkWarp = 21;
+// Registers: the converting warps hold 64 words of codes, which the last four give up (6 x 128 threads, 80 registers each at launch)
+constexpr int kConvRegs = 104, kOtherRegs = 56;
+static_assert(kConvRegs + kOtherRegs <= 2 * 80, "register split");
 constexpr int kOperandBytes = 128 * kDim * 2;                 // of a Q tile, of a tile of K or of V, in fp16
 constexpr int kQAt = 0, kKAt = 2 * kOperandBytes, kVAt = 4 * kOperandBytes;
 constexpr size_t kSmem = 1024 + 6 * (size_t)kOperandBytes;
@@ -171,6 +175,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     __shared__ int64_t s_upto[kThreads];
     __shared__ KeyTile s_tiles[kTileQueue];
     __shared__ UnitInfo s_units[kUnitQueue];
+    __shared__ float s_pair[2][2][kTileRows];         // what the two threads of a row tell each other
     extern __shared__ uint8_t smem_raw[];
     const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -182,8 +187,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     grid_dependency_wait();
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(&ctrl.q_full[i]), 4), mbar_init(bar(&ctrl.s_full[i]), 1);
-            mbar_init(bar(&ctrl.p_full[i]), kTileRows), mbar_init(bar(&ctrl.o_full[i]), 1);
+            mbar_init(bar(&ctrl.q_full[i]), 8), mbar_init(bar(&ctrl.s_full[i]), 1);
+            mbar_init(bar(&ctrl.p_full[i]), 2 * kTileRows), mbar_init(bar(&ctrl.o_full[i]), 1);
             mbar_init(bar(&ctrl.k_full[i]), 128), mbar_init(bar(&ctrl.k_empty[i]), 1);
             mbar_init(bar(&ctrl.v_full[i]), 128), mbar_init(bar(&ctrl.v_empty[i]), 1);
         }
@@ -233,11 +238,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
 
     if (warp < kConvWarp0) {
-        // ============================================================ a row per thread
-        const int t = warp >> 2, row = (warp & 3) * 32 + lane;       // tile, and row of the tile = lane of TMEM
+        // ============================================================ half a row per thread
+        const int t = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane;       // tile, half of the keys, row of the tile = lane of TMEM
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_at = tmem + lane_addr + (uint32_t)(t * 128), o_at = tmem + lane_addr + kOCol + (uint32_t)(t * 128);
+        const uint32_t s_at = tmem + lane_addr + (uint32_t)(t * 128 + half * 64), o_at = tmem + lane_addr + kOCol + (uint32_t)(t * 128 + half * 64);
         uint8_t* const q_tile = smem + kQAt + t * kOperandBytes;
+        const int pair = 1 + t * 4 + (warp & 3);      // barrier of the two warps that share 32 rows
+        auto pair_sync = [&]() { asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair) : "memory"); };
+        auto pair_any = [&](bool v) {
+            uint32_t r;
+            asm volatile(
+                "{\n\t.reg .pred P, Q;\n\tsetp.ne.b32 P, %1, 0;\n\tbarrier.cta.red.or.pred Q, %2, 64, P;\n\tselp.u32 %0, 1, 0, Q;\n\t}"
+                : "=r"(r)
+                : "r"((uint32_t)v), "r"(pair)
+                : "memory");
+            return r != 0;
+        };
         int tiles = 0, own = 0, finished = 0;         // key tiles of the share so far; of them, those that this tile of rows took part in; its Os
         float rowf = 0.f;
         int64_t out_at = 0, lse_at = 0;
@@ -255,42 +271,47 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int64_t at = (int64_t)u.row0 + token, in = at * a.ldq + (int64_t)qh * kDim;
             out_at = at * a.ldo + (int64_t)qh * kDim, lse_at = at * a.heads + qh;
             if (u.n <= 0) return;
-#pragma unroll 1
-            for (int i0 = 0; i0 < 16; i0 += 4) {
-                uint4 w[4];
+            uint4 w[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t from = __shfl_sync(0xFFFFFFFFu, in, 2 * (i0 + i) + (lane >> 4));
-                    w[i] = ld128_rw_stream(static_cast<const __nv_bfloat16*>(a.q) + from + (lane & 15) * 8);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x[8], amax = 0.f;
-                    unpack<__nv_bfloat16>(w[i], x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
-#pragma unroll
-                    for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
-                    // the row's largest element to [2^14, 2^15)
-                    const int e = amax > 0.f ? min(100, 14 - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
-                    const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-                    const float down = __shfl_sync(0xFFFFFFFFu, a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23), (lane & 1) * 16);
-                    if (lane >> 1 == i0 + i) rowf = down;
-                    uint32_t h[4];
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) {
-                        const __half2 p = __floats2half2_rn(x[2 * z] * up, x[2 * z + 1] * up);
-                        h[z] = *reinterpret_cast<const uint32_t*>(&p);
-                    }
-                    const int line = (warp & 3) * 32 + 2 * (i0 + i) + (lane >> 4), chunk = lane & 15;
-                    *reinterpret_cast<uint4*>(q_tile + (chunk >> 3) * (kOperandBytes / 2) + line * 128 + (((chunk ^ line) & 7) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const int64_t from = __shfl_sync(0xFFFFFFFFu, in, half * 16 + 2 * i + (lane >> 4));
+                w[i] = ld128_rw_stream(static_cast<const __nv_bfloat16*>(a.q) + from + (lane & 15) * 8);
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float x[8], amax = 0.f;
+                unpack<__nv_bfloat16>(w[i], x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
+                // the row's largest element to [2^14, 2^15)
+                const int e = amax > 0.f ? min(100, 14 - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
+                const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+                uint32_t h[4];
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    const __half2 p = __floats2half2_rn(x[2 * z] * up, x[2 * z + 1] * up);
+                    h[z] = *reinterpret_cast<const uint32_t*>(&p);
+                }
+                const int line = (warp & 3) * 32 + half * 16 + 2 * i + (lane >> 4), chunk = lane & 15;
+                if (chunk == 0) s_pair[t][0][line] = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
+                *reinterpret_cast<uint4*>(q_tile + (chunk >> 3) * (kOperandBytes / 2) + line * 128 + (((chunk ^ line) & 7) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+            pair_sync();
+            rowf = s_pair[t][0][row];
+            pair_sync();                              // (s_pair is free again)
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(&ctrl.q_full[t]));
         };
-        UnitInfo u = unit(0);
+        // (after an abort the waits fall through: the two warps of a pair leave together, so that neither is left at a barrier)
+        auto next_unit = [&](int k) {
+            UnitInfo u = unit(k);
+            if (pair_any(u.n < 0)) u.n = -1;
+            return u;
+        };
+        UnitInfo u = next_unit(0);
         if (u.n >= 0 && takes_part(u)) begin_unit(u);
         for (int k = 1; u.n >= 0; ++k) {
             const int n = u.n, slot_at = u.slot, mine = t * kTileRows + row;
@@ -308,84 +329,77 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tc_fence_after();
                     const KeyTile& tile = s_tiles[kt % kTileQueue];
                     const bool border = tile.kind != 0;
-                    const int first = lo_row - tile.key0, behind = hi_row - tile.key0;      // the row sees keys [first, behind) of the tile
-                    uint32_t v[2][32];                // scores, the next 32 on their way
-                    // what hides scores 32 c .. 32 c + 31
-                    auto hide = [&](int c, uint32_t* w) {
+                    const int first = lo_row - tile.key0 - half * 64, behind = hi_row - tile.key0 - half * 64;      // the row sees [first, behind) of these 64
+                    const float4* scales = tile.scale + 4 * half;
+                    uint32_t v[2][16];                // scores, the next 16 on their way
+                    // what hides scores 16 g .. 16 g + 15
+                    auto hide = [&](int g, uint32_t* w) {
                         // bits of the keys that the row sees, and of those that are a NaN for it
-                        const int lo = min(max(first - 32 * c, 0), 32), hi = min(max(behind - 32 * c, 0), 32);
-                        uint32_t sees = (hi == 32 ? 0xFFFFFFFFu : (1u << hi) - 1u) & ~(lo == 32 ? 0xFFFFFFFFu : (1u << lo) - 1u);
-                        if (tile.scale[2 * c].w == 0.f) sees &= 0xFFFF0000u;
-                        if (tile.scale[2 * c + 1].w == 0.f) sees &= 0xFFFFu;
-                        const uint32_t nan = tile.nan[c];
+                        const int lo = min(max(first - 16 * g, 0), 16), hi = min(max(behind - 16 * g, 0), 16);
+                        const uint32_t sees = scales[g].w == 0.f ? 0u : ((1u << hi) - 1u) & ~((1u << lo) - 1u);
+                        const uint32_t nan = tile.nan[2 * half + (g >> 1)] >> (16 * (g & 1));
 #pragma unroll
-                        for (int z = 0; z < 32; ++z) w[z] = !((sees >> z) & 1u) ? 0xFF800000u : (nan >> z) & 1u ? 0x7FC00000u : w[z];
+                        for (int z = 0; z < 16; ++z) w[z] = !((sees >> z) & 1u) ? 0xFF800000u : (nan >> z) & 1u ? 0x7FC00000u : w[z];
                     };
                     // ---- the largest exponent
                     float top = -INFINITY;
-                    tmem_ld_x32(s_at, v[0]);
+                    tmem_ld_x16(s_at, v[0]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t* w = v[c & 1];
+                    for (int g = 0; g < 4; ++g) {
+                        uint32_t* w = v[g & 1];
                         tmem_wait_ld();
-                        if (c < 3) tmem_ld_x32(s_at + (c + 1) * 32, v[(c + 1) & 1]);
-                        if (border) hide(c, w);
+                        if (g < 3) tmem_ld_x16(s_at + (g + 1) * 16, v[(g + 1) & 1]);
+                        if (border) hide(g, w);
+                        float tops[4];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float4 sc = tile.scale[2 * c + h];
-                            float tops[4];
-#pragma unroll
-                            for (int z = 0; z < 4; ++z)
-                                tops[z] = fmaxf(fmaxf(__uint_as_float(w[16 * h + z]), __uint_as_float(w[16 * h + z + 4])),
-                                                fmaxf(__uint_as_float(w[16 * h + z + 8]), __uint_as_float(w[16 * h + z + 12])));
-                            const float raw = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-                            top = fmaxf(top, fmaf(raw, fmaxf(rowf * sc.x, 1.17549435e-38f), sc.y));      // (never 0: a hidden score is -infinity times it)
-                        }
+                        for (int z = 0; z < 4; ++z)
+                            tops[z] = fmaxf(fmaxf(__uint_as_float(w[z]), __uint_as_float(w[z + 4])), fmaxf(__uint_as_float(w[z + 8]), __uint_as_float(w[z + 12])));
+                        const float raw = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                        top = fmaxf(top, fmaf(raw, fmaxf(rowf * scales[g].x, 1.17549435e-38f), scales[g].y));      // (never 0: a hidden score is -infinity times it)
                     }
-                    const bool moves = top - m > kTop + kSlack;
-                    if (__any_sync(0xFFFFFFFFu, moves)) {
-                        const float next = moves ? top - kTop : m, shrink = ex2(m - next);
+                    if (pair_any(top - m > kTop + kSlack)) {
+                        s_pair[t][half][row] = top;
+                        pair_sync();
+                        top = fmaxf(top, s_pair[t][half ^ 1][row]);
+                        const float next = top - m > kTop + kSlack ? top - kTop : m, shrink = ex2(m - next);
                         m = next;
                         l *= shrink;
                         if (i > 0) {                  // (S of this tile was asked for behind O of the last, which is therefore done)
 #pragma unroll 1
-                            for (int c16 = 0; c16 < 8; ++c16) {
-                                uint32_t o[16];
-                                tmem_ld_x16(o_at + c16 * 16, o);
+                            for (int g = 0; g < 4; ++g) {
+                                tmem_ld_x16(o_at + g * 16, v[0]);
                                 tmem_wait_ld();
 #pragma unroll
-                                for (int z = 0; z < 16; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * shrink);
-                                tmem_st<16>(o_at + c16 * 16, o);
+                                for (int z = 0; z < 16; ++z) v[0][z] = __float_as_uint(__uint_as_float(v[0][z]) * shrink);
+                                tmem_st<16>(o_at + g * 16, v[0]);
                             }
                         }
+                        pair_sync();                  // (s_pair is free again)
                     }
                     // ---- the weights, two to a column, over scores that have been read
-                    tmem_ld_x32(s_at, v[0]);
+                    tmem_ld_x16(s_at, v[0]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t* w = v[c & 1];
+                    for (int g = 0; g < 4; ++g) {
+                        uint32_t* w = v[g & 1];
                         tmem_wait_ld();
-                        if (c < 3) tmem_ld_x32(s_at + (c + 1) * 32, v[(c + 1) & 1]);
-                        if (border) hide(c, w);
-                        uint32_t p[16];
+                        if (g < 3) tmem_ld_x16(s_at + (g + 1) * 16, v[(g + 1) & 1]);
+                        if (border) hide(g, w);
+                        const float4 sc = scales[g];
+                        const float f = fmaxf(rowf * sc.x, 1.17549435e-38f), off = sc.y - m;
+                        float e[16];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float4 sc = tile.scale[2 * c + h];
-                            const float f = fmaxf(rowf * sc.x, 1.17549435e-38f), off = sc.y - m;
-                            float e[16];
+                        for (int z = 0; z < 16; ++z) e[z] = ex2(fmaf(__uint_as_float(w[z]), f, off));
+                        float sums[4];
 #pragma unroll
-                            for (int z = 0; z < 16; ++z) e[z] = ex2(fmaf(__uint_as_float(w[16 * h + z]), f, off));
-                            float sums[4];
+                        for (int z = 0; z < 4; ++z) sums[z] = (e[z] + e[z + 4]) + (e[z + 8] + e[z + 12]);
+                        l = fmaf((sums[0] + sums[1]) + (sums[2] + sums[3]), sc.z, l);
+                        uint32_t p[8];
 #pragma unroll
-                            for (int z = 0; z < 4; ++z) sums[z] = (e[z] + e[z + 4]) + (e[z + 8] + e[z + 12]);
-                            l = fmaf((sums[0] + sums[1]) + (sums[2] + sums[3]), sc.z, l);
-#pragma unroll
-                            for (int z = 0; z < 8; ++z) {
-                                const __half2 w2 = __floats2half2_rn(e[2 * z], e[2 * z + 1]);
-                                p[8 * h + z] = *reinterpret_cast<const uint32_t*>(&w2);
-                            }
+                        for (int z = 0; z < 8; ++z) {
+                            const __half2 w2 = __floats2half2_rn(e[2 * z], e[2 * z + 1]);
+                            p[z] = *reinterpret_cast<const uint32_t*>(&w2);
                         }
-                        tmem_st<16>(s_at + c * 16, p);
+                        tmem_st<8>(s_at + g * 8, p);
                     }
                     tmem_wait_st();
                     tc_fence_before();
@@ -396,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int64_t out_was = out_at, lse_was = lse_at;
             const bool real_was = real;
             // ---- the next unit's q while the last O is on its way
-            u = unit(k);
+            u = next_unit(k);
             if (u.n >= 0 && takes_part(u)) begin_unit(u);
             if (!part) continue;
             if (n > 0) {
@@ -405,41 +419,46 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();
                 tc_fence_after();
             }
+            s_pair[t][half][row] = l;
+            pair_sync();
+            l += s_pair[t][half ^ 1][row];
             const bool whole = slot_at < 0, store = real_was && *abort_flag == 0;       // (nothing of an aborted call is stored)
             const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + out_was;
             float* slot = slots + max(slot_at, 0) * (int64_t)slot_floats(kUnitRows, kDim);
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[32];
+            for (int g = 0; g < 4; ++g) {             // 16 elements of this half
+                uint32_t v[16];
                 if (n > 0) {
-                    tmem_ld_x16(o_at + c * 32, v);
-                    tmem_ld_x16(o_at + c * 32 + 16, v + 16);
+                    tmem_ld_x16(o_at + g * 16, v);
                     tmem_wait_ld();
                 } else {
 #pragma unroll
-                    for (int z = 0; z < 32; ++z) v[z] = 0;
+                    for (int z = 0; z < 16; ++z) v[z] = 0;
                 }
-                float x[32];
+                float x[16];
 #pragma unroll
-                for (int z = 0; z < 32; ++z) x[z] = __uint_as_float(v[z]) * inv;
+                for (int z = 0; z < 16; ++z) x[z] = __uint_as_float(v[z]) * inv;
                 if (!store) continue;
+                const int at = half * 64 + g * 16;
                 if (whole) {
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) stg128(out + c * 32 + z * 8, pack<__nv_bfloat16>(x + 8 * z));
+                    for (int z = 0; z < 2; ++z) stg128(out + at + z * 8, pack<__nv_bfloat16>(x + 8 * z));
                 } else {
 #pragma unroll
-                    for (int z = 0; z < 8; ++z) stg128(slot + 2 * kUnitRows + mine * kDim + c * 32 + z * 4, pack<float>(x + 4 * z));
+                    for (int z = 0; z < 4; ++z) stg128(slot + 2 * kUnitRows + mine * kDim + at + z * 4, pack<float>(x + 4 * z));
                 }
             }
             tc_fence_before();                        // (the next O begins behind this thread's next weights)
-            if (store) {
+            if (store && half == 0) {
                 if (!whole) slot[mine] = m, slot[kUnitRows + mine] = l;
                 else if (a.lse != nullptr) a.lse[lse_was] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718056f;
             }
+            pair_sync();                              // (s_pair is free again)
         }
     } else if (warp < kMmaWarp) {
         // ============================================================ codes -> fp16
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConvRegs));
         const int ct = tid - kConvWarp0 * 32, chunk = ct & 7, r0 = ct >> 3;      // chunk of 16 elements, lines r0 + 16 j
         const int64_t lane_at = (int64_t)r0 * kDim + chunk * 16;
         uint4 k[8], v[8];
@@ -494,7 +513,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_arrive(bar(&ctrl.v_full[st]));
             if (more) load(next, a.c.v, v);
         }
-    } else if (warp == kMmaWarp) {
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+      if (warp == kMmaWarp) {
         // ============================================================ MMAs
         const bool leader = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
@@ -526,7 +547,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const uint64_t va = (uint64_t)((kt & 1) * (kOperandBytes >> 4));
 #pragma unroll
                 for (int j = 0; j < 8; ++j)           // 16 keys a step: two groups of 8 lines
-                    umma_bf16_ts(tm + kOCol + (uint32_t)(t * 128), tm + (uint32_t)(t * 128 + j * 8), v_desc + va + j * (2048 >> 4), idesc_o, !begins || j > 0);
+                    umma_bf16_ts(tm + kOCol + (uint32_t)(t * 128), tm + (uint32_t)(t * 128 + (j >> 2) * 64 + (j & 3) * 8), v_desc + va + j * (2048 >> 4), idesc_o, !begins || j > 0);
                 if (last) {
                     umma_commit(bar(&ctrl.v_empty[kt & 1]));
                     umma_commit(bar(&ctrl.tile_empty[kt % kTileQueue]));
@@ -568,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         while (!mbar_try_wait(bar(&ctrl.drained), 0))
             if (clock64() - c0 > kTimeoutCycles) break;
         __syncwarp();
-    } else {
+      } else if (warp == kWalkWarp) {
         // ============================================================ units, pages, scales
         const int plog = a.c.page_log2;
         TileWalk walk(a);
@@ -648,6 +669,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) tile.kind = 2;
         hand_over();
         if (lane == 0) cuts[blockIdx.x] = *abort_flag == 0 ? cut : CutUnit{0, 0, 0, 0};
+      }
     }
     tc_fence_before();
     __syncthreads();
