@@ -1,36 +1,41 @@
 // Position rotation and append to the paged 8-bit cache (molora_kv_append).
 //
-// A block of the cache (one page of one head) has one scale, so what a call adds to a block is handled by one CTA (or, a few
-// tokens only, by one warp): it holds the rotated values in registers, reduces their largest magnitude, and writes codes and
-// scale.  Nothing is read twice; older tokens of the block are touched only when the scale has to grow, which a power of two
-// does seldom and, for e4m3 codes, without rounding anything but values that become subnormal.
+// A block of the cache (one page of one head) has one scale, so what a call adds to a block is handled by one CTA, or, a few
+// tokens only, by a part of a warp: it holds the rotated values in registers, reduces their largest magnitude, and writes codes and
+// scale.  Older tokens of the block are touched only when the scale has to grow, which a power of two does seldom and, for e4m3
+// codes, without rounding anything but values that become subnormal.
 //   grid.x   runs of `run` consecutive rows; a CTA takes the pieces (rows of one sequence inside one page) that begin in its run
 //   grid.y   groups of kHeadsPerCta heads of k, of v, of q
-// A thread's unit is 16 elements of a row -- two 8-element vectors that the rotation pairs, or that lie side by side -- and stays
-// the same for every head of the group, so sines and cosines are computed once per CTA, in turns: p * f / 2 pi in 64 bits, reduced
-// to half a turn, then sinpi / cospi in fp32.
+// Sines and cosines are computed once per piece, into shared memory, in turns: p * f / 2 pi in 64 bits, reduced to half a turn, then
+// sinpi / cospi in fp32.  A thread's unit is 16 elements of a row -- two 8-element vectors that the rotation pairs, or that lie side by
+// side -- and stays the same for every head of the group; the next head's vectors are on their way while a head is worked on (asked
+// for when its turn came, two units a thread: 71 us against 55 for 8192 tokens of 32 + 2 x 8 heads of 128, 185 MB, 3.3 TB/s).
+// What bounds it there: issue slots (60 % busy, the conversions above all) and 16 warps per SM; a token each: the chain of dependent reads.
 #include "kv_cache.cuh"
 
 namespace molora {
 namespace {
 
 constexpr int kHeadsPerCta = 8;
-constexpr int kUnits = 2;              // units per thread: a page of 128 tokens of 128 elements over 512 threads
-constexpr int kWarpTokens = 8;         // pieces of up to this many tokens: a warp per head
+constexpr int kMaxThreads = 1024;      // a page of 128 tokens of 128 elements
 
+// the two vectors of a unit as they lie in memory
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* x);
-template <>
-__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float* x)
-{
-    unpack<__nv_bfloat16>(ld128_rw_stream(p), x);
-}
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float* x)
-{
-    unpack<float>(ld128_rw_stream(p), x);
-    unpack<float>(ld128_rw_stream(p + 4), x + 4);
-}
+struct Raw {
+    static constexpr int kWords = 16 / VecTraits<T>::kElems;
+    uint4 w[kWords];
+    __device__ __forceinline__ void load(const T* row, int off0, int off1)
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+            w[i] = ld128_rw_stream(row + (i < kWords / 2 ? off0 : off1) + i % (kWords / 2) * VecTraits<T>::kElems);
+    }
+    __device__ __forceinline__ void values(float* x) const
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) unpack<T>(w[i], x + i * VecTraits<T>::kElems);
+    }
+};
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const float* x)
 {
@@ -57,52 +62,46 @@ __device__ __forceinline__ float scale_for(float amax)
     return __uint_as_float((uint32_t)(max(-64, min(64, e)) + 127) << 23);
 }
 
-// One unit of a thread: where its two vectors lie in a row, and its eight pairs' cosines and sines.
+// One unit of a thread: where its two vectors lie in a row, and its eight pairs' cosines and sines (in shared memory).
 struct Unit {
-    int token;                 // within the piece; past its end: no unit
+    int token;                 // within the piece
     int off0, off1;
     int kind;                  // 0: not rotated, 1: pairs across the two vectors, 2: neighbours inside each
-    float c[8], s[8];
+    const float4* turn;        // cos, sin, cos, sin of two pairs each
+    __device__ __forceinline__ Unit(int id, const AppendArgs& a, bool rotate, const float2* turns)
+    {
+        const int per_token = a.dim >> 4, j = id % per_token;
+        token = id / per_token;
+        const int rotary = rotate ? a.rotary : 0;
+        off0 = j * 16, off1 = j * 16 + 8, kind = 0, turn = nullptr;
+        if (j * 16 < rotary) {
+            kind = a.interleaved ? 2 : 1;
+            if (!a.interleaved) off0 = j * 8, off1 = j * 8 + rotary / 2;
+            turn = reinterpret_cast<const float4*>(turns + token * (rotary / 2) + j * 8);
+        }
+    }
+    __device__ __forceinline__ void rotate(float* x) const
+    {
+        if (kind == 0) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 t = turn[i];
+            if (kind == 1) {
+                turn_pair(x[2 * i], x[8 + 2 * i], t.x, t.y);
+                turn_pair(x[2 * i + 1], x[8 + 2 * i + 1], t.z, t.w);
+            } else {
+                turn_pair(x[4 * i], x[4 * i + 1], t.x, t.y);
+                turn_pair(x[4 * i + 2], x[4 * i + 3], t.z, t.w);
+            }
+        }
+    }
+    static __device__ __forceinline__ void turn_pair(float& p, float& q, float c, float s)
+    {
+        const float a = p, b = q;
+        p = a * c - b * s;
+        q = b * c + a * s;
+    }
 };
-
-__device__ __forceinline__ void make_unit(Unit& u, int id, int count, int pos0, const AppendArgs& a, bool rotate)
-{
-    const int per_token = a.dim >> 4, j = id % per_token;
-    u.token = id / per_token;
-    const int rotary = rotate ? a.rotary : 0;
-    u.off0 = j * 16, u.off1 = j * 16 + 8, u.kind = 0;
-    if (j * 16 < rotary) {
-        u.kind = a.interleaved ? 2 : 1;
-        if (!a.interleaved) u.off0 = j * 8, u.off1 = j * 8 + rotary / 2;
-    }
-    if (u.kind == 0 || u.token >= count) return;
-    const double pos = (double)(pos0 + u.token);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const double turns = pos * (double)ptx::ld_dependent(a.inv_freq + j * 8 + i) * 0.15915494309189533577;      // 1 / 2 pi
-        const float half_turns = (float)((turns - rint(turns)) * 2.0);
-        sincospif(half_turns, &u.s[i], &u.c[i]);
-    }
-}
-
-__device__ __forceinline__ void rotate_unit(const Unit& u, float* x)
-{
-    if (u.kind == 1) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float a = x[i], b = x[8 + i];
-            x[i] = a * u.c[i] - b * u.s[i];
-            x[8 + i] = b * u.c[i] + a * u.s[i];
-        }
-    } else if (u.kind == 2) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float a = x[2 * i], b = x[2 * i + 1];
-            x[2 * i] = a * u.c[i] - b * u.s[i];
-            x[2 * i + 1] = b * u.c[i] + a * u.s[i];
-        }
-    }
-}
 
 __device__ __forceinline__ float finite_amax(const float* x, float m)
 {
@@ -160,11 +159,12 @@ __device__ __forceinline__ int sequence_of_row(const int32_t* cu, int B, int64_t
 }
 
 template <typename T>
-__global__ void __launch_bounds__(512) kv_append_kernel(const __grid_constant__ AppendArgs a)
+__global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_constant__ AppendArgs a)
 {
-    __shared__ float warp_max[16];
+    __shared__ float warp_max[kMaxThreads / 32];
+    extern __shared__ __align__(16) float2 turns[];        // [token of the piece][pair]: cosine, sine
     ptx::grid_dependency_sync();
-    const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31, threads = (int)blockDim.x, warps = threads >> 5;
+    const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31, threads = (int)blockDim.x;
     // the group of heads
     const int g = (int)blockIdx.y;
     const int kind = g < a.k_groups ? 0 : g < 2 * a.k_groups ? 1 : 2;                  // k, v, q
@@ -189,8 +189,7 @@ __global__ void __launch_bounds__(512) kv_append_kernel(const __grid_constant__ 
         const int64_t j = i - sq.row0;
         if (j < 0) break;                                  // (rows of no sequence: cu does not start at 0)
         const int pos = sq.first_pos() + (int)j;
-        const bool report = sq.bad && tid == 0 && g == 0 && a.dev_status != nullptr;
-        if (report) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
+        if (sq.bad && tid == 0 && g == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
         if (pos < 0) {                                     // in front of the sequence's beginning: left out
             i = min(end, i - pos);
             continue;
@@ -203,75 +202,104 @@ __global__ void __launch_bounds__(512) kv_append_kernel(const __grid_constant__ 
         }
         const int at = pos >> a.c.page_log2;
         const int32_t id = at < a.c.max_pages ? ptx::ld_dependent(a.c.table + b * a.c.ld_table + at) : -1;
-        const bool usable = id >= 0 && id < a.c.n_pages;
-        if (!usable && kind != 2) {
+        if ((id < 0 || id >= a.c.n_pages) && kind != 2) {
             if (tid == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
             i += count;
             continue;
         }
-        const bool by_warp = count <= kWarpTokens;
-        const int id0 = by_warp ? lane : tid, stride = by_warp ? 32 : threads;
-        Unit u[kUnits];
-#pragma unroll
-        for (int n = 0; n < kUnits; ++n) make_unit(u[n], id0 + n * stride, count, pos, a, kind != 1);
-        if (kind == 2) {
-            const int ahead = by_warp ? warps : 1;
-            for (int h = h0 + (by_warp ? warp : 0); h < h1; h += ahead) {
-                float x[kUnits][16];
-#pragma unroll
-                for (int n = 0; n < kUnits; ++n) {
-                    if (u[n].token >= count) continue;
-                    const T* p = src + (i + u[n].token) * ld + h * a.dim;
-                    load8(p + u[n].off0, x[n]);
-                    load8(p + u[n].off1, x[n] + 8);
-                }
-#pragma unroll
-                for (int n = 0; n < kUnits; ++n) {
-                    if (u[n].token >= count) continue;
-                    rotate_unit(u[n], x[n]);
-                    T* p = static_cast<T*>(a.q_out) + (i + u[n].token) * a.ldqo + h * a.dim;
-                    store8(p + u[n].off0, x[n]);
-                    store8(p + u[n].off1, x[n] + 8);
-                }
+        // Threads per head, a power of two: as many as the piece has units, so that several heads are in hand at a time where it is short
+        // (what lies inside a warp needs no barrier); a piece of more units than there are threads is gone through twice.
+        const int total = count * units;
+        const bool small = total <= threads;
+        const int sub = small ? 1 << (32 - __clz(max(total - 1, 1))) : threads;
+        const bool by_warp = sub <= 32;
+        const int mine = tid & (sub - 1), first = h0 + tid / sub, step = threads / sub;
+        if (kind != 1 && a.rotary > 0) {
+            const int pairs = a.rotary >> 1;
+            __syncthreads();                               // (the last piece's are done with)
+            for (int z = tid; z < count * pairs; z += threads) {
+                const int token = z / pairs;
+                const double angle = (double)(pos + token) * (double)ptx::ld_dependent(a.inv_freq + (z - token * pairs)) * 0.15915494309189533577;      // 1 / 2 pi
+                float2 t;
+                sincospif((float)((angle - rint(angle)) * 2.0), &t.y, &t.x);
+                turns[z] = t;
             }
-        } else {
-            for (int h = h0 + (by_warp ? warp : 0); h < h1; h += by_warp ? warps : 1) {
-                const int64_t block = (int64_t)id * a.c.kv_heads + h;
-                uint8_t* rows = codes + ((block << a.c.page_log2) * a.dim);
-                const float old = row0 > 0 ? scales[block] : 0.f;
-                float x[kUnits][16], m = 0.f;
-#pragma unroll
-                for (int n = 0; n < kUnits; ++n) {
-                    if (u[n].token >= count) continue;
-                    const T* p = src + (i + u[n].token) * ld + h * a.dim;
-                    load8(p + u[n].off0, x[n]);
-                    load8(p + u[n].off1, x[n] + 8);
+            __syncthreads();
+        }
+        const Unit u(min(mine, total - 1), a, kind != 1, turns);
+        // (whole warps stay together: heads past the last and lanes without a unit go along)
+        const int rounds = (h1 - h0 + step - 1) / step;
+        const bool have = mine < total;
+        Raw<T> raw;
+        auto row_of = [&](int h, const Unit& v) { return src + (i + v.token) * ld + h * a.dim; };
+        if (have && first < h1) raw.load(row_of(first, u), u.off0, u.off1);
+        for (int r = 0; r < rounds; ++r) {
+            const int h = first + r * step;
+            const bool on = have && h < h1;
+            float x[16];
+            raw.values(x);
+            if (have && h + step < h1) raw.load(row_of(h + step, u), u.off0, u.off1);
+            u.rotate(x);
+            if (kind == 2) {
+                auto put = [&](const Unit& v) {
+                    T* p = static_cast<T*>(a.q_out) + (i + v.token) * a.ldqo + h * a.dim;
+                    store8(p + v.off0, x);
+                    store8(p + v.off1, x + 8);
+                };
+                if (on) put(u);
+                if (!small)
+                    for (int z = tid + threads; z < total; z += threads) {
+                        const Unit v(z, a, true, turns);
+                        Raw<T> w;
+                        w.load(row_of(h, v), v.off0, v.off1);
+                        w.values(x);
+                        v.rotate(x);
+                        put(v);
+                    }
+                continue;
+            }
+            const int64_t block = (int64_t)id * a.c.kv_heads + min(h, h1 - 1);
+            uint8_t* rows = codes + ((block << a.c.page_log2) * a.dim);
+            const float old = row0 > 0 ? scales[block] : 0.f;
+            float m = on ? finite_amax(x, 0.f) : 0.f;
+            if (!small)                                    // more units than threads: the others are read twice
+                for (int z = tid + threads; z < total; z += threads) {
+                    const Unit v(z, a, kind == 0, turns);
+                    Raw<T> w;
+                    float y[16];
+                    w.load(row_of(h, v), v.off0, v.off1);
+                    w.values(y);
+                    v.rotate(y);
+                    m = finite_amax(y, m);
                 }
-#pragma unroll
-                for (int n = 0; n < kUnits; ++n) {
-                    if (u[n].token >= count) continue;
-                    rotate_unit(u[n], x[n]);
-                    m = finite_amax(x[n], m);
-                }
+            for (int o = min(sub, 32) >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+            if (!by_warp) {
+                if (lane == 0) warp_max[warp] = m;
+                __syncthreads();
+                const int per = sub >> 5;                  // warps of this head
+                m = warp_max[(warp & ~(per - 1)) + (lane & (per - 1))];
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-                if (!by_warp) {
-                    if (lane == 0) warp_max[warp] = m;
-                    __syncthreads();
-                    for (int w = 0; w < warps; ++w) m = fmaxf(m, warp_max[w]);
-                    __syncthreads();                       // (everybody has read it, and the old scale, before either is written again)
+                __syncthreads();                           // (everybody has read it, and the old scale, before either is written again)
+            }
+            __syncwarp();
+            const float scale = row0 > 0 ? fmaxf(old, scale_for(m)) : scale_for(m);
+            if (h >= h1) continue;
+            if (mine == 0) scales[block] = scale;
+            const float inv = 1.f / scale;
+            if (have) store_codes(rows + (int64_t)(row0 + u.token) * a.dim, u, x, inv);
+            if (!small)
+                for (int z = tid + threads; z < total; z += threads) {
+                    const Unit v(z, a, kind == 0, turns);
+                    Raw<T> w;
+                    w.load(row_of(h, v), v.off0, v.off1);
+                    w.values(x);
+                    v.rotate(x);
+                    store_codes(rows + (int64_t)(row0 + v.token) * a.dim, v, x, inv);
                 }
-                __syncwarp();
-                const float scale = row0 > 0 ? fmaxf(old, scale_for(m)) : scale_for(m);
-                if (id0 == 0) scales[block] = scale;
-                const float inv = 1.f / scale;
-#pragma unroll
-                for (int n = 0; n < kUnits; ++n)
-                    if (u[n].token < count) store_codes(rows + (int64_t)(row0 + u[n].token) * a.dim, u[n], x[n], inv);
-                if (row0 > 0 && scale != old) {
-                    const float ratio = old * inv;
-                    for (int w = id0; w < row0 * units; w += stride) regrow16(rows + (int64_t)w * 16, ratio);
-                }
+            if (row0 > 0 && scale != old) {
+                const float ratio = old * inv;
+                for (int w = mine; w < row0 * units; w += sub) regrow16(rows + (int64_t)w * 16, ratio);
             }
         }
         i += count;
@@ -281,11 +309,19 @@ __global__ void __launch_bounds__(512) kv_append_kernel(const __grid_constant__ 
 template <typename T>
 molora_status_t launch(const AppendArgs& a, cudaStream_t s)
 {
-    const int page = 1 << a.c.page_log2;
-    const int threads = max(256, page * (a.dim >> 4) / kUnits);
+    // powers of two: single tokens, a warp for four heads of 128; drafts; one unit per thread of the largest piece there can be
+    const int most = (1 << a.c.page_log2) * (a.dim >> 4);
+    const int threads = a.run == 1 ? 128 : a.run < 16 ? 256 : max(512, min(kMaxThreads, most));
     const int groups = 2 * a.k_groups + ceil_div(a.heads, kHeadsPerCta);
     const dim3 grid((unsigned)ceil_div64(a.N, a.run), (unsigned)groups);
-    return cuda_ok(launch_kernel(kv_append_kernel<T>, grid, dim3((unsigned)threads), 0, s, 1, true, a));
+    const size_t turns = (size_t)min((int64_t)(1 << a.c.page_log2), a.N) * (a.rotary >> 1) * sizeof(float2);      // at most 64 KB
+    static bool ready[kMaxDevices] = {};
+    bool& done = ready[device_slot()];
+    if (!done) {
+        if (cudaFuncSetAttribute(kv_append_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 65536) != cudaSuccess) return MOLORA_ERR_CUDA;
+        done = true;
+    }
+    return cuda_ok(launch_kernel(kv_append_kernel<T>, grid, dim3((unsigned)threads), turns, s, 1, true, a));
 }
 
 }  // namespace
@@ -303,8 +339,9 @@ molora_status_t launch_kv_append(const KvView& c, molora_dtype_t dt, int64_t N, 
     a.inv_freq = inv_freq;
     a.dev_status = dev_status;
     a.k_groups = ceil_div(c.kv_heads, kHeadsPerCta);
-    // rows per CTA: one while that is a few waves, else as many as the smallest page, so that most CTAs begin a piece
-    a.run = N <= 1024 ? 1 : 16;
+    // Rows per CTA: as many as a sequence has on average, a page at most.  A CTA in whose run no piece begins costs its search (2 us, and
+    // with runs of 16 rows three of four have none where whole pages of 64 are written), one in whose run many begin takes them in turn.
+    a.run = (int32_t)max((int64_t)1, min((int64_t)(1 << c.page_log2), N / c.B));
     return dt == MOLORA_F32 ? launch<float>(a, s) : launch<__nv_bfloat16>(a, s);
 }
 
