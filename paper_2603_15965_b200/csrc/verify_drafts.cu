@@ -4,16 +4,17 @@
 // draft: three dependent gathers).  That names the one row of p, and after a refusal the one row of q, that have to be
 // read: max(p - q, 0) is summed in 64 bits, each warp over a contiguous piece of the CTA's contiguous slice, the slices' sums are
 // exchanged through distributed shared memory, and the CTA in which the running sum passes u * total looks at the piece
-// of the warp in which it does once more (from L2), a short run per thread.  So the vocabulary is read once, and the order of summation does not matter to more
-// than the last bits of 64.
-// What bounds it: the two rows, 8 bytes per word of the vocabulary in fp32; with few sequences the chain of dependent reads.
+// of the warp in which it does once more (from L2), a short run per thread.  So the vocabulary is read once, and the order of
+// summation does not matter to more than the last bits of 64.
+// What bounds it: the two rows, 8 bytes per word of the vocabulary in fp32 (64 sequences, 160,000 words, five drafts: 21.5 us for the
+// 68 MB that these acceptances ask for, 3.2 TB/s); the chain of dependent reads and the exchange take 6 us of any call.
 #include "common.cuh"
 #include "kv_cache.cuh"
 
 namespace molora {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kMaxThreads = 512, kMaxWarps = kMaxThreads / 32;
 constexpr int kMaxCluster = 8;
 
 __device__ __forceinline__ float load_prob(const float* p) { return ptx::ld_dependent(p); }
@@ -90,7 +91,7 @@ __device__ double piece_sum(const Residual<T>& r, int lo, int hi)
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) verify_drafts_kernel(const T* __restrict__ target, int64_t tls, int64_t tl,
+__global__ void __launch_bounds__(kMaxThreads, 2) verify_drafts_kernel(const T* __restrict__ target, int64_t tls, int64_t tl,
                                                                  const T* __restrict__ draft, int64_t dls, int64_t dl,
                                                                  const int32_t* __restrict__ drafted,
                                                                  const int32_t* __restrict__ n_drafted,
@@ -99,11 +100,12 @@ __global__ void __launch_bounds__(kThreads) verify_drafts_kernel(const T* __rest
                                                                  uint32_t* dev_status)
 {
     __shared__ double slice_sum[2];                    // this CTA's, read by its peers: with q, and without (the second only where needed)
-    __shared__ double piece[kWarps], run[kWarps];
+    __shared__ double piece[kMaxWarps], run[kMaxWarps];
     __shared__ int s_accepted, s_n, s_bad, s_last;
     ptx::grid_dependency_sync();
     const int ctas = (int)ptx::cluster_nctarank(), rank = (int)ptx::cluster_ctarank();
     const int b = (int)blockIdx.x / ctas, tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int threads = (int)blockDim.x, warps = threads >> 5;
 
     if (warp == 0) {
         const int n = n_drafted != nullptr ? max(0, min(S, ptx::ld_dependent(n_drafted + b))) : S;
@@ -133,14 +135,14 @@ __global__ void __launch_bounds__(kThreads) verify_drafts_kernel(const T* __rest
     // slices of whole 32-byte sectors, pieces of the slices likewise
     const int slice = ceil_div(ceil_div(V, ctas), 16) * 16;
     const int lo = min(V, rank * slice), hi = min(V, lo + slice);
-    const int per = ceil_div(ceil_div(slice, kWarps), 16) * 16;
+    const int per = ceil_div(ceil_div(slice, warps), 16) * 16;
     double sums[kMaxCluster], total = 0.0;                // the slices' sums, the same bits in every CTA
     for (int round = 0;; ++round) {
         const double s = piece_sum(r, min(hi, lo + warp * per), min(hi, lo + (warp + 1) * per));
         if (lane == 0) piece[warp] = s;
         __syncthreads();
         double own = 0.0;
-        for (int w = 0; w < kWarps; ++w) own += piece[w];
+        for (int w = 0; w < warps; ++w) own += piece[w];
         if (ctas > 1) {
             if (tid == 0) slice_sum[round] = own;
             ptx::cluster_sync_all();
@@ -185,14 +187,14 @@ __global__ void __launch_bounds__(kThreads) verify_drafts_kernel(const T* __rest
             double at = before;
             int w = 0, held = -1;
             double held_at = before;
-            for (; w < kWarps; ++w) {                     // (every thread walks the same few sums)
+            for (; w < warps; ++w) {                     // (every thread walks the same few sums)
                 if (piece[w] > 0.0) held = w, held_at = at;
                 if (at + piece[w] > goal && piece[w] > 0.0) break;
                 at += piece[w];
             }
             w = held, at = held_at;
             const int p0 = min(hi, lo + w * per), p1 = min(hi, lo + (w + 1) * per);
-            const int len = ceil_div(max(p1 - p0, 1), kThreads);
+            const int len = ceil_div(max(p1 - p0, 1), threads);
             const int t0 = min(p1, p0 + tid * len), t1 = min(p1, t0 + len);
             double mine_sum = 0.0;
             for (int t = t0; t < t1; ++t) mine_sum += r.at(t);
@@ -252,11 +254,14 @@ molora_status_t launch(const void* target, int64_t tls, int64_t tl, const void* 
                        const int32_t* n_drafted, const float* uniform, int32_t B, int32_t S, int32_t V, int32_t* tokens, int32_t* accepted,
                        uint32_t* dev_status, cudaStream_t s)
 {
-    // CTAs per sequence: enough for the SMs (two CTAs each), none with less than 2048 words
+    // CTAs per sequence: enough for the SMs (four CTAs of 256 threads each, 64 registers a thread), none with less than 2048 words; 512
+    // threads where two such CTAs per SM take them all.  What is past the SMs' room waits for a whole CTA's time: 64 sequences of 160,000
+    // words in clusters of eight CTAs of 512 threads took 29 us.
     int ctas = 1;
     while (ctas < kMaxCluster && (int64_t)B * ctas < 2 * sm_count() && V >= ctas * 2 * 2048) ctas *= 2;
+    const int threads = (int64_t)B * ctas <= 2 * sm_count() ? kMaxThreads : kMaxThreads / 2;
     const dim3 grid((unsigned)(B * (int64_t)ctas));
-    return cuda_ok(launch_kernel(verify_drafts_kernel<T>, grid, dim3(kThreads), 0, s, (unsigned)ctas, true, static_cast<const T*>(target), tls, tl,
+    return cuda_ok(launch_kernel(verify_drafts_kernel<T>, grid, dim3((unsigned)threads), 0, s, (unsigned)ctas, true, static_cast<const T*>(target), tls, tl,
                                  static_cast<const T*>(draft), dls, dl, drafted, n_drafted, uniform, S, V, tokens, accepted, dev_status));
 }
 
