@@ -21,7 +21,7 @@
 namespace molora {
 namespace {
 
-constexpr int kDim = 128, kKeys = 128, kTileRows = 128, kUnitRows = 256;
+constexpr int kDim = 128, kKeys = 128, kStepKeys = 64, kTileRows = 128, kUnitRows = 256;
 constexpr int kThreads = 768;                                 // (the last two warps only make a warpgroup of four)
 constexpr int kConvWarp0 = 16, kMmaWarp = 20, kWalkWarp = 21;
 // Registers: the converting warps hold 64 words of codes, which the last four give up (6 x 128 threads, 80 registers each at launch)
@@ -32,11 +32,12 @@ constexpr int kQAt = 0, kKAt = 2 * kOperandBytes, kVAt = 4 * kOperandBytes;
 constexpr size_t kSmem = 1024 + 6 * (size_t)kOperandBytes;
 constexpr uint32_t kTmemCols = 512, kOCol = 256;
 constexpr int kTileQueue = 8, kUnitQueue = 4;
-constexpr int kUnitCost = 1, kMinShare = 2;                   // tiles of keys
+constexpr int kUnitCost = 3, kMinShare = 4;                   // tiles of keys
 constexpr float kTop = 7.f, kSlack = 8.f;                     // a row's largest weight when its reference is set, and by how much it may grow: fp16
 
 struct Control {
-    uint64_t q_full[2], s_full[2], p_full[2], o_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2];
+    uint64_t s_full[2][2], p_full[2][2], o_done[2][2];         // of each tile of rows, for even and odd steps of it
+    uint64_t q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2];
     uint64_t tile_full[kTileQueue], tile_empty[kTileQueue], unit_full[kUnitQueue], unit_empty[kUnitQueue], drained;
     uint32_t tmem_base;
     int abort_flag;
@@ -56,6 +57,7 @@ struct UnitInfo {
     int32_t row0, first_pos, len;              // of its sequence
     int32_t tile_row, n_rows, head;
     int32_t key0, n;                           // first key, tiles of keys; n -1: there are no more units
+    int32_t steps;                             // of 64 keys: 2 n, or one less where no row sees the last
     int32_t slot;                              // where its piece goes, -1: it is whole
 };
 
@@ -187,8 +189,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     grid_dependency_wait();
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(&ctrl.q_full[i]), 8), mbar_init(bar(&ctrl.s_full[i]), 1);
-            mbar_init(bar(&ctrl.p_full[i]), 2 * kTileRows), mbar_init(bar(&ctrl.o_full[i]), 1);
+            for (int z = 0; z < 2; ++z)
+                mbar_init(bar(&ctrl.s_full[i][z]), 1), mbar_init(bar(&ctrl.p_full[i][z]), 2 * kTileRows), mbar_init(bar(&ctrl.o_done[i][z]), 1);
+            mbar_init(bar(&ctrl.q_full[i]), 8);
             mbar_init(bar(&ctrl.k_full[i]), 128), mbar_init(bar(&ctrl.k_empty[i]), 1);
             mbar_init(bar(&ctrl.v_full[i]), 128), mbar_init(bar(&ctrl.v_empty[i]), 1);
         }
@@ -241,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ============================================================ half a row per thread
         const int t = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane;       // tile, half of the keys, row of the tile = lane of TMEM
         const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_at = tmem + lane_addr + (uint32_t)(t * 128 + half * 64), o_at = tmem + lane_addr + kOCol + (uint32_t)(t * 128 + half * 64);
+        const uint32_t s_at = tmem + lane_addr + (uint32_t)(t * 128 + half * 32), o_at = tmem + lane_addr + kOCol + (uint32_t)(t * 128 + half * 64);
         uint8_t* const q_tile = smem + kQAt + t * kOperandBytes;
         const int pair = 1 + t * 4 + (warp & 3);      // barrier of the two warps that share 32 rows
         auto pair_sync = [&]() { asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair) : "memory"); };
@@ -254,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 : "memory");
             return r != 0;
         };
-        int tiles = 0, own = 0, finished = 0;         // key tiles of the share so far; of them, those that this tile of rows took part in; its Os
+        int tiles = 0, own = 0;                       // key tiles of the share so far; steps that this tile of rows took part in
         float rowf = 0.f;
         int64_t out_at = 0, lse_at = 0;
         int hi_row = 0, lo_row = 0;
@@ -314,49 +317,56 @@ __global__ void __launch_bounds__(kThreads, 1)
         UnitInfo u = next_unit(0);
         if (u.n >= 0 && takes_part(u)) begin_unit(u);
         for (int k = 1; u.n >= 0; ++k) {
-            const int n = u.n, slot_at = u.slot, mine = t * kTileRows + row;
+            const int n = u.n, steps = u.steps, slot_at = u.slot, mine = t * kTileRows + row;
             const bool part = takes_part(u);
             float m = kNone, l = 0.f;
             if (part) {
 #pragma unroll 1
-                for (int i = 0; i < n; ++i, ++own) {
-                    const int kt = tiles + i;
-                    wait_bar(bar(&ctrl.s_full[t]), (uint32_t)own & 1u, abort_flag, a.dev_status);
+                for (int i = 0; i < steps; ++i, ++own) {
+                    const int kt = tiles + (i >> 1), b = own & 1;
+                    const uint32_t parity = (uint32_t)(own >> 1) & 1u;
+                    wait_bar(bar(&ctrl.s_full[t][b]), parity, abort_flag, a.dev_status);
                     // for the scales and what is known of V (its place is not filled again before this thread has handed over its weights, so that this
                     // phase cannot be missed)
-                    wait_bar(bar(&ctrl.v_full[kt & 1]), (uint32_t)(kt >> 1) & 1u, abort_flag, a.dev_status);
+                    if ((i & 1) == 0) wait_bar(bar(&ctrl.v_full[kt & 1]), (uint32_t)(kt >> 1) & 1u, abort_flag, a.dev_status);
+                    // (done before S of this step; waited for so that no phase is missed)
+                    if (own >= 2) wait_bar(bar(&ctrl.o_done[t][b]), parity ^ 1u, abort_flag, a.dev_status);
                     __syncwarp();
                     tc_fence_after();
+                    uint32_t v[32];
+                    tmem_ld_x32(s_at + b * kStepKeys, v);
                     const KeyTile& tile = s_tiles[kt % kTileQueue];
-                    const bool border = tile.kind != 0;
-                    const int first = lo_row - tile.key0 - half * 64, behind = hi_row - tile.key0 - half * 64;      // the row sees [first, behind) of these 64
-                    const float4* scales = tile.scale + 4 * half;
-                    uint32_t v[2][16];                // scores, the next 16 on their way
-                    // what hides scores 16 g .. 16 g + 15
-                    auto hide = [&](int g, uint32_t* w) {
-                        // bits of the keys that the row sees, and of those that are a NaN for it
-                        const int lo = min(max(first - 16 * g, 0), 16), hi = min(max(behind - 16 * g, 0), 16);
-                        const uint32_t sees = scales[g].w == 0.f ? 0u : ((1u << hi) - 1u) & ~((1u << lo) - 1u);
-                        const uint32_t nan = tile.nan[2 * half + (g >> 1)] >> (16 * (g & 1));
+                    const int at = (i & 1) * kStepKeys + half * 32;      // this thread's 32 keys of the tile
+                    const float4* scales = tile.scale + (at >> 4);
+                    const float4 sc0 = scales[0], sc1 = scales[1];
+                    bool seen = true;                                    // some row of the warp sees some of these keys
+                    tmem_wait_ld();
+                    if (tile.kind != 0) {
+                        const int first = max(lo_row - tile.key0 - at, 0), behind = hi_row - tile.key0 - at;      // the row sees [first, behind)
+                        uint32_t sees = first > 31 || behind <= 0 ? 0u : (0xFFFFFFFFu << first) & (0xFFFFFFFFu >> (32 - min(behind, 32)));
+                        if (sc0.w == 0.f) sees &= 0xFFFF0000u;
+                        if (sc1.w == 0.f) sees &= 0x0000FFFFu;
+                        const uint32_t nan = tile.nan[at >> 5];
+                        seen = __any_sync(0xFFFFFFFFu, sees != 0);
+                        if (nan != 0)
 #pragma unroll
-                        for (int z = 0; z < 16; ++z) w[z] = !((sees >> z) & 1u) ? 0xFF800000u : (nan >> z) & 1u ? 0x7FC00000u : w[z];
-                    };
-                    // ---- the largest exponent
-                    float top = -INFINITY;
-                    tmem_ld_x16(s_at, v[0]);
+                            for (int z = 0; z < 32; ++z)
+                                if ((nan >> z) & 1u) v[z] = 0x7FC00000u;
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        uint32_t* w = v[g & 1];
-                        tmem_wait_ld();
-                        if (g < 3) tmem_ld_x16(s_at + (g + 1) * 16, v[(g + 1) & 1]);
-                        if (border) hide(g, w);
+                        for (int z = 0; z < 32; ++z)
+                            if (!((sees >> z) & 1u)) v[z] = 0xFF800000u;
+                    }
+                    // ---- the largest exponent (a factor is never 0: a hidden score is -infinity times it)
+                    const float f0 = fmaxf(rowf * sc0.x, 1.17549435e-38f), f1 = fmaxf(rowf * sc1.x, 1.17549435e-38f);
+                    auto top_of = [](const uint32_t* w) {
                         float tops[4];
 #pragma unroll
                         for (int z = 0; z < 4; ++z)
                             tops[z] = fmaxf(fmaxf(__uint_as_float(w[z]), __uint_as_float(w[z + 4])), fmaxf(__uint_as_float(w[z + 8]), __uint_as_float(w[z + 12])));
-                        const float raw = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-                        top = fmaxf(top, fmaf(raw, fmaxf(rowf * scales[g].x, 1.17549435e-38f), scales[g].y));      // (never 0: a hidden score is -infinity times it)
-                    }
+                        return fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                    };
+                    float top = -INFINITY;
+                    if (seen) top = fmaxf(fmaf(top_of(v), f0, sc0.y), fmaf(top_of(v + 16), f1, sc1.y));
                     if (pair_any(top - m > kTop + kSlack)) {
                         s_pair[t][half][row] = top;
                         pair_sync();
@@ -364,46 +374,47 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const float next = top - m > kTop + kSlack ? top - kTop : m, shrink = ex2(m - next);
                         m = next;
                         l *= shrink;
-                        if (i > 0) {                  // (S of this tile was asked for behind O of the last, which is therefore done)
+                        if (i > 0) {
+                            wait_bar(bar(&ctrl.o_done[t][b ^ 1]), (uint32_t)((own - 1) >> 1) & 1u, abort_flag, a.dev_status);
+                            __syncwarp();
+                            tc_fence_after();
 #pragma unroll 1
-                            for (int g = 0; g < 4; ++g) {
-                                tmem_ld_x16(o_at + g * 16, v[0]);
+                            for (int g = 0; g < 8; ++g) {
+                                uint32_t o[8];
+                                tmem_ld_x8(o_at + g * 8, o);
                                 tmem_wait_ld();
 #pragma unroll
-                                for (int z = 0; z < 16; ++z) v[0][z] = __float_as_uint(__uint_as_float(v[0][z]) * shrink);
-                                tmem_st<16>(o_at + g * 16, v[0]);
+                                for (int z = 0; z < 8; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * shrink);
+                                tmem_st<8>(o_at + g * 8, o);
                             }
                         }
                         pair_sync();                  // (s_pair is free again)
                     }
                     // ---- the weights, two to a column, over scores that have been read
-                    tmem_ld_x16(s_at, v[0]);
+                    uint32_t p[16];
+                    if (seen) {
+                        const float off0 = sc0.y - m, off1 = sc1.y - m;
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        uint32_t* w = v[g & 1];
-                        tmem_wait_ld();
-                        if (g < 3) tmem_ld_x16(s_at + (g + 1) * 16, v[(g + 1) & 1]);
-                        if (border) hide(g, w);
-                        const float4 sc = scales[g];
-                        const float f = fmaxf(rowf * sc.x, 1.17549435e-38f), off = sc.y - m;
-                        float e[16];
+                        for (int g = 0; g < 2; ++g) {
+                            float sums[4] = {};
 #pragma unroll
-                        for (int z = 0; z < 16; ++z) e[z] = ex2(fmaf(__uint_as_float(w[z]), f, off));
-                        float sums[4];
-#pragma unroll
-                        for (int z = 0; z < 4; ++z) sums[z] = (e[z] + e[z + 4]) + (e[z + 8] + e[z + 12]);
-                        l = fmaf((sums[0] + sums[1]) + (sums[2] + sums[3]), sc.z, l);
-                        uint32_t p[8];
-#pragma unroll
-                        for (int z = 0; z < 8; ++z) {
-                            const __half2 w2 = __floats2half2_rn(e[2 * z], e[2 * z + 1]);
-                            p[z] = *reinterpret_cast<const uint32_t*>(&w2);
+                            for (int z = 0; z < 8; ++z) {
+                                const float x = ex2(fmaf(__uint_as_float(v[16 * g + 2 * z]), g == 0 ? f0 : f1, g == 0 ? off0 : off1));
+                                const float y = ex2(fmaf(__uint_as_float(v[16 * g + 2 * z + 1]), g == 0 ? f0 : f1, g == 0 ? off0 : off1));
+                                sums[z & 3] += x + y;
+                                const __half2 w2 = __floats2half2_rn(x, y);
+                                p[8 * g + z] = *reinterpret_cast<const uint32_t*>(&w2);
+                            }
+                            l = fmaf((sums[0] + sums[1]) + (sums[2] + sums[3]), g == 0 ? sc0.z : sc1.z, l);
                         }
-                        tmem_st<8>(s_at + g * 8, p);
+                    } else {
+#pragma unroll
+                        for (int z = 0; z < 16; ++z) p[z] = 0;
                     }
+                    tmem_st<16>(s_at + b * kStepKeys, p);
                     tmem_wait_st();
                     tc_fence_before();
-                    mbar_arrive(bar(&ctrl.p_full[t]));
+                    mbar_arrive(bar(&ctrl.p_full[t][b]));
                 }
             }
             tiles += n;
@@ -414,8 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (u.n >= 0 && takes_part(u)) begin_unit(u);
             if (!part) continue;
             if (n > 0) {
-                wait_bar(bar(&ctrl.o_full[t]), (uint32_t)finished & 1u, abort_flag, a.dev_status);
-                ++finished;
+                wait_bar(bar(&ctrl.o_done[t][(own - 1) & 1]), (uint32_t)((own - 1) >> 1) & 1u, abort_flag, a.dev_status);
                 __syncwarp();
                 tc_fence_after();
             }
@@ -519,40 +529,45 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ============================================================ MMAs
         const bool leader = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
-        constexpr uint32_t idesc_s = idesc_f16_f32(kTileRows, kKeys, 0), idesc_o = idesc_f16_f32(kTileRows, kDim, 1);
+        constexpr uint32_t idesc_s = idesc_f16_f32(kTileRows, kStepKeys, 0), idesc_o = idesc_f16_f32(kTileRows, kDim, 1);
         constexpr uint32_t kL128 = swizzle_layout_type(Swizzle::B128);
         const uint64_t q_desc = smem_desc(base + kQAt, 16, 1024, kL128), k_desc = smem_desc(base + kKAt, 16, 1024, kL128);
         const uint64_t v_desc = smem_desc(base + kVAt, kOperandBytes / 2, 1024, kL128);      // 64 elements a group, 8 keys a group
         bool live = true;
-        int units0 = 0, units1 = 0, weights0 = 0, weights1 = 0;      // of each tile of rows: units with keys, weights waited for
-        int tiles = 0;
-        auto issue_s = [&](int t, int kt, bool last) {
+        int units0 = 0, units1 = 0, begun0 = 0, begun1 = 0;          // of each tile of rows: units with keys, steps of earlier units
+        int tiles = 0, steps = 0;
+        bool two = false;
+        // S and O of step i of the unit; the last tile of rows gives back what the step is the last to read
+        auto issue_s = [&](int t, int i) {
+            const int kt = tiles + (i >> 1), b = ((t == 0 ? begun0 : begun1) + i) & 1;
             if (leader && live) {
-                const uint64_t qa = (uint64_t)(t * (kOperandBytes >> 4)), ka = (uint64_t)((kt & 1) * (kOperandBytes >> 4));
+                const uint64_t qa = (uint64_t)(t * (kOperandBytes >> 4)), ka = (uint64_t)((kt & 1) * (kOperandBytes >> 4) + (i & 1) * (kStepKeys * 128 >> 4));
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {         // 16 elements a step, 64 a part
                     const uint64_t off = (uint64_t)((j >> 2) * (kOperandBytes / 2 >> 4) + (j & 3) * 2);
-                    umma_bf16(tm + (uint32_t)(t * 128), q_desc + qa + off, k_desc + ka + off, idesc_s, j > 0);
+                    umma_bf16(tm + (uint32_t)(t * 128 + b * kStepKeys), q_desc + qa + off, k_desc + ka + off, idesc_s, j > 0);
                 }
-                umma_commit(bar(&ctrl.s_full[t]));
-                if (last) umma_commit(bar(&ctrl.k_empty[kt & 1]));
+                umma_commit(bar(&ctrl.s_full[t][b]));
+                if (t == (int)two && ((i & 1) || i + 1 == steps)) umma_commit(bar(&ctrl.k_empty[kt & 1]));
             }
             __syncwarp();
         };
-        auto issue_o = [&](int t, int kt, bool begins, bool ends, bool last) {
-            live = wait_bar(bar(&ctrl.p_full[t]), (uint32_t)(t == 0 ? weights0++ : weights1++) & 1u, abort_flag, a.dev_status) && live;
-            live = wait_bar(bar(&ctrl.v_full[kt & 1]), (uint32_t)(kt >> 1) & 1u, abort_flag, a.dev_status) && live;
+        auto issue_o = [&](int t, int i) {
+            const int kt = tiles + (i >> 1), own = (t == 0 ? begun0 : begun1) + i, b = own & 1;
+            live = wait_bar(bar(&ctrl.p_full[t][b]), (uint32_t)(own >> 1) & 1u, abort_flag, a.dev_status) && live;
+            if ((i & 1) == 0) live = wait_bar(bar(&ctrl.v_full[kt & 1]), (uint32_t)(kt >> 1) & 1u, abort_flag, a.dev_status) && live;
             tc_fence_after();
             if (leader && live) {
-                const uint64_t va = (uint64_t)((kt & 1) * (kOperandBytes >> 4));
+                const uint64_t va = (uint64_t)((kt & 1) * (kOperandBytes >> 4) + (i & 1) * (kStepKeys * 128 >> 4));
 #pragma unroll
-                for (int j = 0; j < 8; ++j)           // 16 keys a step: two groups of 8 lines
-                    umma_bf16_ts(tm + kOCol + (uint32_t)(t * 128), tm + (uint32_t)(t * 128 + (j >> 2) * 64 + (j & 3) * 8), v_desc + va + j * (2048 >> 4), idesc_o, !begins || j > 0);
-                if (last) {
+                for (int j = 0; j < 4; ++j)           // 16 keys a step: two groups of 8 lines
+                    umma_bf16_ts(tm + kOCol + (uint32_t)(t * 128), tm + (uint32_t)(t * 128 + b * kStepKeys + (j >> 1) * 32 + (j & 1) * 8), v_desc + va + j * (2048 >> 4),
+                                 idesc_o, i > 0 || j > 0);
+                umma_commit(bar(&ctrl.o_done[t][b]));
+                if (t == (int)two && ((i & 1) || i + 1 == steps)) {
                     umma_commit(bar(&ctrl.v_empty[kt & 1]));
                     umma_commit(bar(&ctrl.tile_empty[kt % kTileQueue]));
                 }
-                if (ends) umma_commit(bar(&ctrl.o_full[t]));
             }
             __syncwarp();
         };
@@ -562,27 +577,28 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         for (int z = 0; live; ++z) {
             const UnitInfo u = unit(z);
-            const int n = u.n;
-            if (n < 0) break;
-            if (n == 0) continue;
-            const bool two = u.n_rows > kTileRows;
+            if (u.n < 0) break;
+            if (u.n == 0) continue;
+            steps = u.steps, two = u.n_rows > kTileRows;
             for (int t = 0; t < 1 + (int)two; ++t) {
                 live = wait_bar(bar(&ctrl.q_full[t]), (uint32_t)(t == 0 ? units0++ : units1++) & 1u, abort_flag, a.dev_status) && live;
                 if (t == 0) wait_k(tiles);
                 tc_fence_after();
-                issue_s(t, tiles, t == (int)two);
+                issue_s(t, 0);
+                if (steps > 1) issue_s(t, 1);
             }
-            for (int i = 0; i < n && live; ++i) {
-                const int kt = tiles + i;
-                const bool ends = i + 1 == n;
-                issue_o(0, kt, i == 0, ends, !two);
-                if (!ends) wait_k(kt + 1), issue_s(0, kt + 1, !two);
-                if (two) {
-                    issue_o(1, kt, i == 0, ends, true);
-                    if (!ends) issue_s(1, kt + 1, true);
+            for (int i = 0; i < steps && live; ++i) {
+                for (int t = 0; t < 1 + (int)two; ++t) {
+                    issue_o(t, i);
+                    if (i + 2 < steps) {
+                        if (t == 0 && (i & 1) == 0) wait_k(tiles + (i >> 1) + 1);
+                        issue_s(t, i + 2);
+                    }
                 }
             }
-            tiles += n;
+            tiles += u.n;
+            begun0 += steps;
+            if (two) begun1 += steps;
         }
         if (leader) umma_commit(bar(&ctrl.drained));  // nothing of the tensor cores' is in flight when TMEM and shared memory are given up
         const long long c0 = clock64();
@@ -625,6 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             info.row0 = u.sq.row0, info.first_pos = u.sq.first_pos(), info.len = u.sq.len;
             info.tile_row = u.tile_row, info.n_rows = u.n_rows, info.head = u.head;
             info.key0 = u.lo + u.u0 * kKeys, info.n = max(u.u1 - u.u0, 0);
+            info.steps = 2 * info.n - (info.n > 0 && u.lo + u.u1 * kKeys - kStepKeys >= u.hi_max ? 1 : 0);
             info.slot = whole ? -1 : 2 * (int)blockIdx.x + (begins ? 1 : 0);
             push_unit(info);
             // lanes hold 32 sixteens of keys: four tiles
