@@ -156,6 +156,30 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, int b_mn_majo
     return (1u << 4) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// two sums, two products and sums in one instruction each
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 A, B, C;\n\tmov.b64 A, {%2, %3};\n\tmov.b64 B, {%4, %5};\n\tadd.rn.f32x2 C, A, B;\n\tmov.b64 {%0, %1}, C;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 A, B, C, D;\n\tmov.b64 A, {%2, %3};\n\tmov.b64 B, {%4, %5};\n\tmov.b64 C, {%6, %7};\n\tfma.rn.f32x2 D, A, B, C;\n\tmov.b64 {%0, %1}, D;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+
 // 16 codes of element chunk c (of 16) of line r of a [2][128][64] fp16 operand with 128-byte swizzle
 __device__ __forceinline__ void store_codes_f16(uint8_t* operand, int r, int c, uint4 w)
 {
@@ -326,15 +350,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const int kt = tiles + (i >> 1), b = own & 1;
                     const uint32_t parity = (uint32_t)(own >> 1) & 1u;
                     wait_bar(bar(&ctrl.s_full[t][b]), parity, abort_flag, a.dev_status);
+                    __syncwarp();
+                    tc_fence_after();
+                    uint32_t v[32];
+                    tmem_ld_x32(s_at + b * kStepKeys, v);
                     // for the scales and what is known of V (its place is not filled again before this thread has handed over its weights, so that this
                     // phase cannot be missed)
                     if ((i & 1) == 0) wait_bar(bar(&ctrl.v_full[kt & 1]), (uint32_t)(kt >> 1) & 1u, abort_flag, a.dev_status);
                     // (done before S of this step; waited for so that no phase is missed)
                     if (own >= 2) wait_bar(bar(&ctrl.o_done[t][b]), parity ^ 1u, abort_flag, a.dev_status);
                     __syncwarp();
-                    tc_fence_after();
-                    uint32_t v[32];
-                    tmem_ld_x32(s_at + b * kStepKeys, v);
                     const KeyTile& tile = s_tiles[kt % kTileQueue];
                     const int at = (i & 1) * kStepKeys + half * 32;      // this thread's 32 keys of the tile
                     const float4* scales = tile.scale + (at >> 4);
@@ -359,11 +384,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                     // ---- the largest exponent (a factor is never 0: a hidden score is -infinity times it)
                     const float f0 = fmaxf(rowf * sc0.x, 1.17549435e-38f), f1 = fmaxf(rowf * sc1.x, 1.17549435e-38f);
                     auto top_of = [](const uint32_t* w) {
-                        float tops[4];
+                        float x = max3(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]));
+                        float y = max3(__uint_as_float(w[3]), __uint_as_float(w[4]), __uint_as_float(w[5]));
 #pragma unroll
-                        for (int z = 0; z < 4; ++z)
-                            tops[z] = fmaxf(fmaxf(__uint_as_float(w[z]), __uint_as_float(w[z + 4])), fmaxf(__uint_as_float(w[z + 8]), __uint_as_float(w[z + 12])));
-                        return fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                        for (int z = 6; z < 14; z += 4) {
+                            x = max3(x, __uint_as_float(w[z]), __uint_as_float(w[z + 1]));
+                            y = max3(y, __uint_as_float(w[z + 2]), __uint_as_float(w[z + 3]));
+                        }
+                        return fmaxf(max3(x, __uint_as_float(w[14]), __uint_as_float(w[15])), y);
                     };
                     float top = -INFINITY;
                     if (seen) top = fmaxf(fmaf(top_of(v), f0, sc0.y), fmaf(top_of(v + 16), f1, sc1.y));
@@ -393,19 +421,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                     // ---- the weights, two to a column, over scores that have been read
                     uint32_t p[16];
                     if (seen) {
-                        const float off0 = sc0.y - m, off1 = sc1.y - m;
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
-                            float sums[4] = {};
+                            const float f = g == 0 ? f0 : f1, off = (g == 0 ? sc0.y : sc1.y) - m;
+                            float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
                             for (int z = 0; z < 8; ++z) {
-                                const float x = ex2(fmaf(__uint_as_float(v[16 * g + 2 * z]), g == 0 ? f0 : f1, g == 0 ? off0 : off1));
-                                const float y = ex2(fmaf(__uint_as_float(v[16 * g + 2 * z + 1]), g == 0 ? f0 : f1, g == 0 ? off0 : off1));
-                                sums[z & 3] += x + y;
-                                const __half2 w2 = __floats2half2_rn(x, y);
+                                float2 x = make_float2(__uint_as_float(v[16 * g + 2 * z]), __uint_as_float(v[16 * g + 2 * z + 1]));
+                                x = fma2(x, make_float2(f, f), make_float2(off, off));
+                                x = make_float2(ex2(x.x), ex2(x.y));
+                                sum = add2(sum, x);
+                                const __half2 w2 = __floats2half2_rn(x.x, x.y);
                                 p[8 * g + z] = *reinterpret_cast<const uint32_t*>(&w2);
                             }
-                            l = fmaf((sums[0] + sums[1]) + (sums[2] + sums[3]), g == 0 ? sc0.z : sc1.z, l);
+                            l = fmaf(sum.x + sum.y, g == 0 ? sc0.z : sc1.z, l);
                         }
                     } else {
 #pragma unroll
