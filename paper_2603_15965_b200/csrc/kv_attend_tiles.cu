@@ -22,8 +22,8 @@ namespace molora {
 namespace {
 
 constexpr int kDim = 128, kKeys = 128, kStepKeys = 64, kTileRows = 128, kUnitRows = 256;
-constexpr int kThreads = 768;                                 // (the last two warps only make a warpgroup of four)
-constexpr int kConvWarp0 = 16, kMmaWarp = 20, kWalkWarp = 21;
+constexpr int kThreads = 768;                                 // (the last warp only makes a warpgroup of four)
+constexpr int kConvWarp0 = 16, kMmaWarp0 = 20, kMmaWarp1 = 21, kWalkWarp = 22;      // an MMA warp for each tile of rows
 // Registers: the converting warps hold 64 words of codes, which the last four give up (6 x 128 threads, 80 registers each at launch)
 constexpr int kConvRegs = 104, kOtherRegs = 56;
 static_assert(kConvRegs + kOtherRegs <= 2 * 80, "register split");
@@ -38,11 +38,11 @@ constexpr float kTop = 7.f, kSlack = 8.f;                     // a row's largest
 struct Control {
     uint64_t s_full[2][2], p_full[2][2], o_done[2][2];         // of each tile of rows, for even and odd steps of it
     uint64_t q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2];
-    uint64_t tile_full[kTileQueue], tile_empty[kTileQueue], unit_full[kUnitQueue], unit_empty[kUnitQueue], drained;
+    uint64_t tile_full[kTileQueue], tile_empty[kTileQueue], unit_full[kUnitQueue], unit_empty[kUnitQueue], drained[2];
     uint32_t tmem_base;
     int abort_flag;
 };
-constexpr int kUnitReaders = kConvWarp0 + 1;                  // the warps of rows, the MMAs'
+constexpr int kUnitReaders = kConvWarp0 + 2;                  // the warps of rows, those of the MMAs
 
 // A tile of keys in the queue.
 struct KeyTile {
@@ -216,16 +216,16 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int z = 0; z < 2; ++z)
                 mbar_init(bar(&ctrl.s_full[i][z]), 1), mbar_init(bar(&ctrl.p_full[i][z]), 2 * kTileRows), mbar_init(bar(&ctrl.o_done[i][z]), 1);
             mbar_init(bar(&ctrl.q_full[i]), 8);
-            mbar_init(bar(&ctrl.k_full[i]), 128), mbar_init(bar(&ctrl.k_empty[i]), 1);
-            mbar_init(bar(&ctrl.v_full[i]), 128), mbar_init(bar(&ctrl.v_empty[i]), 1);
+            mbar_init(bar(&ctrl.k_full[i]), 128), mbar_init(bar(&ctrl.k_empty[i]), 2);
+            mbar_init(bar(&ctrl.v_full[i]), 128), mbar_init(bar(&ctrl.v_empty[i]), 2);
+            mbar_init(bar(&ctrl.drained[i]), 1);
         }
-        for (int i = 0; i < kTileQueue; ++i) mbar_init(bar(&ctrl.tile_full[i]), 1), mbar_init(bar(&ctrl.tile_empty[i]), 1);
+        for (int i = 0; i < kTileQueue; ++i) mbar_init(bar(&ctrl.tile_full[i]), 1), mbar_init(bar(&ctrl.tile_empty[i]), 2);
         for (int i = 0; i < kUnitQueue; ++i) mbar_init(bar(&ctrl.unit_full[i]), 1), mbar_init(bar(&ctrl.unit_empty[i]), kUnitReaders);
-        mbar_init(bar(&ctrl.drained), 1);
         ctrl.abort_flag = 0;
         fence_mbar_init();
     }
-    if (warp == kMmaWarp) {
+    if (warp == kMmaWarp0) {
         tmem_alloc(smem_u32(&ctrl.tmem_base), kTmemCols);
         tmem_relinquish();
     }
@@ -495,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             pair_sync();                              // (s_pair is free again)
         }
-    } else if (warp < kMmaWarp) {
+    } else if (warp < kMmaWarp0) {
         // ============================================================ codes -> fp16
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConvRegs));
         const int ct = tid - kConvWarp0 * 32, chunk = ct & 7, r0 = ct >> 3;      // chunk of 16 elements, lines r0 + 16 j
@@ -554,46 +554,46 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-      if (warp == kMmaWarp) {
-        // ============================================================ MMAs
+      if (warp == kMmaWarp0 || warp == kMmaWarp1) {
+        // ============================================================ MMAs of a tile of rows
         const bool leader = elect_one();
-        const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+        const int t = warp - kMmaWarp0;
+        const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0), s_col = tm + (uint32_t)(t * 128), o_col = tm + kOCol + (uint32_t)(t * 128);
         constexpr uint32_t idesc_s = idesc_f16_f32(kTileRows, kStepKeys, 0), idesc_o = idesc_f16_f32(kTileRows, kDim, 1);
         constexpr uint32_t kL128 = swizzle_layout_type(Swizzle::B128);
-        const uint64_t q_desc = smem_desc(base + kQAt, 16, 1024, kL128), k_desc = smem_desc(base + kKAt, 16, 1024, kL128);
+        const uint64_t q_desc = smem_desc(base + kQAt + t * kOperandBytes, 16, 1024, kL128), k_desc = smem_desc(base + kKAt, 16, 1024, kL128);
         const uint64_t v_desc = smem_desc(base + kVAt, kOperandBytes / 2, 1024, kL128);      // 64 elements a group, 8 keys a group
         bool live = true;
-        int units0 = 0, units1 = 0, begun0 = 0, begun1 = 0;          // of each tile of rows: units with keys, steps of earlier units
-        int tiles = 0, steps = 0;
-        bool two = false;
-        // S and O of step i of the unit; the last tile of rows gives back what the step is the last to read
-        auto issue_s = [&](int t, int i) {
-            const int kt = tiles + (i >> 1), b = ((t == 0 ? begun0 : begun1) + i) & 1;
+        int units = 0, begun = 0, tiles = 0, steps = 0;              // units with rows here, steps of earlier ones; tiles of keys; steps of the unit
+        // S and O of step i of the unit; the last step of a tile gives back what was read
+        auto issue_s = [&](int i) {
+            const int kt = tiles + (i >> 1), b = (begun + i) & 1;
             if (leader && live) {
-                const uint64_t qa = (uint64_t)(t * (kOperandBytes >> 4)), ka = (uint64_t)((kt & 1) * (kOperandBytes >> 4) + (i & 1) * (kStepKeys * 128 >> 4));
+                const uint64_t ka = k_desc + (uint64_t)((kt & 1) * (kOperandBytes >> 4) + (i & 1) * (kStepKeys * 128 >> 4));
+                const uint32_t d = s_col + (uint32_t)(b * kStepKeys);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {         // 16 elements a step, 64 a part
                     const uint64_t off = (uint64_t)((j >> 2) * (kOperandBytes / 2 >> 4) + (j & 3) * 2);
-                    umma_bf16(tm + (uint32_t)(t * 128 + b * kStepKeys), q_desc + qa + off, k_desc + ka + off, idesc_s, j > 0);
+                    umma_bf16(d, q_desc + off, ka + off, idesc_s, j > 0);
                 }
                 umma_commit(bar(&ctrl.s_full[t][b]));
-                if (t == (int)two && ((i & 1) || i + 1 == steps)) umma_commit(bar(&ctrl.k_empty[kt & 1]));
+                if ((i & 1) || i + 1 == steps) umma_commit(bar(&ctrl.k_empty[kt & 1]));
             }
             __syncwarp();
         };
-        auto issue_o = [&](int t, int i) {
-            const int kt = tiles + (i >> 1), own = (t == 0 ? begun0 : begun1) + i, b = own & 1;
+        auto issue_o = [&](int i) {
+            const int kt = tiles + (i >> 1), own = begun + i, b = own & 1;
             live = wait_bar(bar(&ctrl.p_full[t][b]), (uint32_t)(own >> 1) & 1u, abort_flag, a.dev_status) && live;
             if ((i & 1) == 0) live = wait_bar(bar(&ctrl.v_full[kt & 1]), (uint32_t)(kt >> 1) & 1u, abort_flag, a.dev_status) && live;
             tc_fence_after();
             if (leader && live) {
-                const uint64_t va = (uint64_t)((kt & 1) * (kOperandBytes >> 4) + (i & 1) * (kStepKeys * 128 >> 4));
+                const uint64_t va = v_desc + (uint64_t)((kt & 1) * (kOperandBytes >> 4) + (i & 1) * (kStepKeys * 128 >> 4));
+                const uint32_t p = s_col + (uint32_t)(b * kStepKeys);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)           // 16 keys a step: two groups of 8 lines
-                    umma_bf16_ts(tm + kOCol + (uint32_t)(t * 128), tm + (uint32_t)(t * 128 + b * kStepKeys + (j >> 1) * 32 + (j & 1) * 8), v_desc + va + j * (2048 >> 4),
-                                 idesc_o, i > 0 || j > 0);
+                    umma_bf16_ts(o_col, p + (j >> 1) * 32 + (j & 1) * 8, va + j * (2048 >> 4), idesc_o, i > 0 || j > 0);
                 umma_commit(bar(&ctrl.o_done[t][b]));
-                if (t == (int)two && ((i & 1) || i + 1 == steps)) {
+                if ((i & 1) || i + 1 == steps) {
                     umma_commit(bar(&ctrl.v_empty[kt & 1]));
                     umma_commit(bar(&ctrl.tile_empty[kt % kTileQueue]));
                 }
@@ -608,30 +608,35 @@ __global__ void __launch_bounds__(kThreads, 1)
             const UnitInfo u = unit(z);
             if (u.n < 0) break;
             if (u.n == 0) continue;
-            steps = u.steps, two = u.n_rows > kTileRows;
-            for (int t = 0; t < 1 + (int)two; ++t) {
-                live = wait_bar(bar(&ctrl.q_full[t]), (uint32_t)(t == 0 ? units0++ : units1++) & 1u, abort_flag, a.dev_status) && live;
-                if (t == 0) wait_k(tiles);
-                tc_fence_after();
-                issue_s(t, 0);
-                if (steps > 1) issue_s(t, 1);
+            steps = u.steps;
+            if (t * kTileRows >= u.n_rows) {          // no rows here: the tiles are given back as they come
+                for (int i = 0; i < u.n && live; ++i) {
+                    const int kt = tiles + i;
+                    wait_k(kt);
+                    live = wait_bar(bar(&ctrl.v_full[kt & 1]), (uint32_t)(kt >> 1) & 1u, abort_flag, a.dev_status) && live;
+                    if (leader && live) mbar_arrive(bar(&ctrl.k_empty[kt & 1])), mbar_arrive(bar(&ctrl.v_empty[kt & 1])), mbar_arrive(bar(&ctrl.tile_empty[kt % kTileQueue]));
+                    __syncwarp();
+                }
+                tiles += u.n;
+                continue;
             }
+            live = wait_bar(bar(&ctrl.q_full[t]), (uint32_t)(units++) & 1u, abort_flag, a.dev_status) && live;
+            wait_k(tiles);
+            issue_s(0);
+            if (steps > 1) issue_s(1);
             for (int i = 0; i < steps && live; ++i) {
-                for (int t = 0; t < 1 + (int)two; ++t) {
-                    issue_o(t, i);
-                    if (i + 2 < steps) {
-                        if (t == 0 && (i & 1) == 0) wait_k(tiles + (i >> 1) + 1);
-                        issue_s(t, i + 2);
-                    }
+                issue_o(i);
+                if (i + 2 < steps) {
+                    if ((i & 1) == 0) wait_k(tiles + (i >> 1) + 1);
+                    issue_s(i + 2);
                 }
             }
             tiles += u.n;
-            begun0 += steps;
-            if (two) begun1 += steps;
+            begun += steps;
         }
-        if (leader) umma_commit(bar(&ctrl.drained));  // nothing of the tensor cores' is in flight when TMEM and shared memory are given up
+        if (leader) umma_commit(bar(&ctrl.drained[t]));   // nothing of the tensor cores' is in flight when TMEM and shared memory are given up
         const long long c0 = clock64();
-        while (!mbar_try_wait(bar(&ctrl.drained), 0))
+        while (!mbar_try_wait(bar(&ctrl.drained[t]), 0))
             if (clock64() - c0 > kTimeoutCycles) break;
         __syncwarp();
       } else if (warp == kWalkWarp) {
@@ -719,7 +724,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == kMmaWarp) tmem_dealloc(tmem, kTmemCols);
+    if (warp == kMmaWarp0) tmem_dealloc(tmem, kTmemCols);
 }
 
 int64_t share_count() { return sm_count(); }
