@@ -56,7 +56,7 @@ struct Cfg {
     static_assert(kStages <= kMaxStages, "stages");
 };
 
-// A thread that waits for a phase by its parity must have seen the phase before it.  Hence barriers of their own where a role does not look
+// A warp arrives as one: arrivals of single threads at a barrier follow one another.  A thread that waits for a phase by its parity must have seen the phase before it.  Hence barriers of their own where a role does not look
 // at every phase: s_full for the tiles of each set, q_ready (for the MMAs) beside q_full, since units without tiles pass the MMAs by.
 struct Control {
     uint64_t full[kMaxStages], empty[kMaxStages];
@@ -151,10 +151,10 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
         prefetch_tensormap(&tm_v);
         for (int s = 0; s < C::kStages; ++s) mbar_init(bar(&ctrl.full[s]), 1), mbar_init(bar(&ctrl.empty[s]), 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(&ctrl.s_full[0][i]), 1), mbar_init(bar(&ctrl.s_full[1][i]), 1), mbar_init(bar(&ctrl.s_empty[i]), C::kKeyThreads);
-            mbar_init(bar(&ctrl.p_full[i]), C::kKeyThreads), mbar_init(bar(&ctrl.p_empty[i]), 1);
-            mbar_init(bar(&ctrl.q_full[i]), 1), mbar_init(bar(&ctrl.q_ready[i]), 1), mbar_init(bar(&ctrl.q_empty[i]), C::kKeyThreads);
-            mbar_init(bar(&ctrl.o_empty[i]), C::kKeyThreads);
+            mbar_init(bar(&ctrl.s_full[0][i]), 1), mbar_init(bar(&ctrl.s_full[1][i]), 1), mbar_init(bar(&ctrl.s_empty[i]), C::kKeyThreads / 32);
+            mbar_init(bar(&ctrl.p_full[i]), C::kKeyThreads / 32), mbar_init(bar(&ctrl.p_empty[i]), 1);
+            mbar_init(bar(&ctrl.q_full[i]), 1), mbar_init(bar(&ctrl.q_ready[i]), 1), mbar_init(bar(&ctrl.q_empty[i]), C::kKeyThreads / 32);
+            mbar_init(bar(&ctrl.o_empty[i]), C::kKeyThreads / 32);
         }
         mbar_init(bar(&ctrl.drained), 1);
         ctrl.abort_flag = 0;
@@ -443,7 +443,8 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                     for (int r = 0; r < RPG; ++r) y[r] = fmaf(__uint_as_float(v1[r]), 1.f / kTermStep, __uint_as_float(v0[r]));
                 }
                 tc_fence_before();
-                mbar_arrive(bar(&ctrl.s_empty[b]));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&ctrl.s_empty[b]));
                 const int key = key0 + key_lane;
                 const bool border = key0 + kKeys > hi_min || key0 < lo_max;
                 // y: the logarithm of what the key contributes to the row, over the row's reference
@@ -538,7 +539,8 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 }
                 fence_proxy_async_smem();
                 tc_fence_before();
-                mbar_arrive(bar(&ctrl.p_full[b]));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&ctrl.p_full[b]));
             }
             // ---- the unit's result, or a piece of it: an element per thread
 #pragma unroll
@@ -565,7 +567,8 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                     for (int r = 0; r < RPG; ++r) o[r] = fmaf(__uint_as_float(v[r]), f, o[r]);
                 }
                 tc_fence_before();
-                mbar_arrive(bar(&ctrl.o_empty[set]));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(&ctrl.o_empty[set]));
             }
             const bool live = *abort_flag == 0;       // (nothing of an aborted call is stored)
             sync_threads_of<128>(1 + all);
@@ -584,7 +587,8 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                     if (key_lane == 0) slot[row] = m[r], slot[ROWS + row] = sum;
                 }
             }
-            mbar_arrive(bar(&ctrl.q_empty[k & 1]));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(&ctrl.q_empty[k & 1]));
             sync_threads_of<128>(1 + all);             // (s_part)
         }
     }

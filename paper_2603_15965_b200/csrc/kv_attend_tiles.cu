@@ -35,6 +35,7 @@ constexpr int kTileQueue = 8, kUnitQueue = 4;
 constexpr int kUnitCost = 3, kMinShare = 4;                   // tiles of keys
 constexpr float kTop = 7.f, kSlack = 8.f;                     // a row's largest weight when its reference is set, and by how much it may grow: fp16
 
+// (a warp arrives as one: arrivals of single threads at a barrier follow one another, 256 of them cost a step as much as its weights)
 struct Control {
     uint64_t s_full[2][2], p_full[2][2], o_done[2][2];         // of each tile of rows, for even and odd steps of it
     uint64_t q_full[2], k_full[2], k_empty[2], v_full[2], v_empty[2];
@@ -214,10 +215,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             for (int z = 0; z < 2; ++z)
-                mbar_init(bar(&ctrl.s_full[i][z]), 1), mbar_init(bar(&ctrl.p_full[i][z]), 2 * kTileRows), mbar_init(bar(&ctrl.o_done[i][z]), 1);
+                mbar_init(bar(&ctrl.s_full[i][z]), 1), mbar_init(bar(&ctrl.p_full[i][z]), 8), mbar_init(bar(&ctrl.o_done[i][z]), 1);
             mbar_init(bar(&ctrl.q_full[i]), 8);
-            mbar_init(bar(&ctrl.k_full[i]), 128), mbar_init(bar(&ctrl.k_empty[i]), 2);
-            mbar_init(bar(&ctrl.v_full[i]), 128), mbar_init(bar(&ctrl.v_empty[i]), 2);
+            mbar_init(bar(&ctrl.k_full[i]), 4), mbar_init(bar(&ctrl.k_empty[i]), 2);
+            mbar_init(bar(&ctrl.v_full[i]), 4), mbar_init(bar(&ctrl.v_empty[i]), 2);
             mbar_init(bar(&ctrl.drained[i]), 1);
         }
         for (int i = 0; i < kTileQueue; ++i) mbar_init(bar(&ctrl.tile_full[i]), 1), mbar_init(bar(&ctrl.tile_empty[i]), 2);
@@ -443,7 +444,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tmem_st<16>(s_at + b * kStepKeys, p);
                     tmem_wait_st();
                     tc_fence_before();
-                    mbar_arrive(bar(&ctrl.p_full[t][b]));
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(&ctrl.p_full[t][b]));
                 }
             }
             tiles += n;
@@ -524,7 +526,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int j = 0; j < 8; ++j) store_codes_f16(smem + kKAt + st * kOperandBytes, 16 * j + r0, chunk, k[j]);
             fence_proxy_async_smem();
-            mbar_arrive(bar(&ctrl.k_full[st]));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(&ctrl.k_full[st]));
             more = there(kt + 1);
             if (more) load(next, a.c.k, k);
             if (tile.kind == 1) {
@@ -549,7 +552,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int j = 0; j < 8; ++j) store_codes_f16(smem + kVAt + st * kOperandBytes, 16 * j + r0, chunk, v[j]);
             fence_proxy_async_smem();
-            mbar_arrive(bar(&ctrl.v_full[st]));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(&ctrl.v_full[st]));
             if (more) load(next, a.c.v, v);
         }
     } else {
