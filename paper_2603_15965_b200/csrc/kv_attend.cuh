@@ -37,6 +37,13 @@ __device__ __forceinline__ Span span_of(const Sequence& s, int group, int window
     r.tiles = (int32_t)(((int64_t)s.n * group + ROWS - 1) / ROWS);
     return r;
 }
+// steps of all units of a sequence
+template <int ROWS, int KEYS, int COST>
+__device__ __forceinline__ int64_t steps_of(const AttendArgs& a, const Sequence& s, int group)
+{
+    const Span sp = span_of<ROWS, KEYS, COST>(s, group, a.window);
+    return (int64_t)sp.steps * sp.tiles * a.c.kv_heads;
+}
 
 // A unit, and what of its keys lies in this share.
 struct Unit {
@@ -57,13 +64,24 @@ __device__ __forceinline__ int lower_key(const AttendArgs& a, const Sequence& sq
     return a.window > 0 ? max(0, sq.first_pos() + token - a.window + 1) : 0;
 }
 
+// a / b of numbers that are not negative; most a are below 2^32, where it is a fifth of the instructions
+__device__ __forceinline__ int64_t quotient(int64_t a, int32_t b)
+{
+    return (uint64_t)a >> 32 == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// Where a share begins: which part of the sequences (see cut_shares), the first step of it, how many steps there are and how many a share has.
+struct ShareStart {
+    int64_t base, total, share;
+    int32_t part;
+};
+
 // The units of a share, in order; every thread (or warp) that asks gets the same.
 template <int ROWS, int KEYS, int COST>
 struct Walk {
     const AttendArgs& a;
     int64_t at, stop, base;                 // next step, end of the share, first step of sequence b
-    const int64_t* s_upto = nullptr;
-    int64_t total = 0, share = 1;           // steps of all units, and of a share
+    int64_t share = 1;
     int b, group;
     Sequence sq;
     Span sp;
@@ -82,11 +100,11 @@ struct Walk {
             ++b;
             load();
         }
-        const int64_t unit = (at - base) / sp.steps;
+        const int64_t unit = quotient(at - base, sp.steps);
         u.sq = sq, u.sp = sp, u.b = b;
         u.at = base + unit * sp.steps;
         u.first = (int)(at - u.at), u.last = (int)min((int64_t)sp.steps, stop - u.at);
-        u.head = (int)(unit % a.c.kv_heads), u.tile = (int)(unit / a.c.kv_heads);
+        u.tile = (int)quotient(unit, a.c.kv_heads), u.head = (int)(unit - (int64_t)u.tile * a.c.kv_heads);
         u.tile_row = u.tile * ROWS;
         u.n_rows = (int)min((int64_t)ROWS, (int64_t)sq.n * group - u.tile_row);
         at = u.at + u.last;
@@ -99,56 +117,55 @@ struct Walk {
     }
     // the shares in which the unit lies, from this one (w), where it begins, on
     __device__ int32_t pieces(const Unit& u, int64_t w) const { return (int32_t)((u.at + u.sp.steps - 1) / share - w + 1); }
-    // Puts the walk at the beginning of share w; `parts`: how many parts of the sequences s_upto counts.
-    __device__ void begin(int64_t w, int parts)
+    // Puts the walk at the beginning of share w; `parts`: into how many parts the sequences are divided.
+    __device__ void begin(const ShareStart& from, int64_t w, int parts)
     {
+        share = from.share;
         at = w * share;
-        stop = min(total, at + share);
+        stop = min(from.total, at + share);
         if (at >= stop) return;
-        int lo = 0, hi = parts - 1;         // the part in which the share begins
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (s_upto[mid] > at) hi = mid;
-            else lo = mid + 1;
-        }
-        b = lo * ((a.c.B + parts - 1) / parts);
-        base = lo > 0 ? s_upto[lo - 1] : 0;
+        b = from.part * ((a.c.B + parts - 1) / parts);
+        base = from.base;
         load();
     }
 };
 
-// Steps of the sequences up to the end of each thread's part of them, into s_upto (THREADS words); all THREADS threads of the CTA.
-template <int THREADS, int ROWS, int KEYS, int COST>
-__device__ __forceinline__ void count_steps(const AttendArgs& a, int64_t* s_upto)
+// Equal shares of all steps, none shorter than min_share: where the W shares from first_share on begin, into s_start.  All THREADS threads of
+// the CTA; each looks after a part of the sequences, steps_of tells the steps of one.
+template <int THREADS, int W, typename StepsOf>
+__device__ __forceinline__ void cut_shares(const AttendArgs& a, int64_t first_share, int64_t shares, int min_share, ShareStart* s_start, StepsOf steps_of)
 {
-    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, group = a.heads / a.c.kv_heads;
+    __shared__ int64_t s_warp[32];
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int part = (a.c.B + THREADS - 1) / THREADS;
-    int64_t incl = 0;
+    int64_t own = 0;
     for (int b = tid * part; b < min(a.c.B, (tid + 1) * part); ++b) {
         const Sequence sq = sequence_of(a.c, b, a.N);
-        const Span sp = span_of<ROWS, KEYS, COST>(sq, group, a.window);
-        incl += (int64_t)sp.steps * sp.tiles * a.c.kv_heads;
+        own += steps_of(sq);
         if (sq.bad && blockIdx.x == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
     }
+    auto scan = [lane](int64_t v) {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-        if (lane >= o) incl += up;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, v, o);
+            if (lane >= o) v += up;
+        }
+        return v;
+    };
+    int64_t upto = scan(own);
+    if (lane == 31) s_warp[warp] = upto;
+    __syncthreads();
+    const int64_t warps = scan(lane < THREADS / 32 ? s_warp[lane] : 0);
+    const int64_t before = __shfl_sync(0xFFFFFFFFu, warps, (warp - 1) & 31), total = __shfl_sync(0xFFFFFFFFu, warps, 31);
+    if (warp > 0) upto += before;
+    const int64_t share = max(quotient(total + shares - 1, (int32_t)shares), (int64_t)min_share);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        const int64_t at = (first_share + w) * share;
+        if (at >= upto - own && at < upto) s_start[w].base = upto - own, s_start[w].part = tid;
+        if (tid == 0) s_start[w].total = total, s_start[w].share = share;
     }
-    if (lane == 31) s_upto[tid] = incl;
     __syncthreads();
-    for (int z = 0; z < warp; ++z) incl += s_upto[32 * z + 31];
-    __syncthreads();
-    s_upto[tid] = incl;
-    __syncthreads();
-}
-// Equal shares of all steps, none shorter than min_share.
-template <int ROWS, int KEYS, int COST>
-__device__ __forceinline__ void cut_shares(Walk<ROWS, KEYS, COST>& walk, const int64_t* s_upto, int parts, int64_t shares, int min_share)
-{
-    walk.s_upto = s_upto;
-    walk.total = s_upto[parts - 1];
-    walk.share = max((walk.total + shares - 1) / shares, (int64_t)min_share);
 }
 
 // scales of v outside [2^-100, 2^100] are read as its ends

@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
     constexpr int kVBytes = D / 8;                      // of a value, per lane
     constexpr int kMT = D / 16;                         // 16-element tiles of the values
     constexpr bool kPairs = Sh::kPairs;
-    __shared__ int64_t s_upto[kThreads];                // steps of the sequences up to the end of thread i's part
+    __shared__ ShareStart s_start;
     __shared__ float4 s_scales[kWarpsPerCta][kStages][2];  // of a half: scale of K, logarithm and reciprocal of V's, whether its page can be used
     __shared__ float s_m[kWarpsPerCta][kRows], s_l[kWarpsPerCta][kRows];
     extern __shared__ __align__(16) uint8_t ring_all[];
@@ -123,9 +123,8 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
 
     const int64_t w = blockIdx.x;
     Walk<kRows, kStepKeys, kUnitCost> walk(a);
-    count_steps<kThreads, kRows, kStepKeys, kUnitCost>(a, s_upto);
-    cut_shares(walk, s_upto, kThreads, gridDim.x, kMinShare);
-    walk.begin(w, kThreads);
+    cut_shares<kThreads, 1>(a, w, gridDim.x, kMinShare, &s_start, [&](const Sequence& sq) { return steps_of<kRows, kStepKeys, kUnitCost>(a, sq, group); });
+    walk.begin(s_start, w, kThreads);
     CutUnit cut{0, 0, 0, 0};
     Unit un;
     while (walk.next(un)) {

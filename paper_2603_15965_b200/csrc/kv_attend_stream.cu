@@ -29,8 +29,8 @@ namespace molora {
 namespace {
 
 constexpr int kDim = 128, kKeys = 128;
-constexpr int kFirstGroupWarp = 4;
-constexpr int kMaxStages = 6;                // tiles in flight or in use
+constexpr int kRoleWarps = 4;                // of a worker: copies, MMAs, rows (two)
+constexpr int kMaxStages = 5;                // tiles in flight or in use
 constexpr int kTileBytes = kKeys * kDim, kStageBytes = 2 * kTileBytes;      // K, then V
 constexpr int kMinShare = 2;                 // tiles
 constexpr int kTermsQ = 2, kTermsP = 3;
@@ -40,31 +40,30 @@ constexpr float kNan = __builtin_nanf("");
 
 template <int ROWS>
 struct Cfg {
-    static constexpr int kRowsPerGroup = ROWS == 16 || ROWS == 32 ? 8 : 4, kGroups = ROWS / kRowsPerGroup;
-    static constexpr int kSets = ROWS <= 16 ? 2 : 1;                      // units in hand at a time
-    static constexpr int kUnitCost = kSets == 2 ? 2 : 4;                  // tiles that a unit's rows and results cost
-    static constexpr int kKeyThreads = 128 * kGroups, kThreads = 32 * kFirstGroupWarp + kSets * kKeyThreads;      // (kKeyThreads: of a set)
+    static constexpr int kRowsPerGroup = ROWS >= 16 ? 8 : 4, kGroups = ROWS / kRowsPerGroup;
+    static constexpr int kWorkers = ROWS <= 24 ? 2 : 1;
+    static constexpr int kUnitCost = 2;                                   // tiles that a unit's rows and results cost
+    static constexpr int kKeyThreads = 128 * kGroups, kFirstGroupWarp = kRoleWarps * kWorkers;      // (kKeyThreads: of a worker)
+    static constexpr int kThreads = 32 * kFirstGroupWarp + kWorkers * kKeyThreads;
     static_assert(kThreads <= 1024, "threads");
     static constexpr int kNS = (kTermsQ * ROWS + 15) / 16 * 16;           // columns of S and of O: multiples of 16, the last ones unused
     static constexpr int kNP = (kTermsP * ROWS + 15) / 16 * 16;
     static constexpr int kQBytes = kNS / 8 * 1024, kPBytes = kNP / 8 * 1024;
-    static constexpr uint32_t kSCol1 = 64, kOCol = 128, kOSet = 64, kTmemCols = 256;  // S of odd tiles, O of each set
-    static_assert(kNS <= 64 && kNP <= (kSets == 2 ? 64 : 128), "TMEM columns");
-    static constexpr int kStages = ROWS <= 16 ? 6 : 5;
-    static constexpr int kQAt = kStages * kStageBytes, kPAt = kQAt + 2 * kQBytes;
-    static constexpr size_t kSmem = 1024 + (size_t)kPAt + 2 * kPBytes;
+    static constexpr uint32_t kSCol1 = 64, kOCol = 128, kWorkerCols = 256, kTmemCols = kWorkers * kWorkerCols;      // S of even tiles, of odd tiles, O
+    static_assert(kNS <= 64 && kNP <= 128, "TMEM columns");
+    static constexpr int kStages = kWorkers == 1 ? 5 : ROWS <= 16 ? 3 : 2;
+    static constexpr int kQAt = kStages * kStageBytes, kPAt = kQAt + 2 * kQBytes, kWorkerBytes = kPAt + kPBytes;
+    static constexpr size_t kSmem = 1024 + (size_t)kWorkers * kWorkerBytes;
     static_assert(kStages <= kMaxStages, "stages");
 };
 
-// A warp arrives as one: arrivals of single threads at a barrier follow one another.  A thread that waits for a phase by its parity must have seen the phase before it.  Hence barriers of their own where a role does not look
-// at every phase: s_full for the tiles of each set, q_ready (for the MMAs) beside q_full, since units without tiles pass the MMAs by.
+// A warp arrives as one: arrivals of single threads at a barrier follow one another.  A thread that waits for a phase by its parity must have seen
+// the phase before it; hence q_ready (for the MMAs) beside q_full, since units without tiles pass the MMAs by.
 struct Control {
     uint64_t full[kMaxStages], empty[kMaxStages];
-    uint64_t s_full[2][2], s_empty[2], p_full[2], p_empty[2], o_empty[2];
+    uint64_t s_full[2], s_empty[2], p_full, p_empty;
     uint64_t q_full[2], q_ready[2], q_empty[2];
     uint64_t drained;
-    uint32_t tmem_base;
-    int abort_flag;
 };
 // A tile in the ring: the scales of every 16 keys (of K, logarithm and reciprocal of V's, whether their page can be used), and where in its unit it
 // stands.
@@ -79,13 +78,13 @@ struct Rows {
     float factor[ROWS];                       // of a score: scale, powers of two
     int32_t lower[ROWS], upper[ROWS];         // keys that the row sees
     int64_t out[ROWS], lse[ROWS];             // places in out and lse
-    int32_t tile0, tiles;                     // its tiles; -1: there are no more units
+    int32_t tiles;                            // -1: there are no more units
     int32_t key0, n_rows;                     // first key of the first tile
     int32_t hi_min, hi_max, lo_min, lo_max;
     int32_t slot;                             // where a piece goes; -1: the unit is whole
 };
 
-// barriers of a group (1 + group) and of a set (14 + set)
+// barriers of a group (1 + group) and of a worker (14 + worker)
 template <int THREADS>
 __device__ __forceinline__ void sync_threads_of(int id) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "n"(THREADS) : "memory"); }
 template <int THREADS>
@@ -130,55 +129,70 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                          CutUnit* __restrict__ cuts, float* __restrict__ slots)
 {
     using C = Cfg<ROWS>;
-    constexpr int RPG = C::kRowsPerGroup;
+    constexpr int RPG = C::kRowsPerGroup, W = C::kWorkers;
     using namespace ptx;
-    __shared__ Control ctrl;
-    __shared__ int64_t s_upto[C::kThreads];
-    __shared__ Tile s_tiles[C::kStages];
-    __shared__ Rows<ROWS> s_rows[2];
-    __shared__ float s_part[C::kSets * C::kGroups][4][RPG];
+    __shared__ Control ctrls[W];
+    __shared__ uint32_t s_tmem_base;
+    __shared__ int s_abort;
+    __shared__ ShareStart s_start[W];
+    __shared__ Tile s_tiles_all[W][C::kStages];
+    __shared__ Rows<ROWS> s_rows_all[W][2];
+    __shared__ float s_part[W * C::kGroups][4][RPG];
     extern __shared__ uint8_t smem_raw[];
     const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    // which worker the warp belongs to
+    const int worker = warp < C::kFirstGroupWarp ? warp / kRoleWarps : (warp - C::kFirstGroupWarp) / (4 * C::kGroups);
+    const uint32_t raw = smem_u32(smem_raw), first = (raw + 1023u) & ~1023u, base = first + (uint32_t)(worker * C::kWorkerBytes);
     uint8_t* const smem = smem_raw + (base - raw);
     const uint32_t q_at = base + C::kQAt, p_at = base + C::kPAt;
-    volatile int* abort_flag = &ctrl.abort_flag;
+    volatile int* abort_flag = &s_abort;
+    Control& ctrl = ctrls[worker];
+    Tile* const s_tiles = s_tiles_all[worker];
+    Rows<ROWS>* const s_rows = s_rows_all[worker];
     auto bar = [](const uint64_t* b) { return smem_u32(b); };
 
     grid_dependency_wait();
-    if (tid == 0) {
-        prefetch_tensormap(&tm_k);
-        prefetch_tensormap(&tm_v);
-        for (int s = 0; s < C::kStages; ++s) mbar_init(bar(&ctrl.full[s]), 1), mbar_init(bar(&ctrl.empty[s]), 1);
+    if (tid < W) {
+        Control& c = ctrls[tid];
+        for (int s = 0; s < C::kStages; ++s) mbar_init(bar(&c.full[s]), 1), mbar_init(bar(&c.empty[s]), 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(&ctrl.s_full[0][i]), 1), mbar_init(bar(&ctrl.s_full[1][i]), 1), mbar_init(bar(&ctrl.s_empty[i]), C::kKeyThreads / 32);
-            mbar_init(bar(&ctrl.p_full[i]), C::kKeyThreads / 32), mbar_init(bar(&ctrl.p_empty[i]), 1);
-            mbar_init(bar(&ctrl.q_full[i]), 1), mbar_init(bar(&ctrl.q_ready[i]), 1), mbar_init(bar(&ctrl.q_empty[i]), C::kKeyThreads / 32);
-            mbar_init(bar(&ctrl.o_empty[i]), C::kKeyThreads / 32);
+            mbar_init(bar(&c.s_full[i]), 1), mbar_init(bar(&c.s_empty[i]), C::kKeyThreads / 32);
+            mbar_init(bar(&c.q_full[i]), 2), mbar_init(bar(&c.q_ready[i]), 2), mbar_init(bar(&c.q_empty[i]), C::kKeyThreads / 32);
         }
-        mbar_init(bar(&ctrl.drained), 1);
-        ctrl.abort_flag = 0;
+        mbar_init(bar(&c.p_full), C::kKeyThreads / 32), mbar_init(bar(&c.p_empty), 1);
+        mbar_init(bar(&c.drained), 1);
+        if (tid == 0) {
+            prefetch_tensormap(&tm_k);
+            prefetch_tensormap(&tm_v);
+            s_abort = 0;
+        }
         fence_mbar_init();
     }
     if (warp == 1) {
-        tmem_alloc(smem_u32(&ctrl.tmem_base), C::kTmemCols);
+        tmem_alloc(smem_u32(&s_tmem_base), C::kTmemCols);
         tmem_relinquish();
     }
     // operand lines of no row are zero for good
-    for (int i = tid; i < (2 * C::kQBytes + 2 * C::kPBytes) / 16; i += C::kThreads) *reinterpret_cast<uint4*>(smem + C::kQAt + i * 16) = make_uint4(0, 0, 0, 0);
+    constexpr int kLines = (2 * C::kQBytes + C::kPBytes) / 16;
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+        for (int i = tid; i < kLines; i += C::kThreads)
+            *reinterpret_cast<uint4*>(smem_raw + (first - raw) + w * C::kWorkerBytes + C::kQAt + i * 16) = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
-    count_steps<C::kThreads, ROWS, kKeys, C::kUnitCost>(a, s_upto);
+    const int group = a.heads / a.c.kv_heads, plog = a.c.page_log2;
+    cut_shares<C::kThreads, W>(a, (int64_t)blockIdx.x * W, (int64_t)gridDim.x * W, kMinShare, s_start,
+                               [&](const Sequence& sq) { return steps_of<ROWS, kKeys, C::kUnitCost>(a, sq, group); });
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     grid_dependency_trigger();                        // (not before TMEM is mine)
-    const uint32_t tmem = ctrl.tmem_base;
-    const int group = a.heads / a.c.kv_heads, plog = a.c.page_log2;
+    const uint32_t tmem = s_tmem_base + (uint32_t)worker * C::kWorkerCols;
+    const int64_t share = (int64_t)blockIdx.x * W + worker;
     Walk<ROWS, kKeys, C::kUnitCost> walk(a);
-    cut_shares(walk, s_upto, C::kThreads, (int64_t)gridDim.x, kMinShare);
-    walk.begin((int64_t)blockIdx.x, C::kThreads);
+    const int role = warp < C::kFirstGroupWarp ? warp % kRoleWarps : kRoleWarps;
+    if (role < kRoleWarps && role != 1) walk.begin(s_start[worker], share, C::kThreads);
 
-    if (warp == 0) {
+    if (role == 0) {
         // ============================================================ pages, scales, copies
         const uint32_t page_bytes = (uint32_t)kDim << plog;
         const int step = kKeys >> plog;                       // pages of a tile, a copy of K and one of V each
@@ -251,7 +265,7 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 while (!mbar_try_wait(bar(&ctrl.full[z % C::kStages]), (uint32_t)(z / C::kStages) & 1u))
                     if (clock64() - t0 > kTimeoutCycles) break;
             }
-    } else if (warp == 1) {
+    } else if (role == 1) {
         // ============================================================ MMAs
         const bool leader = elect_one();
         const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
@@ -260,14 +274,11 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
         const uint64_t k_desc = smem_desc(base, 16, 1024, kL128), v_desc = smem_desc(base + kTileBytes, 0, 1024, kL128);
         const uint64_t q_desc = smem_desc(q_at, 16, 1024, kL128), p_desc = smem_desc(p_at, 16, 1024, kL128);
         bool live = true;
-        int ahead = 0, begun0 = 0, begun1 = 0, asked0 = 0, asked1 = 0;      // tiles whose S has been asked for; of each set: units begun, tiles asked for
+        int ahead = 0, done = 0;                      // tiles whose S, whose O has been asked for
         int ready0 = 0, ready1 = 0;                   // units with tiles whose rows have been waited for, per buffer
-        // S of a tile goes out before O of the one before it, but nothing that is not there yet is waited for while an O is due: the next unit's
-        // rows may be waiting in turn for whoever waits for that O.
-        int done = 0;                                 // tiles whose O has been asked for
+        // S of a tile goes out before O of the one before it, but nothing that is not there yet is waited for while an O is due.
         bool end = false;                             // no more tiles
-        bool first_a = false, first_b = false;        // of the tiles in between, in order: whether they begin a unit, and their sets
-        int set_a = 0, set_b = 0;
+        bool first_a = false, first_b = false;        // of the tiles in between, in order: whether they begin a unit
         auto there = [&](const uint64_t* b, uint32_t parity, bool wait) {
             if (wait) return live = wait_bar(bar(b), parity, abort_flag, a.dev_status) && live;
             return __shfl_sync(0xFFFFFFFFu, (int)mbar_test_wait(bar(b), parity), 0) != 0;
@@ -280,8 +291,7 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
             if (kind & kLast) end = true, go = false;
             if (go && (kind & kFirst) && !there(&ctrl.q_ready[qb], (uint32_t)(qb == 0 ? ready0 : ready1) & 1u, !due)) go = false;
             if (go && live) {
-                const int b = ahead & 1, set = C::kSets == 2 ? qb : 0;
-                const int mine = set == 0 ? asked0++ : asked1++;
+                const int b = ahead & 1;
                 if (kind & kFirst) ++(qb == 0 ? ready0 : ready1);
                 if (ahead >= 2) live = wait_bar(bar(&ctrl.s_empty[b]), ((uint32_t)(ahead >> 1) & 1u) ^ 1u, abort_flag, a.dev_status) && live;
                 tc_fence_after();
@@ -289,11 +299,11 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                     const uint64_t at = (uint64_t)(s * (kStageBytes >> 4)), qa = (uint64_t)(qb * (C::kQBytes >> 4));
 #pragma unroll
                     for (int j = 0; j < 4; ++j) umma_f8(tm + (b ? C::kSCol1 : 0u), k_desc + at + j * 2, q_desc + qa + j * 2, idesc_s, j > 0);      // 32 elements a step
-                    umma_commit(bar(&ctrl.s_full[set][mine & 1]));
+                    umma_commit(bar(&ctrl.s_full[b]));
                 }
                 __syncwarp();
-                if (ahead == done) first_a = (kind & kFirst) != 0, set_a = set;
-                else first_b = (kind & kFirst) != 0, set_b = set;
+                if (ahead == done) first_a = (kind & kFirst) != 0;
+                else first_b = (kind & kFirst) != 0;
                 ++ahead;
                 if (ahead - done < 2) continue;
             }
@@ -301,77 +311,71 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 if (end) break;
                 continue;
             }
-            const int so = done % C::kStages, bo = done & 1;
-            live = wait_bar(bar(&ctrl.p_full[bo]), (uint32_t)(done >> 1) & 1u, abort_flag, a.dev_status) && live;
-            if (first_a) {
-                const int n = set_a == 0 ? begun0++ : begun1++;
-                if (n > 0) live = wait_bar(bar(&ctrl.o_empty[set_a]), ((uint32_t)n & 1u) ^ 1u, abort_flag, a.dev_status) && live;
-            }
+            const int so = done % C::kStages;
+            live = wait_bar(bar(&ctrl.p_full), (uint32_t)done & 1u, abort_flag, a.dev_status) && live;
             tc_fence_after();
             if (leader && live) {
-                const uint64_t at = (uint64_t)(so * (kStageBytes >> 4)), pa = (uint64_t)(bo * (C::kPBytes >> 4));
+                const uint64_t at = (uint64_t)(so * (kStageBytes >> 4));
 #pragma unroll
                 for (int j = 0; j < 4; ++j)           // 32 keys a step: 4 groups of 8 lines of V
-                    umma_f8(tm + C::kOCol + set_a * C::kOSet, v_desc + at + j * (4096 >> 4), p_desc + pa + j * 2, idesc_o, !first_a || j > 0);
-                umma_commit(bar(&ctrl.p_empty[bo]));
+                    umma_f8(tm + C::kOCol, v_desc + at + j * (4096 >> 4), p_desc + j * 2, idesc_o, !first_a || j > 0);
+                umma_commit(bar(&ctrl.p_empty));
                 umma_commit(bar(&ctrl.empty[so]));
             }
             __syncwarp();
             ++done;
-            first_a = first_b, set_a = set_b;
+            first_a = first_b;
         }
         if (leader) umma_commit(bar(&ctrl.drained));  // nothing of the tensor cores' is in flight when TMEM and shared memory are given up
         const long long c0 = clock64();
         while (!mbar_try_wait(bar(&ctrl.drained), 0))
             if (clock64() - c0 > kTimeoutCycles) break;
         __syncwarp();
-    } else if (warp == 2) {
-        // ============================================================ the rows of the units, one unit ahead
+    } else if (role < kRoleWarps) {
+        // ============================================================ the rows of the units, one unit ahead: pairs of rows in turn
         Unit u;
         CutUnit cut{0, 0, 0, 0};
-        const int share = (int)blockIdx.x;
-        int tiles = 0, ends = 0;
-        for (int k = 0; ends < C::kSets; ++k) {
-            if (ends > 0 || !walk.next(u)) ++ends;
+        const int turn = role - 2;
+        for (int k = 0;; ++k) {
+            const bool more = walk.next(u);
             if (k >= 2) wait_bar(bar(&ctrl.q_empty[k & 1]), ((uint32_t)(k >> 1) & 1u) ^ 1u, abort_flag, a.dev_status);
             if (*abort_flag) break;
             __syncwarp();
             Rows<ROWS>& rows = s_rows[k & 1];
-            if (ends > 0) {                           // for every set: there are no more units
+            if (!more) {
                 if (lane == 0) {
-                    rows.tiles = -1;
+                    if (turn == 0) rows.tiles = -1;
                     mbar_arrive(bar(&ctrl.q_full[k & 1]));
                 }
-                continue;
+                break;
             }
             const bool begins = u.first == 0, whole = begins && u.last == u.sp.steps;
             if (begins && !whole) cut.b = u.b, cut.row_tile = u.tile, cut.head = u.head, cut.pieces = walk.pieces(u, share);
             const int n = max(u.u1 - u.u0, 0);
-            if (lane == 0) {
-                rows.tile0 = tiles, rows.tiles = n, rows.key0 = u.sp.lo + u.u0 * kKeys, rows.n_rows = u.n_rows;
+            if (turn == 0 && lane == 0) {
+                rows.tiles = n, rows.key0 = u.sp.lo + u.u0 * kKeys, rows.n_rows = u.n_rows;
                 rows.hi_min = u.hi_min, rows.hi_max = u.hi_max, rows.lo_min = u.lo_min, rows.lo_max = u.lo_max;
-                rows.slot = whole ? -1 : 2 * share + (begins ? 1 : 0);
+                rows.slot = whole ? -1 : (int)(2 * share + (begins ? 1 : 0));
             }
-            tiles += n;
             const int row = min(lane, u.n_rows - 1);
             const int token = (u.tile_row + row) / group, qh = u.head * group + (u.tile_row + row - token * group);
             const int64_t in = ((int64_t)u.sq.row0 + token) * a.ldq + (int64_t)qh * kDim;
-            if (lane < ROWS) {
+            if (turn == 0 && lane < ROWS) {
                 rows.lower[lane] = lower_key(a, u.sq, token);
                 rows.upper[lane] = upper_key(a, u.sq, token);
                 rows.out[lane] = ((int64_t)u.sq.row0 + token) * a.ldo + (int64_t)qh * kDim;
                 rows.lse[lane] = ((int64_t)u.sq.row0 + token) * a.heads + qh;
             }
-            uint4 q[ROWS / 2];                        // half a warp a row, eight elements a lane; asked for together
+            uint4 q[ROWS / 4];                        // half a warp a row, eight elements a lane; asked for together
 #pragma unroll
-            for (int i = 0; i < ROWS / 2; ++i) {
-                const int r = 2 * i + (lane >> 4);
+            for (int i = 0; i < ROWS / 4; ++i) {
+                const int r = 4 * i + 2 * turn + (lane >> 4);
                 const int64_t from = __shfl_sync(0xFFFFFFFFu, in, r);
                 q[i] = r < u.n_rows ? ld128_rw_stream(static_cast<const __nv_bfloat16*>(a.q) + from + (lane & 15) * 8) : make_uint4(0, 0, 0, 0);
             }
 #pragma unroll
-            for (int i = 0; i < ROWS / 2; ++i) {
-                const int r = 2 * i + (lane >> 4), chunk = lane & 15;
+            for (int i = 0; i < ROWS / 4; ++i) {
+                const int r = 4 * i + 2 * turn + (lane >> 4), chunk = lane & 15;
                 float x[8], amax = 0.f;
                 unpack<__nv_bfloat16>(q[i], x);
 #pragma unroll
@@ -400,33 +404,30 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 if (n > 0) mbar_arrive(bar(&ctrl.q_ready[k & 1]));
             }
         }
-        if (lane == 0) cuts[blockIdx.x] = *abort_flag == 0 ? cut : CutUnit{0, 0, 0, 0};
-    } else if (warp >= kFirstGroupWarp) {
+        if (turn == 0 && lane == 0) cuts[share] = *abort_flag == 0 ? cut : CutUnit{0, 0, 0, 0};
+    } else {
         // ============================================================ a key per thread
         const int q4 = warp & 3, key_lane = q4 * 32 + lane;      // the quarter of TMEM's lanes that this warp may access
-        const int all = (warp - kFirstGroupWarp) >> 2, set = all / C::kGroups, gr = all % C::kGroups, r0 = gr * RPG;
-        const uint32_t o_col = C::kOCol + set * C::kOSet;
+        const int all = (warp - C::kFirstGroupWarp) >> 2, gr = all % C::kGroups, r0 = gr * RPG;
         const uint32_t lane_addr = (uint32_t)(q4 * 32) << 16;
-        uint32_t p_off[RPG];                          // of this key in the lines of the weights
-#pragma unroll
-        for (int r = 0; r < RPG; ++r) p_off[r] = (uint32_t)(((((key_lane >> 4) ^ (r0 + r)) & 7) << 4) + (key_lane & 15));
-        int own = 0;                                  // tiles of this set so far
-        for (int k = set;; k += C::kSets) {
+        const uint32_t p_off = (uint32_t)(((((key_lane >> 4) ^ r0) & 7) << 4) + (key_lane & 15));      // of this key in line r0 of the weights; r bits 4.. on
+        int tiles = 0;                                // so far
+        for (int k = 0;; ++k) {
             wait_bar(bar(&ctrl.q_full[k & 1]), (uint32_t)(k >> 1) & 1u, abort_flag, a.dev_status);
-            // after an abort the waits fall through: a set leaves here together, or goes on to the end of its unit together, so that nobody is left
-            // at a barrier
-            if (threads_any<C::kKeyThreads>(14 + set, *abort_flag != 0)) break;
+            // after an abort the waits fall through: a worker's groups leave here together, or go on to the end of the unit together, so that
+            // nobody is left at a barrier
+            if (threads_any<C::kKeyThreads>(14 + worker, *abort_flag != 0)) break;
             const Rows<ROWS>& rows = s_rows[k & 1];
             const int n = rows.tiles, n_rows = rows.n_rows, hi_min = rows.hi_min, hi_max = rows.hi_max, lo_min = rows.lo_min, lo_max = rows.lo_max;
             if (n < 0) break;
-            int tiles = rows.tile0, key0 = rows.key0;
-            float m[RPG], l[RPG], rowf[RPG];
+            int key0 = rows.key0;
+            float m[RPG], l[RPG];
 #pragma unroll
-            for (int r = 0; r < RPG; ++r) m[r] = kNone, l[r] = 0.f, rowf[r] = rows.factor[r0 + r];
+            for (int r = 0; r < RPG; ++r) m[r] = kNone, l[r] = 0.f;
 #pragma unroll 1
-            for (int i = 0; i < n; ++i, ++tiles, ++own, key0 += kKeys) {
+            for (int i = 0; i < n; ++i, ++tiles, key0 += kKeys) {
                 const int b = tiles & 1;
-                wait_bar(bar(&ctrl.s_full[set][own & 1]), (uint32_t)(own >> 1) & 1u, abort_flag, a.dev_status);
+                wait_bar(bar(&ctrl.s_full[b]), (uint32_t)(tiles >> 1) & 1u, abort_flag, a.dev_status);
                 const int s = tiles % C::kStages;
                 wait_bar(bar(&ctrl.full[s]), (uint32_t)(tiles / C::kStages) & 1u, abort_flag, a.dev_status);      // (long complete: for what was written there)
                 __syncwarp();
@@ -451,7 +452,7 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 float c[RPG], e[RPG], top = -INFINITY;
 #pragma unroll
                 for (int r = 0; r < RPG; ++r) {
-                    c[r] = rowf[r] * sc.x;
+                    c[r] = rows.factor[r0 + r] * sc.x;
                     e[r] = fmaf(y[r], c[r], sc.y - m[r]);
                 }
                 const bool hidden = sc.w == 0.f || key >= hi_max || key < lo_min;      // no row sees the key, or its page cannot be used
@@ -466,7 +467,7 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                             const uint4 x = *reinterpret_cast<const uint4*>(line + ((c ^ lane) & 7) * 16);
                             nan |= (e4m3x4_nan_bits(x.x) | e4m3x4_nan_bits(x.y) | e4m3x4_nan_bits(x.z) | e4m3x4_nan_bits(x.w)) != 0;
                         }
-                    if (border && C::kGroups > 1) sync_threads_of<C::kKeyThreads>(14 + set);      // every group has looked
+                    if (border && C::kGroups > 1) sync_threads_of<C::kKeyThreads>(14 + worker);      // every group has looked
                     if (gr == 0 && (hidden || nan))
 #pragma unroll 2
                         for (int c = 0; c < 8; ++c) {
@@ -502,25 +503,25 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                         e[r] = y[r] - next;
                     }
                     if (i > 0) {                      // what is in O already: the MMAs of the tile before are done, those of this one wait for its weights
-                        wait_bar(bar(&ctrl.p_empty[b ^ 1]), (uint32_t)((tiles - 1) >> 1) & 1u, abort_flag, a.dev_status);
+                        wait_bar(bar(&ctrl.p_empty), (uint32_t)(tiles - 1) & 1u, abort_flag, a.dev_status);
                         __syncwarp();
                         tc_fence_after();
 #pragma unroll 1
                         for (int z = 0; z < kTermsP; ++z) {
                             uint32_t v[RPG];
-                            tmem_load<RPG>(tmem + lane_addr + o_col + z * ROWS + r0, v);
+                            tmem_load<RPG>(tmem + lane_addr + C::kOCol + z * ROWS + r0, v);
                             tmem_wait_ld();
 #pragma unroll
                             for (int r = 0; r < RPG; ++r) v[r] = __float_as_uint(__uint_as_float(v[r]) * shrink[r]);
-                            tmem_st<RPG>(tmem + lane_addr + o_col + z * ROWS + r0, v);
+                            tmem_st<RPG>(tmem + lane_addr + C::kOCol + z * ROWS + r0, v);
                         }
                         tmem_wait_st();
                         tc_fence_before();
                     }
                     sync_threads_of<128>(1 + all);     // (s_part is free again)
                 }
-                if (tiles >= 2) wait_bar(bar(&ctrl.p_empty[b]), ((uint32_t)(tiles >> 1) & 1u) ^ 1u, abort_flag, a.dev_status);
-                uint8_t* const p = smem + (p_at - base) + b * C::kPBytes + r0 * 128;
+                if (tiles >= 1) wait_bar(bar(&ctrl.p_empty), (uint32_t)(tiles - 1) & 1u, abort_flag, a.dev_status);
+                uint8_t* const p = smem + (p_at - base) + r0 * 128;
 #pragma unroll
                 for (int r = 0; r < RPG; r += 2) {
                     const float w0 = ex2(e[r]), w1 = ex2(e[r + 1]);
@@ -532,15 +533,14 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                         const uint32_t back = e4m3x2_to_f16x2(code);
                         rest = __hmul2(__hsub2(rest, *reinterpret_cast<const __half2*>(&back)), __float2half2_rn(kTermStep));
                         // line z ROWS + r0 + r: r0 is a multiple of 4 (and of 8 where groups have 8 rows)
-                        const uint32_t swz = (uint32_t)((z * ROWS) & 7) << 4;
-                        p[(z * ROWS + r) * 128 + (p_off[r] ^ swz)] = (uint8_t)code;
-                        p[(z * ROWS + r + 1) * 128 + (p_off[r + 1] ^ swz)] = (uint8_t)(code >> 8);
+                        p[(z * ROWS + r) * 128 + (p_off ^ (uint32_t)((z * ROWS ^ r) & 7) << 4)] = (uint8_t)code;
+                        p[(z * ROWS + r + 1) * 128 + (p_off ^ (uint32_t)((z * ROWS ^ (r + 1)) & 7) << 4)] = (uint8_t)(code >> 8);
                     }
                 }
                 fence_proxy_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(&ctrl.p_full[b]));
+                if (lane == 0) mbar_arrive(bar(&ctrl.p_full));
             }
             // ---- the unit's result, or a piece of it: an element per thread
 #pragma unroll
@@ -553,22 +553,19 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
 #pragma unroll
             for (int r = 0; r < RPG; ++r) o[r] = 0.f;
             if (n > 0) {
-                const int t = tiles - 1;
-                wait_bar(bar(&ctrl.p_empty[t & 1]), (uint32_t)(t >> 1) & 1u, abort_flag, a.dev_status);
+                wait_bar(bar(&ctrl.p_empty), (uint32_t)(tiles - 1) & 1u, abort_flag, a.dev_status);
                 __syncwarp();
                 tc_fence_after();
                 float f = 1.f;
 #pragma unroll
                 for (int z = 0; z < kTermsP; ++z, f /= kTermStep) {
                     uint32_t v[RPG];
-                    tmem_load<RPG>(tmem + lane_addr + o_col + z * ROWS + r0, v);
+                    tmem_load<RPG>(tmem + lane_addr + C::kOCol + z * ROWS + r0, v);
                     tmem_wait_ld();
 #pragma unroll
                     for (int r = 0; r < RPG; ++r) o[r] = fmaf(__uint_as_float(v[r]), f, o[r]);
                 }
                 tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(&ctrl.o_empty[set]));
             }
             const bool live = *abort_flag == 0;       // (nothing of an aborted call is stored)
             sync_threads_of<128>(1 + all);
@@ -594,11 +591,11 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 1) tmem_dealloc(tmem, C::kTmemCols);
+    if (warp == 1) tmem_dealloc(s_tmem_base, C::kTmemCols);
 }
 
 template <int ROWS>
-int64_t share_count() { return sm_count(); }
+int64_t share_count() { return (int64_t)sm_count() * Cfg<ROWS>::kWorkers; }
 
 template <int ROWS>
 size_t bytes_needed() { return cut_bytes(share_count<ROWS>()) + (size_t)(2 * share_count<ROWS>() * slot_floats(ROWS, kDim)) * sizeof(float); }
@@ -622,7 +619,7 @@ molora_status_t launch(const AttendArgs& a, void* ws, cudaStream_t s)
     const int64_t shares = share_count<ROWS>();
     CutUnit* cuts = static_cast<CutUnit*>(ws);
     float* slots = reinterpret_cast<float*>(static_cast<char*>(ws) + cut_bytes(shares));
-    if (launch_kernel(attend_stream_kernel<ROWS>, dim3((unsigned)shares), dim3(C::kThreads), C::kSmem, s, 1, true, a, tm_k, tm_v, cuts, slots) != cudaSuccess)
+    if (launch_kernel(attend_stream_kernel<ROWS>, dim3((unsigned)sm_count()), dim3(C::kThreads), C::kSmem, s, 1, true, a, tm_k, tm_v, cuts, slots) != cudaSuccess)
         return MOLORA_ERR_CUDA;
     return cuda_ok(launch_kernel(attend_join_kernel<__nv_bfloat16, kDim, ROWS>, dim3((unsigned)shares, ROWS / kJoinRows), dim3(kJoinWarps * 32), 0, s, 1, true, a,
                                  static_cast<const CutUnit*>(cuts), static_cast<const float*>(slots)));

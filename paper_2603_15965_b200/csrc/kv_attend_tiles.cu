@@ -112,21 +112,14 @@ struct TileWalk {
             }
         }
     }
-    __device__ void begin(const int64_t* s_upto, int64_t w)
+    __device__ void begin(const ShareStart& from, int64_t w)
     {
-        const int64_t total = s_upto[kThreads - 1];
-        share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kMinShare);
+        share = from.share;
         at = w * share;
-        stop = min(total, at + share);
+        stop = min(from.total, at + share);
         if (at >= stop) return;
-        int lo = 0, hi = kThreads - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (s_upto[mid] > at) hi = mid;
-            else lo = mid + 1;
-        }
-        b = lo * ((a.c.B + kThreads - 1) / kThreads);
-        base = lo > 0 ? s_upto[lo - 1] : 0;
+        b = from.part * ((a.c.B + kThreads - 1) / kThreads);
+        base = from.base;
         load();
     }
     __device__ bool next(TileUnit& u)
@@ -134,7 +127,7 @@ struct TileWalk {
         if (at >= stop) return false;
         skip_to(at);
         u.sq = sq, u.b = b, u.tile = tile;
-        u.head = (int)((at - base) / sp.steps);
+        u.head = (int)quotient(at - base, sp.steps);
         u.at = base + (int64_t)u.head * sp.steps;
         u.lo = sp.lo, u.steps = sp.steps;
         u.first = (int)(at - u.at), u.last = (int)min((int64_t)sp.steps, stop - u.at);
@@ -199,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 {
     using namespace ptx;
     __shared__ Control ctrl;
-    __shared__ int64_t s_upto[kThreads];
+    __shared__ ShareStart s_start;
     __shared__ KeyTile s_tiles[kTileQueue];
     __shared__ UnitInfo s_units[kUnitQueue];
     __shared__ float s_pair[2][2][kTileRows];         // what the two threads of a row tell each other
@@ -230,26 +223,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_alloc(smem_u32(&ctrl.tmem_base), kTmemCols);
         tmem_relinquish();
     }
-    {
-        const int part = (a.c.B + kThreads - 1) / kThreads;
-        int64_t incl = 0;
-        for (int b = tid * part; b < min(a.c.B, (tid + 1) * part); ++b) {
-            const Sequence sq = sequence_of(a.c, b, a.N);
-            const int tiles = row_tiles(sq, group);
-            for (int t = 0; t < tiles; ++t) incl += (int64_t)tile_span(a, sq, t, group).steps * a.c.kv_heads;
-            if (sq.bad && blockIdx.x == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
-        }
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-            if (lane >= o) incl += up;
-        }
-        if (lane == 31) s_upto[tid] = incl;
-        __syncthreads();
-        for (int z = 0; z < warp; ++z) incl += s_upto[32 * z + 31];
-        __syncthreads();
-        s_upto[tid] = incl;
-    }
+    cut_shares<kThreads, 1>(a, blockIdx.x, gridDim.x, kMinShare, &s_start, [&](const Sequence& sq) {
+        int64_t steps = 0;
+        const int tiles = row_tiles(sq, group);
+        for (int t = 0; t < tiles; ++t) steps += (int64_t)tile_span(a, sq, t, group).steps * a.c.kv_heads;
+        return steps;
+    });
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -647,7 +626,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ============================================================ units, pages, scales
         const int plog = a.c.page_log2;
         TileWalk walk(a);
-        walk.begin(s_upto, blockIdx.x);
+        walk.begin(s_start, blockIdx.x);
         CutUnit cut{0, 0, 0, 0};
         int tiles = 0, units = 0;
         auto push_unit = [&](const UnitInfo& info) {
