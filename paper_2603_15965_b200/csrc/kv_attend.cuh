@@ -74,6 +74,7 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int32_t b)
 struct ShareStart {
     int64_t base, total, share;
     int32_t part;
+    Sequence sq;                            // the part's first sequence
 };
 
 // The units of a share, in order; every thread (or warp) that asks gets the same.
@@ -126,7 +127,8 @@ struct Walk {
         if (at >= stop) return;
         b = from.part * ((a.c.B + parts - 1) / parts);
         base = from.base;
-        load();
+        sq = from.sq;
+        sp = span_of<ROWS, KEYS, COST>(sq, group, a.window);
     }
 };
 
@@ -139,8 +141,10 @@ __device__ __forceinline__ void cut_shares(const AttendArgs& a, int64_t first_sh
     const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int part = (a.c.B + THREADS - 1) / THREADS;
     int64_t own = 0;
+    Sequence first{};
     for (int b = tid * part; b < min(a.c.B, (tid + 1) * part); ++b) {
         const Sequence sq = sequence_of(a.c, b, a.N);
+        if (b == tid * part) first = sq;
         own += steps_of(sq);
         if (sq.bad && blockIdx.x == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
     }
@@ -162,7 +166,7 @@ __device__ __forceinline__ void cut_shares(const AttendArgs& a, int64_t first_sh
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         const int64_t at = (first_share + w) * share;
-        if (at >= upto - own && at < upto) s_start[w].base = upto - own, s_start[w].part = tid;
+        if (at >= upto - own && at < upto) s_start[w].base = upto - own, s_start[w].part = tid, s_start[w].sq = first;
         if (tid == 0) s_start[w].total = total, s_start[w].share = share;
     }
     __syncthreads();

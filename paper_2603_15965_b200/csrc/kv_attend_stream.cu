@@ -151,7 +151,6 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
     Rows<ROWS>* const s_rows = s_rows_all[worker];
     auto bar = [](const uint64_t* b) { return smem_u32(b); };
 
-    grid_dependency_wait();
     if (tid < W) {
         Control& c = ctrls[tid];
         for (int s = 0; s < C::kStages; ++s) mbar_init(bar(&c.full[s]), 1), mbar_init(bar(&c.empty[s]), 1);
@@ -168,10 +167,6 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
         }
         fence_mbar_init();
     }
-    if (warp == 1) {
-        tmem_alloc(smem_u32(&s_tmem_base), C::kTmemCols);
-        tmem_relinquish();
-    }
     // operand lines of no row are zero for good
     constexpr int kLines = (2 * C::kQBytes + C::kPBytes) / 16;
 #pragma unroll
@@ -179,6 +174,11 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
         for (int i = tid; i < kLines; i += C::kThreads)
             *reinterpret_cast<uint4*>(smem_raw + (first - raw) + w * C::kWorkerBytes + C::kQAt + i * 16) = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
+    grid_dependency_wait();
+    if (warp == 1) {
+        tmem_alloc(smem_u32(&s_tmem_base), C::kTmemCols);
+        tmem_relinquish();
+    }
     const int group = a.heads / a.c.kv_heads, plog = a.c.page_log2;
     cut_shares<C::kThreads, W>(a, (int64_t)blockIdx.x * W, (int64_t)gridDim.x * W, kMinShare, s_start,
                                [&](const Sequence& sq) { return steps_of<ROWS, kKeys, C::kUnitCost>(a, sq, group); });

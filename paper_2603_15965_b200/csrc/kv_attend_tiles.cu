@@ -91,9 +91,9 @@ struct TileWalk {
     Sequence sq;
     TileSpan sp{0, 1};
     __device__ explicit TileWalk(const AttendArgs& args) : a(args), group(args.heads / args.c.kv_heads) {}
-    __device__ void load()
+    __device__ void load(const Sequence& s)
     {
-        sq = sequence_of(a.c, b, a.N);
+        sq = s;
         tiles = row_tiles(sq, group);
         tile = 0;
         if (tiles > 0) sp = tile_span(a, sq, 0, group);
@@ -108,7 +108,7 @@ struct TileWalk {
                 if (++tile < tiles) sp = tile_span(a, sq, tile, group);
             } else {
                 ++b;
-                load();
+                load(sequence_of(a.c, b, a.N));
             }
         }
     }
@@ -120,7 +120,7 @@ struct TileWalk {
         if (at >= stop) return;
         b = from.part * ((a.c.B + kThreads - 1) / kThreads);
         base = from.base;
-        load();
+        load(from.sq);
     }
     __device__ bool next(TileUnit& u)
     {
@@ -204,7 +204,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto bar = [](const uint64_t* b) { return smem_u32(b); };
     const int group = a.heads / a.c.kv_heads;
 
-    grid_dependency_wait();
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             for (int z = 0; z < 2; ++z)
@@ -219,6 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ctrl.abort_flag = 0;
         fence_mbar_init();
     }
+    grid_dependency_wait();
     if (warp == kMmaWarp0) {
         tmem_alloc(smem_u32(&ctrl.tmem_base), kTmemCols);
         tmem_relinquish();
