@@ -42,7 +42,7 @@ template <int ROWS>
 struct Cfg {
     static constexpr int kRowsPerGroup = ROWS >= 16 ? 8 : 4, kGroups = ROWS / kRowsPerGroup;
     static constexpr int kWorkers = ROWS <= 24 ? 2 : 1;
-    static constexpr int kUnitCost = 2;                                   // tiles that a unit's rows and results cost
+    static constexpr int kUnitCost = ROWS < 16 ? 2 : 3;                                   // tiles that a unit's rows and results cost
     static constexpr int kKeyThreads = 128 * kGroups, kFirstGroupWarp = kRoleWarps * kWorkers;      // (kKeyThreads: of a worker)
     static constexpr int kThreads = 32 * kFirstGroupWarp + kWorkers * kKeyThreads;
     static_assert(kThreads <= 1024, "threads");
