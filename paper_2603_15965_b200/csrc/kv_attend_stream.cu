@@ -5,11 +5,11 @@
 // written as a sum of e4m3 terms, each in columns of its own:
 //   q (8 significant bits) = t1 + t2 / 32, exactly: the rest that rounding to 4 bits leaves of 8 fits 4; a power of two per row brings the largest
 //       element to [2^7, 2^8), so elements below 2^-14 of it are off by at most 2^-23 of it
-//   a weight, rounded to fp16 (11 bits), = t1 + t2 / 32 + t3 / 1024, exactly (to 2^-20 where a row's largest is 2 or more)
+//   a weight, rounded to fp16 (11 bits), = t1 + t2 / 32 + t3 / 1024, exactly (to 2^-20 where a row's largest is 32 or more)
 //   S^T [128 keys x 2 rows]   = K Q^T     A = K tile, keys the 128 lanes of TMEM; B = q's terms
 //   O^T [128 elements x 3 rows] += V^T P^T  A = V tile read across (MN-major); B = the weights' terms
 // with the key as the lane a thread owns one key: the scales of its block, its mask and its weights are its own, and reductions
-// over keys are needed only when a row's reference moves (a score 2^4 over the reference) and at the end of a unit.
+// over keys are needed only when a row's reference moves (a score 2^8 over the weight of one) and at the end of a unit.
 //   warp 0    pages, scales and TMA (5 or 6 tiles of 128 keys, 32 KB each, in flight or in use)
 //   warp 1    the MMAs, those of S one tile ahead of those of O
 //   warp 2    the units and their rows, one or two units ahead: q's terms, factors, bounds, places of the results
@@ -35,7 +35,7 @@ constexpr int kTileBytes = kKeys * kDim, kStageBytes = 2 * kTileBytes;      // K
 constexpr int kMinShare = 2;                 // tiles
 constexpr int kTermsQ = 2, kTermsP = 3;
 constexpr float kTermStep = 32.f;            // a term's weight against the next
-constexpr float kTop = 1.f, kSlack = 7.f;    // a row's largest weight when its reference is set: 2; it may grow by 2^7 before the reference moves
+constexpr float kTop = 5.f, kSlack = 3.f;    // a row's largest weight when its reference is set: 2^5; it may grow by 2^3 before the reference moves
 constexpr float kNan = __builtin_nanf("");
 
 template <int ROWS>
