@@ -1,5 +1,4 @@
 // C ABI of the paged cache and of draft verification: argument validation on the host, then enqueue.
-#include <algorithm>
 #include <cmath>
 
 #include "kv_cache.cuh"
@@ -17,6 +16,7 @@ molora_status_t check_cache(const molora_kv_cache_t* c, const molora_sequences_t
     if (N >= INT32_MAX || (dt != MOLORA_F32 && dt != MOLORA_BF16) || c->kv_heads > kMaxHeads) return MOLORA_ERR_UNSUPPORTED;
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return MOLORA_ERR_UNSUPPORTED;
     if (c->dim != 64 && c->dim != 128) return MOLORA_ERR_UNSUPPORTED;
+    if ((int64_t)c->n_pages * c->kv_heads * c->page > INT32_MAX) return MOLORA_ERR_UNSUPPORTED;       // lines of the pool (of 64 bytes or more each)
     if (N == 0 || s->B == 0) return MOLORA_OK;
     if (s->cu_tokens == nullptr || s->kv_lens == nullptr || (s->max_pages > 0 && s->page_table == nullptr)) return MOLORA_ERR_INVALID_ARG;
     if (s->B > 1 && s->ld_table < s->max_pages) return MOLORA_ERR_INVALID_ARG;
@@ -75,10 +75,9 @@ molora_status_t molora_kv_append(const molora_kv_cache_t* cache, const molora_se
 size_t molora_kv_attend_workspace_bytes(molora_dtype_t dt, int32_t heads, int32_t kv_heads, int32_t dim, int64_t max_tokens)
 {
     if ((dim != 64 && dim != 128) || kv_heads < 1 || heads < 1 || heads % kv_heads != 0 || max_tokens < 1 || (dt != MOLORA_F32 && dt != MOLORA_BF16)) return 0;
-    // (the choice of kernel depends on the pool too, which is not known here)
     const int64_t rows = max_tokens * (heads / kv_heads);
-    const size_t other = dt != MOLORA_BF16 || dim != 128 ? 0 : rows <= 32 ? attend_stream_workspace_bytes(rows) : attend_tiles_workspace_bytes();
-    return std::max(other, attend_rows_workspace_bytes(dt, dim, rows));
+    if (dt != MOLORA_BF16 || dim != 128) return attend_rows_workspace_bytes(dt, dim, rows);
+    return rows <= kMaxStreamRows ? attend_stream_workspace_bytes(rows) : attend_tiles_workspace_bytes();
 }
 
 molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_sequences_t* seqs, molora_dtype_t dt, int64_t N, const void* q,
@@ -102,9 +101,9 @@ molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_se
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.dev_status = dev_status;
     const int64_t rows = max_tokens * (heads / cache->kv_heads);
-    if (attend_stream_eligible(a.c, dt, rows)) return launch_attend_stream(a, rows, ws, static_cast<cudaStream_t>(stream));
-    if (rows > 32 && attend_tiles_eligible(a.c, dt)) return launch_attend_tiles(a, ws, static_cast<cudaStream_t>(stream));
-    return launch_attend_rows(a, dt, rows, ws, static_cast<cudaStream_t>(stream));
+    if (dt != MOLORA_BF16 || cache->dim != 128) return launch_attend_rows(a, dt, rows, ws, static_cast<cudaStream_t>(stream));
+    if (rows <= kMaxStreamRows) return launch_attend_stream(a, rows, ws, static_cast<cudaStream_t>(stream));
+    return launch_attend_tiles(a, ws, static_cast<cudaStream_t>(stream));
 }
 
 molora_status_t molora_verify_drafts(const void* target, int64_t target_ld_seq, int64_t target_ld, const void* draft, int64_t draft_ld_seq,

@@ -1,4 +1,4 @@
-// Attention over the paged 8-bit cache for tiles of 8 to 32 query rows (molora_kv_attend): single tokens, drafted tokens, fp32.
+// Attention over the paged 8-bit cache for fp32 rows, and for bf16 rows with heads of 64 (molora_kv_attend), in tiles of 8 to 32 rows.
 //
 // A row of a sequence is (new token, query head of the group that shares a key / value head); 8 NT consecutive rows, one
 // key / value head and the keys that they see are a UNIT.  The units' keys, cut into steps of 32, form one long list; every CTA
@@ -128,347 +128,345 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
     CutUnit cut{0, 0, 0, 0};
     Unit un;
     while (walk.next(un)) {
-        {
-            const Sequence& sq = un.sq;
-            const int lo0 = un.sp.lo, head = un.head, n_rows = un.n_rows, tile_row = un.tile_row;
-            const int hi_min = un.hi_min, hi_max = un.hi_max, lo_min = un.lo_min, lo_max = un.lo_max;
-            auto token_of = [&](int r) { return (tile_row + min(r, n_rows - 1)) / group; };
+        const Sequence& sq = un.sq;
+        const int lo0 = un.sp.lo, head = un.head, n_rows = un.n_rows, tile_row = un.tile_row;
+        const int hi_min = un.hi_min, hi_max = un.hi_max, lo_min = un.lo_min, lo_max = un.lo_max;
+        auto token_of = [&](int r) { return (tile_row + min(r, n_rows - 1)) / group; };
 
-            // ---- its steps that some row sees, a contiguous part of them for each warp; the first come in while q does
-            const int u0 = un.u0, u1 = un.u1;
-            const int per_warp = (max(u1 - u0, 0) + kWarpsPerCta - 1) / kWarpsPerCta;
-            const int s0 = u0 + warp * per_warp, s1 = min(u1, s0 + per_warp);
-            const int32_t* table = a.c.table + (int64_t)un.b * a.c.ld_table;
-            int group0 = -1;                              // first of the 32 pages whose ids and scales the lanes hold
-            int32_t page_id = -1;
-            float page_ks = 0.f, page_lvs = 0.f, page_inv = 0.f;
-            auto load_pages = [&](int page) {
-                group0 = page;
-                page_id = -1;
-                if (((int64_t)(page + lane) << plog) < hi_max) {
-                    page_id = ptx::ld_dependent(table + page + lane);
-                    if (page_id < 0 || page_id >= a.c.n_pages) {
-                        page_id = -1;
-                        if (a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
-                    } else {
-                        const int64_t block = (int64_t)page_id * a.c.kv_heads + head;
-                        page_ks = ptx::ld_dependent(a.c.k_scale + block);
-                        const float vs = clamped_scale(ptx::ld_dependent(a.c.v_scale + block));
-                        page_lvs = log2f(vs), page_inv = 1.f / vs;
-                    }
+        // ---- its steps that some row sees, a contiguous part of them for each warp; the first come in while q does
+        const int u0 = un.u0, u1 = un.u1;
+        const int per_warp = (max(u1 - u0, 0) + kWarpsPerCta - 1) / kWarpsPerCta;
+        const int s0 = u0 + warp * per_warp, s1 = min(u1, s0 + per_warp);
+        const int32_t* table = a.c.table + (int64_t)un.b * a.c.ld_table;
+        int group0 = -1;                              // first of the 32 pages whose ids and scales the lanes hold
+        int32_t page_id = -1;
+        float page_ks = 0.f, page_lvs = 0.f, page_inv = 0.f;
+        auto load_pages = [&](int page) {
+            group0 = page;
+            page_id = -1;
+            if (((int64_t)(page + lane) << plog) < hi_max) {
+                page_id = ptx::ld_dependent(table + page + lane);
+                if (page_id < 0 || page_id >= a.c.n_pages) {
+                    page_id = -1;
+                    if (a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
+                } else {
+                    const int64_t block = (int64_t)page_id * a.c.kv_heads + head;
+                    page_ks = ptx::ld_dependent(a.c.k_scale + block);
+                    const float vs = clamped_scale(ptx::ld_dependent(a.c.v_scale + block));
+                    page_lvs = log2f(vs), page_inv = 1.f / vs;
                 }
-            };
-            // 16 keys from `row` (of all tokens of the pool) on
-            auto copy_half = [&](int64_t row, uint32_t dst) {
-                const uint8_t* k = a.c.k + row * D + (g * D + t * 16);
-                const uint32_t kdst = dst + (uint32_t)(lane * 16);
+            }
+        };
+        // 16 keys from `row` (of all tokens of the pool) on
+        auto copy_half = [&](int64_t row, uint32_t dst) {
+            const uint8_t* k = a.c.k + row * D + (g * D + t * 16);
+            const uint32_t kdst = dst + (uint32_t)(lane * 16);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int f = 0; f < HF; ++f) copy_async<16>(kdst + (uint32_t)((j * HF + f) * 512), k + j * 8 * D + f * 64);
+            const uint8_t* v = a.c.v + row * D + (2 * t * D + g * kVBytes);
+            const uint32_t vdst = dst + 2 * HF * 512 + (uint32_t)(lane * kVBytes);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) copy_async<kVBytes>(vdst + (uint32_t)(j * 32 * kVBytes), v + ((j & 1) + 8 * (j >> 1)) * D);
+        };
+        auto issue = [&](int s) {
+            if (s < s1) {
+                const int key = lo0 + s * kStepKeys, page = key >> plog, put = (s - s0) & (kStages - 1);
+                if (group0 < 0 || page >= group0 + 32 || (plog == 4 && page + 1 >= group0 + 32)) load_pages(page);
+                const uint32_t dst = ring_at + (uint32_t)(put * 2 * Sh::kHalfBytes);
+                const int32_t id = __shfl_sync(0xFFFFFFFFu, page_id, page - group0);
+                const float4 sc = make_float4(page_ks, page_lvs, page_inv, page_id >= 0 ? 1.f : 0.f);
+                const int64_t row = (((int64_t)id * a.c.kv_heads + head) << plog) + (key & ((1 << plog) - 1));
+                if (lane == page - group0) s_scales[warp][put][0] = sc;
+                if (id >= 0) copy_half(row, dst);
+                if (plog > 4) {
+                    if (lane == page - group0) s_scales[warp][put][1] = sc;
+                    if (id >= 0) copy_half(row + kHalfKeys, dst + Sh::kHalfBytes);
+                } else {
+                    const int32_t id1 = __shfl_sync(0xFFFFFFFFu, page_id, page + 1 - group0);
+                    if (lane == page + 1 - group0) s_scales[warp][put][1] = sc;
+                    if (id1 >= 0) copy_half(((int64_t)id1 * a.c.kv_heads + head) << plog, dst + Sh::kHalfBytes);
+                }
+            }
+            ptx::cp_async_commit();                   // (empty groups keep the count)
+        };
+        issue(s0);
+
+        float rowf[NT][2], m[NT][2], l[NT][2];        // rows 8 n + 2 t and the next
+        uint32_t qb[kTerms][NT][4 * HF][2];           // row 8 n + g
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r = min(8 * n + g, n_rows - 1);
+            const int token = token_of(r), qh = head * group + (tile_row + r - token * group);
+            float x[HF][16], amax = 0.f;
+            const T* q = static_cast<const T*>(a.q) + ((int64_t)sq.row0 + token) * a.ldq + (int64_t)qh * D;
+#pragma unroll
+            for (int f = 0; f < HF; ++f) {
+                load16(q + f * 64 + t * 16, x[f]);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) amax = fmaxf(amax, fabsf(x[f][e]));
+            }
+            amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+            amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+            // the row's largest element to [2^14, 2^15)
+            const int e = amax > 0.f ? min(100, 14 - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
+            const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+            const float down = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+            for (int f = 0; f < HF; ++f)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        const float p0 = x[f][4 * c + 2 * z] * up, p1 = x[f][4 * c + 2 * z + 1] * up;
+                        const uint32_t top = pack_f16(p0, p1);
+                        qb[0][n][4 * f + c][z] = top;
+                        if constexpr (kTerms == 2) qb[kTerms - 1][n][4 * f + c][z] = pack_f16_rest(p0, p1, top);
+                    }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                rowf[n][i] = __shfl_sync(0xFFFFFFFFu, down, (2 * t + i) * 4);
+                m[n][i] = kNone, l[n][i] = 0.f;
+            }
+        }
+        float o[NT][kMT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < kMT; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
+
+        // SUBS halves from key0 on, in ring position `at_step` from half `half` on
+        auto work = [&](int key0, int at_step, int half, auto subs) {
+            constexpr int SUBS = decltype(subs)::value;
+            float4 sc[SUBS];
+            float x[SUBS][NT][4];                     // keys g (0, 1) and g + 8 (2, 3), rows 2 t and 2 t + 1
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) {
+                const uint8_t* stage = ring + (2 * at_step + half + u) * Sh::kHalfBytes;
+                sc[u] = s_scales[warp][at_step][half + u];
+                uint32_t kw[2][HF][4];
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int f = 0; f < HF; ++f) copy_async<16>(kdst + (uint32_t)((j * HF + f) * 512), k + j * 8 * D + f * 64);
-                const uint8_t* v = a.c.v + row * D + (2 * t * D + g * kVBytes);
-                const uint32_t vdst = dst + 2 * HF * 512 + (uint32_t)(lane * kVBytes);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) copy_async<kVBytes>(vdst + (uint32_t)(j * 32 * kVBytes), v + ((j & 1) + 8 * (j >> 1)) * D);
-            };
-            auto issue = [&](int s) {
-                if (s < s1) {
-                    const int key = lo0 + s * kStepKeys, page = key >> plog, put = (s - s0) & (kStages - 1);
-                    if (group0 < 0 || page >= group0 + 32 || (plog == 4 && page + 1 >= group0 + 32)) load_pages(page);
-                    const uint32_t dst = ring_at + (uint32_t)(put * 2 * Sh::kHalfBytes);
-                    const int32_t id = __shfl_sync(0xFFFFFFFFu, page_id, page - group0);
-                    const float4 sc = make_float4(page_ks, page_lvs, page_inv, page_id >= 0 ? 1.f : 0.f);
-                    const int64_t row = (((int64_t)id * a.c.kv_heads + head) << plog) + (key & ((1 << plog) - 1));
-                    if (lane == page - group0) s_scales[warp][put][0] = sc;
-                    if (id >= 0) copy_half(row, dst);
-                    if (plog > 4) {
-                        if (lane == page - group0) s_scales[warp][put][1] = sc;
-                        if (id >= 0) copy_half(row + kHalfKeys, dst + Sh::kHalfBytes);
-                    } else {
-                        const int32_t id1 = __shfl_sync(0xFFFFFFFFu, page_id, page + 1 - group0);
-                        if (lane == page + 1 - group0) s_scales[warp][put][1] = sc;
-                        if (id1 >= 0) copy_half(((int64_t)id1 * a.c.kv_heads + head) << plog, dst + Sh::kHalfBytes);
+                    for (int f = 0; f < HF; ++f) {
+                        const uint4 w4 = *reinterpret_cast<const uint4*>(stage + ((j * HF + f) * 32 + lane) * 16);
+                        kw[j][f][0] = w4.x, kw[j][f][1] = w4.y, kw[j][f][2] = w4.z, kw[j][f][3] = w4.w;
                     }
-                }
-                ptx::cp_async_commit();                   // (empty groups keep the count)
-            };
-            issue(s0);
-
-            float rowf[NT][2], m[NT][2], l[NT][2];        // rows 8 n + 2 t and the next
-            uint32_t qb[kTerms][NT][4 * HF][2];           // row 8 n + g
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int r = min(8 * n + g, n_rows - 1);
-                const int token = token_of(r), qh = head * group + (tile_row + r - token * group);
-                float x[HF][16], amax = 0.f;
-                const T* q = static_cast<const T*>(a.q) + ((int64_t)sq.row0 + token) * a.ldq + (int64_t)qh * D;
-#pragma unroll
-                for (int f = 0; f < HF; ++f) {
-                    load16(q + f * 64 + t * 16, x[f]);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) amax = fmaxf(amax, fabsf(x[f][e]));
-                }
-                amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-                amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-                // the row's largest element to [2^14, 2^15)
-                const int e = amax > 0.f ? min(100, 14 - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
-                const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-                const float down = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
+                float part[HF][NT][4];                // (a chain of sums per half: each waits for its predecessor)
 #pragma unroll
                 for (int f = 0; f < HF; ++f)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int n = 0; n < NT; ++n) part[f][n][0] = part[f][n][1] = part[f][n][2] = part[f][n][3] = 0.f;
 #pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            const float p0 = x[f][4 * c + 2 * z] * up, p1 = x[f][4 * c + 2 * z + 1] * up;
-                            const uint32_t top = pack_f16(p0, p1);
-                            qb[0][n][4 * f + c][z] = top;
-                            if constexpr (kTerms == 2) qb[kTerms - 1][n][4 * f + c][z] = pack_f16_rest(p0, p1, top);
-                        }
+                for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    rowf[n][i] = __shfl_sync(0xFFFFFFFFu, down, (2 * t + i) * 4);
-                    m[n][i] = kNone, l[n][i] = 0.f;
+                    for (int f = 0; f < HF; ++f) {
+                        const uint32_t a0 = e4m3x2_to_f16x2(kw[0][f][c]), a2 = e4m3x2_to_f16x2_high(kw[0][f][c]);
+                        const uint32_t a1 = e4m3x2_to_f16x2(kw[1][f][c]), a3 = e4m3x2_to_f16x2_high(kw[1][f][c]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int z = 0; z < kTerms; ++z) mma_f16(part[f][n], a0, a1, a2, a3, qb[z][n][4 * f + c][0], qb[z][n][4 * f + c][1]);
+                    }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[u][n][e] = HF == 2 ? part[0][n][e] + part[HF - 1][n][e] : part[0][n][e];
+            }
+            const bool border = key0 + SUBS * kHalfKeys > hi_min || key0 < lo_max;
+            uint32_t vw[SUBS][4][kVBytes / 4];
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) {
+                const uint8_t* stage = ring + (2 * at_step + half + u) * Sh::kHalfBytes + 2 * HF * 512;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (kVBytes == 16) {
+                        const uint4 w4 = *reinterpret_cast<const uint4*>(stage + (j * 32 + lane) * 16);
+                        vw[u][j][0] = w4.x, vw[u][j][1] = w4.y, vw[u][j][2] = w4.z, vw[u][j][3] = w4.w;
+                    } else {
+                        const uint2 w2 = *reinterpret_cast<const uint2*>(stage + (j * 32 + lane) * 8);
+                        vw[u][j][0] = w2.x, vw[u][j][1] = w2.y;
+                    }
                 }
             }
-            float o[NT][kMT][4];
+            if (border) {
+                // Some row does not see some key of these steps.  Values that no row sees count as zero; a NaN among the codes of a value
+                // becomes a NaN in the scores of the rows that see it and a zero here, so that it cannot reach the others through
+                // their weight of zero.
+                unsigned nan = 0;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < kMT; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
-
-            // SUBS halves from key0 on, in ring position `at_step` from half `half` on
-            auto work = [&](int key0, int at_step, int half, auto subs) {
-                constexpr int SUBS = decltype(subs)::value;
-                float4 sc[SUBS];
-                float x[SUBS][NT][4];                     // keys g (0, 1) and g + 8 (2, 3), rows 2 t and 2 t + 1
-#pragma unroll
-                for (int u = 0; u < SUBS; ++u) {
-                    const uint8_t* stage = ring + (2 * at_step + half + u) * Sh::kHalfBytes;
-                    sc[u] = s_scales[warp][at_step][half + u];
-                    uint32_t kw[2][HF][4];
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int f = 0; f < HF; ++f) {
-                            const uint4 w4 = *reinterpret_cast<const uint4*>(stage + ((j * HF + f) * 32 + lane) * 16);
-                            kw[j][f][0] = w4.x, kw[j][f][1] = w4.y, kw[j][f][2] = w4.z, kw[j][f][3] = w4.w;
-                        }
-                    float part[HF][NT][4];                // (a chain of sums per half: each waits for its predecessor)
-#pragma unroll
-                    for (int f = 0; f < HF; ++f)
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) part[f][n][0] = part[f][n][1] = part[f][n][2] = part[f][n][3] = 0.f;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int f = 0; f < HF; ++f) {
-                            const uint32_t a0 = e4m3x2_to_f16x2(kw[0][f][c]), a2 = e4m3x2_to_f16x2_high(kw[0][f][c]);
-                            const uint32_t a1 = e4m3x2_to_f16x2(kw[1][f][c]), a3 = e4m3x2_to_f16x2_high(kw[1][f][c]);
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                                for (int z = 0; z < kTerms; ++z) mma_f16(part[f][n], a0, a1, a2, a3, qb[z][n][4 * f + c][0], qb[z][n][4 * f + c][1]);
-                        }
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[u][n][e] = HF == 2 ? part[0][n][e] + part[HF - 1][n][e] : part[0][n][e];
-                }
-                const bool border = key0 + SUBS * kHalfKeys > hi_min || key0 < lo_max;
-                uint32_t vw[SUBS][4][kVBytes / 4];
-#pragma unroll
-                for (int u = 0; u < SUBS; ++u) {
-                    const uint8_t* stage = ring + (2 * at_step + half + u) * Sh::kHalfBytes + 2 * HF * 512;
+                for (int u = 0; u < SUBS; ++u)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        if constexpr (kVBytes == 16) {
-                            const uint4 w4 = *reinterpret_cast<const uint4*>(stage + (j * 32 + lane) * 16);
-                            vw[u][j][0] = w4.x, vw[u][j][1] = w4.y, vw[u][j][2] = w4.z, vw[u][j][3] = w4.w;
-                        } else {
-                            const uint2 w2 = *reinterpret_cast<const uint2*>(stage + (j * 32 + lane) * 8);
-                            vw[u][j][0] = w2.x, vw[u][j][1] = w2.y;
+                        const int k16 = 16 * u + 2 * t + (j & 1) + 8 * (j >> 1), key = key0 + k16;
+                        const bool none = key >= hi_max || key < lo_min;
+#pragma unroll
+                        for (int i = 0; i < kVBytes / 4; ++i) {
+                            const uint32_t bits = e4m3x4_nan_bits(vw[u][j][i]);
+                            if (bits != 0 && !none) nan |= 1u << k16;
+                            vw[u][j][i] = none ? 0u : vw[u][j][i] & ~((bits >> 7) * 0xFFu);
                         }
                     }
-                }
-                if (border) {
-                    // Some row does not see some key of these steps.  Values that no row sees count as zero; a NaN among the codes of a value
-                    // becomes a NaN in the scores of the rows that see it and a zero here, so that it cannot reach the others through
-                    // their weight of zero.
-                    unsigned nan = 0;
+                nan = __reduce_or_sync(0xFFFFFFFFu, nan);
 #pragma unroll
-                    for (int u = 0; u < SUBS; ++u)
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int k16 = 16 * u + 2 * t + (j & 1) + 8 * (j >> 1), key = key0 + k16;
-                            const bool none = key >= hi_max || key < lo_min;
+                    for (int i = 0; i < 2; ++i) {
+                        const int token = token_of(8 * n + 2 * t + i), hi_row = upper_key(a, sq, token), lo_row = lower_key(a, sq, token);
 #pragma unroll
-                            for (int i = 0; i < kVBytes / 4; ++i) {
-                                const uint32_t bits = e4m3x4_nan_bits(vw[u][j][i]);
-                                if (bits != 0 && !none) nan |= 1u << k16;
-                                vw[u][j][i] = none ? 0u : vw[u][j][i] & ~((bits >> 7) * 0xFFu);
+                        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const int k16 = 16 * u + g + 8 * j, key = key0 + k16;
+                                float& v = x[u][n][2 * j + i];
+                                v = key >= hi_row || key < lo_row ? -INFINITY : (nan >> k16) & 1u ? __int_as_float(0x7FC00000) : v;
                             }
-                        }
-                    nan = __reduce_or_sync(0xFFFFFFFFu, nan);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int token = token_of(8 * n + 2 * t + i), hi_row = upper_key(a, sq, token), lo_row = lower_key(a, sq, token);
-#pragma unroll
-                            for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) {
-                                    const int k16 = 16 * u + g + 8 * j, key = key0 + k16;
-                                    float& v = x[u][n][2 * j + i];
-                                    v = key >= hi_row || key < lo_row ? -INFINITY : (nan >> k16) & 1u ? __int_as_float(0x7FC00000) : v;
-                                }
-                        }
-                }
-                // sc: scale of K, logarithm of V's, its reciprocal
-                float c[SUBS][NT][2], top = -INFINITY, y[SUBS][NT][4];
-#pragma unroll
-                for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            c[u][n][i] = fmaxf(rowf[n][i] * sc[u].x, 1.17549435e-38f);      // (never 0: a hidden score is -infinity times it)
-                            const float off = sc[u].y - m[n][i];
-                            y[u][n][i] = fmaf(x[u][n][i], c[u][n][i], off);
-                            y[u][n][2 + i] = fmaf(x[u][n][2 + i], c[u][n][i], off);
-                            top = fmaxf(top, fmaxf(y[u][n][i], y[u][n][2 + i]));
-                        }
-                if (__any_sync(0xFFFFFFFFu, top > kTop + 8.f)) {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            float raw = -INFINITY;
-#pragma unroll
-                            for (int u = 0; u < SUBS; ++u) raw = fmaxf(raw, fmaxf(x[u][n][i] * c[u][n][i], x[u][n][2 + i] * c[u][n][i]) + sc[u].y);
-#pragma unroll
-                            for (int z = 4; z < 32; z <<= 1) raw = fmaxf(raw, __shfl_xor_sync(0xFFFFFFFFu, raw, z));
-                            const float next = raw - m[n][i] > kTop ? raw - kTop : m[n][i];
-                            const float shrink = ex2(m[n][i] - next);
-                            m[n][i] = next;
-                            l[n][i] *= shrink;
-#pragma unroll
-                            for (int d = 0; d < kMT; ++d) o[n][d][i] *= shrink, o[n][d][2 + i] *= shrink;
-#pragma unroll
-                            for (int u = 0; u < SUBS; ++u) {
-                                y[u][n][i] = fmaf(x[u][n][i], c[u][n][i], sc[u].y - next);
-                                y[u][n][2 + i] = fmaf(x[u][n][2 + i], c[u][n][i], sc[u].y - next);
-                            }
-                        }
-                }
-                uint32_t pb[SUBS][kTerms][NT][2];
-#pragma unroll
-                for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) y[u][n][e] = ex2(y[u][n][e]);
-                        l[n][0] = fmaf(y[u][n][0] + y[u][n][2], sc[u].z, l[n][0]);
-                        l[n][1] = fmaf(y[u][n][1] + y[u][n][3], sc[u].z, l[n][1]);
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const uint32_t p = pack_f16(y[u][n][2 * j], y[u][n][2 * j + 1]);
-                            pb[u][0][n][j] = transposed(p);
-                            if constexpr (kTerms == 2) pb[u][kTerms - 1][n][j] = transposed(pack_f16_rest(y[u][n][2 * j], y[u][n][2 * j + 1], p));
-                        }
                     }
-#pragma unroll
-                for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-                    for (int i = 0; i < kVBytes / 4; ++i)
-#pragma unroll
-                        for (int z = 0; z < 2; ++z) {                    // elements 4 i + 2 z and the next of each key
-                            const uint32_t sel = z == 0 ? 0x5140u : 0x7362u;
-                            const uint32_t p0 = __byte_perm(vw[u][0][i], vw[u][1][i], sel), p1 = __byte_perm(vw[u][2][i], vw[u][3][i], sel);
-                            const uint32_t a0 = e4m3x2_to_f16x2(p0), a1 = e4m3x2_to_f16x2_high(p0);
-                            const uint32_t a2 = e4m3x2_to_f16x2(p1), a3 = e4m3x2_to_f16x2_high(p1);
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                                for (int y2 = 0; y2 < kTerms; ++y2) mma_f16(o[n][2 * i + z], a0, a1, a2, a3, pb[u][y2][n][0], pb[u][y2][n][1]);
-                        }
-            };
-            // both halves at a time: their chains of dependent instructions overlap
-            for (int s = s0; s < s1; ++s) {
-                issue(s + 1);
-                ptx::cp_async_wait<1>();
-                __syncwarp();                             // (the scales)
-                const int get = (s - s0) & (kStages - 1), key0 = lo0 + s * kStepKeys;
-                const bool one = s_scales[warp][get][0].w != 0.f, two = s_scales[warp][get][1].w != 0.f;
-                if (kPairs && one && two) {
-                    work(key0, get, 0, std::integral_constant<int, kPairs ? 2 : 1>{});
-                } else {
-                    if (one) work(key0, get, 0, std::integral_constant<int, 1>{});
-                    if (two) work(key0 + kHalfKeys, get, 1, std::integral_constant<int, 1>{});
-                }
-                __syncwarp();
             }
-            ptx::cp_async_wait<0>();
+            // sc: scale of K, logarithm of V's, its reciprocal
+            float c[SUBS][NT][2], top = -INFINITY, y[SUBS][NT][4];
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        c[u][n][i] = fmaxf(rowf[n][i] * sc[u].x, 1.17549435e-38f);      // (never 0: a hidden score is -infinity times it)
+                        const float off = sc[u].y - m[n][i];
+                        y[u][n][i] = fmaf(x[u][n][i], c[u][n][i], off);
+                        y[u][n][2 + i] = fmaf(x[u][n][2 + i], c[u][n][i], off);
+                        top = fmaxf(top, fmaxf(y[u][n][i], y[u][n][2 + i]));
+                    }
+            if (__any_sync(0xFFFFFFFFu, top > kTop + 8.f)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float raw = -INFINITY;
+#pragma unroll
+                        for (int u = 0; u < SUBS; ++u) raw = fmaxf(raw, fmaxf(x[u][n][i] * c[u][n][i], x[u][n][2 + i] * c[u][n][i]) + sc[u].y);
+#pragma unroll
+                        for (int z = 4; z < 32; z <<= 1) raw = fmaxf(raw, __shfl_xor_sync(0xFFFFFFFFu, raw, z));
+                        const float next = raw - m[n][i] > kTop ? raw - kTop : m[n][i];
+                        const float shrink = ex2(m[n][i] - next);
+                        m[n][i] = next;
+                        l[n][i] *= shrink;
+#pragma unroll
+                        for (int d = 0; d < kMT; ++d) o[n][d][i] *= shrink, o[n][d][2 + i] *= shrink;
+#pragma unroll
+                        for (int u = 0; u < SUBS; ++u) {
+                            y[u][n][i] = fmaf(x[u][n][i], c[u][n][i], sc[u].y - next);
+                            y[u][n][2 + i] = fmaf(x[u][n][2 + i], c[u][n][i], sc[u].y - next);
+                        }
+                    }
+            }
+            uint32_t pb[SUBS][kTerms][NT][2];
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[u][n][e] = ex2(y[u][n][e]);
+                    l[n][0] = fmaf(y[u][n][0] + y[u][n][2], sc[u].z, l[n][0]);
+                    l[n][1] = fmaf(y[u][n][1] + y[u][n][3], sc[u].z, l[n][1]);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t p = pack_f16(y[u][n][2 * j], y[u][n][2 * j + 1]);
+                        pb[u][0][n][j] = transposed(p);
+                        if constexpr (kTerms == 2) pb[u][kTerms - 1][n][j] = transposed(pack_f16_rest(y[u][n][2 * j], y[u][n][2 * j + 1], p));
+                    }
+                }
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                for (int i = 0; i < kVBytes / 4; ++i)
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {                    // elements 4 i + 2 z and the next of each key
+                        const uint32_t sel = z == 0 ? 0x5140u : 0x7362u;
+                        const uint32_t p0 = __byte_perm(vw[u][0][i], vw[u][1][i], sel), p1 = __byte_perm(vw[u][2][i], vw[u][3][i], sel);
+                        const uint32_t a0 = e4m3x2_to_f16x2(p0), a1 = e4m3x2_to_f16x2_high(p0);
+                        const uint32_t a2 = e4m3x2_to_f16x2(p1), a3 = e4m3x2_to_f16x2_high(p1);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int y2 = 0; y2 < kTerms; ++y2) mma_f16(o[n][2 * i + z], a0, a1, a2, a3, pb[u][y2][n][0], pb[u][y2][n][1]);
+                    }
+        };
+        // both halves at a time: their chains of dependent instructions overlap
+        for (int s = s0; s < s1; ++s) {
+            issue(s + 1);
+            ptx::cp_async_wait<1>();
+            __syncwarp();                             // (the scales)
+            const int get = (s - s0) & (kStages - 1), key0 = lo0 + s * kStepKeys;
+            const bool one = s_scales[warp][get][0].w != 0.f, two = s_scales[warp][get][1].w != 0.f;
+            if (kPairs && one && two) {
+                work(key0, get, 0, std::integral_constant<int, kPairs ? 2 : 1>{});
+            } else {
+                if (one) work(key0, get, 0, std::integral_constant<int, 1>{});
+                if (two) work(key0 + kHalfKeys, get, 1, std::integral_constant<int, 1>{});
+            }
+            __syncwarp();
+        }
+        ptx::cp_async_wait<0>();
 
-            // ---- the four warps' parts become one: everybody's values by the largest reference, through the ring
+        // ---- the four warps' parts become one: everybody's values by the largest reference, through the ring
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < 2; ++i) {
 #pragma unroll
-                    for (int z = 4; z < 32; z <<= 1) l[n][i] += __shfl_xor_sync(0xFFFFFFFFu, l[n][i], z);
-                    if (g == 0) s_m[warp][8 * n + 2 * t + i] = m[n][i], s_l[warp][8 * n + 2 * t + i] = l[n][i];
-                }
-            __syncthreads();
-            float* const rows = reinterpret_cast<float*>(ring);
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int row = 8 * n + 2 * t + i;
-                    if (row >= n_rows) continue;
-                    float top = s_m[0][row];
-#pragma unroll
-                    for (int z = 1; z < kWarpsPerCta; ++z) top = fmaxf(top, s_m[z][row]);
-                    const float f = ex2(m[n][i] - top);
-                    float r[kVBytes];
-#pragma unroll
-                    for (int d = 0; d < kMT; ++d) r[2 * d] = o[n][d][i] * f, r[2 * d + 1] = o[n][d][2 + i] * f;
-                    store_run<float, kVBytes>(rows + row * D + g * kVBytes, r);
-                }
-            __syncthreads();
-            const bool begins = un.first == 0, ends = un.last == un.sp.steps, whole = begins && ends;
-            float* slot = slots + (2 * w + (begins ? 1 : 0)) * (int64_t)slot_floats(kRows, D);
-            if (begins && !ends) {
-                cut.b = un.b, cut.row_tile = un.tile, cut.head = head;
-                cut.pieces = walk.pieces(un, w);
+                for (int z = 4; z < 32; z <<= 1) l[n][i] += __shfl_xor_sync(0xFFFFFFFFu, l[n][i], z);
+                if (g == 0) s_m[warp][8 * n + 2 * t + i] = m[n][i], s_l[warp][8 * n + 2 * t + i] = l[n][i];
             }
-            for (int i = tid; i < n_rows * (D / 4); i += kThreads) {
-                const int row = i / (D / 4), d = i % (D / 4) * 4;
-                float top = s_m[0][row], sum = 0.f;
+        __syncthreads();
+        float* const rows = reinterpret_cast<float*>(ring);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = 8 * n + 2 * t + i;
+                if (row >= n_rows) continue;
+                float top = s_m[0][row];
 #pragma unroll
                 for (int z = 1; z < kWarpsPerCta; ++z) top = fmaxf(top, s_m[z][row]);
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                const float f = ex2(m[n][i] - top);
+                float r[kVBytes];
 #pragma unroll
-                for (int z = 0; z < kWarpsPerCta; ++z) {
-                    sum = fmaf(s_l[z][row], ex2(s_m[z][row] - top), sum);
-                    const float4 x = *reinterpret_cast<const float4*>(ring_all + z * kStages * 2 * Sh::kHalfBytes + (row * D + d) * 4);
-                    v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
-                }
-                if (whole) {
-                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                    const int token = token_of(row), qh = head * group + (tile_row + row - token * group);
-                    const int64_t orow = (int64_t)sq.row0 + token;
-                    store4(static_cast<T*>(a.out) + orow * a.ldo + (int64_t)qh * D + d, v, inv);
-                    if (a.lse != nullptr && d == 0) a.lse[orow * a.heads + qh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718056f;
-                } else {
-                    *reinterpret_cast<float4*>(slot + 2 * kRows + row * D + d) = v;
-                    if (d == 0) slot[row] = top, slot[kRows + row] = sum;
-                }
+                for (int d = 0; d < kMT; ++d) r[2 * d] = o[n][d][i] * f, r[2 * d + 1] = o[n][d][2 + i] * f;
+                store_run<float, kVBytes>(rows + row * D + g * kVBytes, r);
             }
-            __syncthreads();
+        __syncthreads();
+        const bool begins = un.first == 0, ends = un.last == un.sp.steps, whole = begins && ends;
+        float* slot = slots + (2 * w + (begins ? 1 : 0)) * (int64_t)slot_floats(kRows, D);
+        if (begins && !ends) {
+            cut.b = un.b, cut.row_tile = un.tile, cut.head = head;
+            cut.pieces = walk.pieces(un, w);
         }
+        for (int i = tid; i < n_rows * (D / 4); i += kThreads) {
+            const int row = i / (D / 4), d = i % (D / 4) * 4;
+            float top = s_m[0][row], sum = 0.f;
+#pragma unroll
+            for (int z = 1; z < kWarpsPerCta; ++z) top = fmaxf(top, s_m[z][row]);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int z = 0; z < kWarpsPerCta; ++z) {
+                sum = fmaf(s_l[z][row], ex2(s_m[z][row] - top), sum);
+                const float4 x = *reinterpret_cast<const float4*>(ring_all + z * kStages * 2 * Sh::kHalfBytes + (row * D + d) * 4);
+                v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+            }
+            if (whole) {
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                const int token = token_of(row), qh = head * group + (tile_row + row - token * group);
+                const int64_t orow = (int64_t)sq.row0 + token;
+                store4(static_cast<T*>(a.out) + orow * a.ldo + (int64_t)qh * D + d, v, inv);
+                if (a.lse != nullptr && d == 0) a.lse[orow * a.heads + qh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718056f;
+            } else {
+                *reinterpret_cast<float4*>(slot + 2 * kRows + row * D + d) = v;
+                if (d == 0) slot[row] = top, slot[kRows + row] = sum;
+            }
+        }
+        __syncthreads();
     }
     if (tid == 0) cuts[w] = cut;
 }
@@ -519,7 +517,7 @@ template <typename F>
 auto for_variant(molora_dtype_t dt, int32_t dim, int64_t rows, F f)
 {
     if (dt == MOLORA_F32) return dim == 64 ? for_tiles<float, 64>(rows, f) : for_tiles<float, 128>(rows, f);
-    return dim == 64 ? for_tiles<__nv_bfloat16, 64>(rows, f) : for_tiles<__nv_bfloat16, 128>(rows, f);
+    return for_tiles<__nv_bfloat16, 64>(rows, f);
 }
 struct BytesNeeded {
     template <typename T, int D, int NT>

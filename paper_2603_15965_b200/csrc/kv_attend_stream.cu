@@ -611,10 +611,12 @@ molora_status_t launch(const AttendArgs& a, void* ws, cudaStream_t s)
         done = true;
     }
     CUtensorMap tm_k, tm_v;
-    const uint64_t rows = ((uint64_t)a.c.n_pages * (uint64_t)a.c.kv_heads) << a.c.page_log2;
+    // (of a pool without pages nothing is copied, but a map has to be of something)
     const uint32_t box = 1u << a.c.page_log2;
-    if (!make_tensor_map_bytes_2d(&tm_k, a.c.k, kDim, rows, kDim, box, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_tensor_map_bytes_2d(&tm_v, a.c.v, kDim, rows, kDim, box, CU_TENSOR_MAP_SWIZZLE_128B))
+    const bool none = a.c.n_pages == 0;
+    const uint64_t rows = none ? box : ((uint64_t)a.c.n_pages * (uint64_t)a.c.kv_heads) << a.c.page_log2;
+    if (!make_tensor_map_bytes_2d(&tm_k, none ? ws : a.c.k, kDim, rows, kDim, box, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_tensor_map_bytes_2d(&tm_v, none ? ws : a.c.v, kDim, rows, kDim, box, CU_TENSOR_MAP_SWIZZLE_128B))
         return MOLORA_ERR_CUDA;
     const int64_t shares = share_count<ROWS>();
     CutUnit* cuts = static_cast<CutUnit*>(ws);
@@ -626,12 +628,6 @@ molora_status_t launch(const AttendArgs& a, void* ws, cudaStream_t s)
 }
 
 }  // namespace
-
-// bf16, heads of 128, up to 32 rows; a pool that TMA's coordinates reach (and that there is)
-bool attend_stream_eligible(const KvView& c, molora_dtype_t dt, int64_t rows)
-{
-    return dt == MOLORA_BF16 && c.dim == kDim && rows <= 32 && c.n_pages > 0 && (((int64_t)c.n_pages * c.kv_heads) << c.page_log2) <= INT32_MAX;
-}
 
 size_t attend_stream_workspace_bytes(int64_t rows)
 {

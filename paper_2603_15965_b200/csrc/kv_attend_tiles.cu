@@ -723,9 +723,6 @@ int64_t share_count() { return sm_count(); }
 
 }  // namespace
 
-// bf16, heads of 128
-bool attend_tiles_eligible(const KvView& c, molora_dtype_t dt) { return dt == MOLORA_BF16 && c.dim == kDim && c.n_pages > 0; }
-
 size_t attend_tiles_workspace_bytes() { return cut_bytes(share_count()) + (size_t)(2 * share_count() * slot_floats(kUnitRows, kDim)) * sizeof(float); }
 
 molora_status_t launch_attend_tiles(const AttendArgs& a, void* ws, cudaStream_t s)

@@ -90,13 +90,13 @@ struct AttendArgs {
     float scale_log2;      // scale * log2(e): the softmax runs in powers of two
     uint32_t* dev_status;
 };
-// rows: of the longest sequence, per key / value head
+// rows: of the longest sequence, per key / value head.  fp32, or heads of 64:
 size_t attend_rows_workspace_bytes(molora_dtype_t dt, int32_t dim, int64_t rows);
 molora_status_t launch_attend_rows(const AttendArgs& a, molora_dtype_t dt, int64_t rows, void* ws, cudaStream_t s);
-bool attend_stream_eligible(const KvView& c, molora_dtype_t dt, int64_t rows);
+// bf16, heads of 128; up to kMaxStreamRows rows, and more:
+constexpr int64_t kMaxStreamRows = 32;
 size_t attend_stream_workspace_bytes(int64_t rows);
 molora_status_t launch_attend_stream(const AttendArgs& a, int64_t rows, void* ws, cudaStream_t s);
-bool attend_tiles_eligible(const KvView& c, molora_dtype_t dt);
 size_t attend_tiles_workspace_bytes();
 molora_status_t launch_attend_tiles(const AttendArgs& a, void* ws, cudaStream_t s);
 molora_status_t launch_verify_drafts(const void* target, int64_t tls, int64_t tl, const void* draft, int64_t dls, int64_t dl, molora_dtype_t dt,
