@@ -370,7 +370,7 @@ molora_status_t molora_route_hotset(const int32_t *ids, const int32_t *adapter_i
  *   scales  k_scale, v_scale: device fp32 [n_pages][kv_heads], one for each BLOCK of `page` tokens of one head:
  *           value = code * scale.  molora_kv_append writes powers of two; molora_kv_attend takes any positive finite scale
  *           (those of v are read as if clamped to [2^-100, 2^100]).
- * page is 16, 32, 64 or 128 tokens, dim 64 or 128, kv_heads >= 1.
+ * page is 16, 32, 64 or 128 tokens, dim 64 or 128, kv_heads >= 1, n_pages * kv_heads * page < 2^31.
  * The sequences of a step:
  *   page_table  device int32 [B][max_pages], row pitch ld_table: token p of sequence b is row p % page of page
  *               page_table[b][p / page]; entries behind a sequence's last token are not read
@@ -424,8 +424,9 @@ molora_status_t molora_kv_append(const molora_kv_cache_t *cache, const molora_se
  *         choice of kernel goes by it, results do not depend on it
  * ws, ws_bytes  device scratch of at least molora_kv_attend_workspace_bytes(...) bytes, 256-byte aligned, need not be cleared;
  *         calls that share it must not overlap on the GPU
- * Scores and sums are fp32, q and the codes enter the tensor cores exactly (fp16 with the rows of q scaled by powers of
- * two; fp32 q as two terms, 22 bits), weights rounded to fp16 (two terms for fp32), one rounding to dt at the end.
+ * Scores and sums are fp32; q (its rows scaled by powers of two) and the codes enter the tensor cores exactly, fp32 q in 22
+ * bits; weights are rounded to 11 bits (22 for fp32) and, below 2^-14 of a row's largest (bf16, heads of 128, up to 32
+ * rows), to steps of 2^-24 of it; one rounding to dt at the end.
  * Tokens that a row does not see leave no trace in it, whatever their codes; a NaN among the codes of a token makes the rows NaN that do
  * see it. */
 size_t molora_kv_attend_workspace_bytes(molora_dtype_t dt, int32_t heads, int32_t kv_heads, int32_t dim, int64_t max_tokens);

@@ -2,7 +2,7 @@
 //
 // A row of a sequence is (new token, query head of the group that shares a key / value head); ROWS consecutive rows, one key /
 // value head and the keys that they see are a UNIT.  The units' keys, cut into steps of KEYS, form one long list; every CTA of the
-// grid takes an equal, contiguous share of it, whatever the lengths of the sequences.  A unit that lies inside one share is written at
+// grid (or each of its workers) takes an equal, contiguous share of it, whatever the lengths of the sequences.  A unit that lies inside one share is written at
 // once; one that is cut leaves its pieces (sum, reference, weighted values, all fp32) in the workspace, and a second kernel joins
 // them in the order of the keys: results do not depend on timing.
 #pragma once

@@ -21,7 +21,9 @@
 // that the weights handed to the tensor cores have the size of what they contribute, and the sum takes it off again.
 // Weights are at most 2^15 (fp16 normal down to 2^-29 of a row's largest): the reference of a row moves only when a score is
 // 2^8 over the weight it gave its largest, and then everything is rescaled.
-// What bounds it: the codes, 2 D bytes per (key, key / value head), from HBM.
+// What bounds it: the codes, 2 D bytes per (key, key / value head), from HBM: 256 sequences of 3 to 4095 tokens, 16 heads over 8 of 64, take 123 us
+// in bf16 and 132 in fp32 (4.3 and 4.0 TB/s), of 128 in fp32 268 us; for prompts the tensor instruction (8 of 1024 tokens, 32 heads of 64: 480 and
+// 717 us), which reaches a quarter of what tcgen05 would give.
 #include <type_traits>
 
 #include "kv_attend.cuh"

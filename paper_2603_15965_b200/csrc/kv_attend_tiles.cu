@@ -2,19 +2,24 @@
 //
 // A unit is 256 consecutive rows of a sequence (new token, query head of the group that shares a key / value head) in two tiles of 128, one key /
 // value head and the keys that they see; here the tensor cores are the bound, so the codes of K and V are brought to fp16 once for both tiles.
-//   S_t = Q_t K^T  [128 rows x 128 keys]       A = Q_t in shared memory, B = K in shared memory
+//   S_t = Q_t K^T  [128 rows x 64 keys]        A = Q_t in shared memory, B = K in shared memory
 //   O_t += P_t V   [128 rows x 128 elements]   A = P_t in TMEM (fp16, in the place of S_t), B = V in shared memory, read across (MN-major)
-//   warps 0-7, 8-15 two threads per row of tile 0 and 1, each with half of the keys: q to fp16 by a power of two, weights of a tile (S_t -> P_t),
+//   warps 0-7, 8-15 two threads per row of tile 0 and 1, each with 32 of a step's 64 keys: q to fp16 by a power of two, weights (S_t -> P_t),
 //                   the sum, the result.  The reference of a row moves when a score is 2^8 over the weight that its largest was given, and then
-//                   O_t is rescaled; whether it does is all that the two ask each other, tile by tile.  (One thread per row, 128 keys one after the other at the
-//                   latencies of one warp per scheduler, took 3500 cycles a tile.)
+//                   O_t is rescaled; whether it does is all that the two ask each other, step by step.  (One thread per row, 128 keys one after
+//                   the other at the latencies of one warp per scheduler, took 3500 cycles per 128 keys.)
 //   warps 16-19     codes -> fp16, two tiles of 128 keys of K and of V ahead, the codes of the next tile on their way in registers
-//   warp 20         the MMAs: O_0 S_0 O_1 S_1 ... -- while the weights of one tile are worked out, the other has the tensor cores
-//   warp 21         units, pages and scales, into queues: what depends on one another there is waited for long before it is needed
-// S_t of the next keys is asked for right behind O_t of the last, which is the last to read P_t: the tensor cores work in the order of issue.
-// TMEM: S_0 S_1 O_0 O_1, 128 columns each.  Shared memory: Q 64 KB, K and V 2 x 32 KB each.
+//   warps 20, 21    the MMAs of tile 0 and of tile 1: O of a step, then S of the step after the next, so that the scores of the next step are there
+//                   when the weights of this one are done.  (One warp for both: 8 % slower; steps of 128 keys, whose S had to wait for all of the
+//                   last P: 8 % slower; S of 64 keys costs the tensor cores 56 cycles per 16 elements where 128 keys cost 64.)
+//   warp 22         units, pages and scales, into queues: what depends on one another there is waited for long before it is needed
+// The tensor cores work in the order of issue: O, which reads P, is through before S is written in its place.
+// TMEM: S_0 S_1 O_0 O_1, 128 columns each, S for even and odd steps.  Shared memory: Q 64 KB, K and V 2 x 32 KB each.
 // Shares, pieces and the join as in kv_attend.cuh, but with the steps that each tile of rows really sees.
-// What bounds it: per 128 keys 4 x 512 cycles of the tensor cores, and as many of the special-function units (256 x 128 exponentials).
+// What bounds it, measured with 2048 rows of 32 heads behind 14336 tokens (640 us, 0.8 PFLOP/s): no unit alone.  Per 128 keys it takes 5200 cycles,
+// of which the tensor cores are busy 54 %, the special-function units 41 % (256 x 128 exponentials), the schedulers 60 %; taking out the
+// exponentials or seven eighths of the MMAs gains 4 % each, both together with the codes 11 %.  With short prompts (8 of 1024 tokens: 174 us) it
+// is what a unit costs by itself, 13,000 cycles, 5500 of them for q.
 #include "kv_attend.cuh"
 #include "pipeline.cuh"
 
