@@ -172,6 +172,13 @@ __device__ __forceinline__ void cut_shares(const AttendArgs& a, int64_t first_sh
     __syncthreads();
 }
 
+// A kernel's columns of TMEM, by one warp: after the wait for its predecessor, which may hold them, and before its successor may start.
+__device__ __forceinline__ void take_tmem(uint32_t* base, uint32_t columns)
+{
+    ptx::tmem_alloc(ptx::smem_u32(base), columns);
+    ptx::tmem_relinquish();
+}
+
 // scales of v outside [2^-100, 2^100] are read as its ends
 __device__ __forceinline__ float clamped_scale(float v) { return fminf(fmaxf(v, 7.8886090522e-31f), 1.2676506002e30f); }
 

@@ -179,10 +179,7 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
             *reinterpret_cast<uint4*>(smem_raw + (first - raw) + w * C::kWorkerBytes + C::kQAt + i * 16) = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
     grid_dependency_wait();
-    if (warp == 1) {
-        tmem_alloc(smem_u32(&s_tmem_base), C::kTmemCols);
-        tmem_relinquish();
-    }
+    if (warp == 1) take_tmem(&s_tmem_base, C::kTmemCols);
     const int group = a.heads / a.c.kv_heads, plog = a.c.page_log2;
     cut_shares<C::kThreads, W>(a, (int64_t)blockIdx.x * W, (int64_t)gridDim.x * W, kMinShare, s_start,
                                [&](const Sequence& sq) { return steps_of<ROWS, kKeys, C::kUnitCost>(a, sq, group); });

@@ -233,10 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_mbar_init();
     }
     grid_dependency_wait();
-    if (warp == kMmaWarp0) {
-        tmem_alloc(smem_u32(&ctrl.tmem_base), kTmemCols);
-        tmem_relinquish();
-    }
+    if (warp == kMmaWarp0) take_tmem(&ctrl.tmem_base, kTmemCols);
     cut_shares<kThreads, 1>(a, blockIdx.x, gridDim.x, kMinShare, &s_start, [&](const Sequence& sq) {
         int64_t steps = 0;
         const int tiles = row_tiles(sq, group);
