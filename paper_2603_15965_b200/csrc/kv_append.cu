@@ -5,7 +5,7 @@
 // scale.  Older tokens of the block are touched only when the scale has to grow, which a power of two does seldom and, for e4m3
 // codes, without rounding anything but values that become subnormal.
 //   grid.x   runs of `run` consecutive rows; a CTA takes the pieces (rows of one sequence inside one page) that begin in its run
-//   grid.y   groups of kHeadsPerCta heads of k, of v, of q
+//   grid.y   groups of heads of k, of v, of q
 // Sines and cosines are computed once per piece, into shared memory, in turns: p * f / 2 pi in 64 bits, reduced to half a turn, then
 // sinpi / cospi in fp32.  A thread's unit is 16 elements of a row -- two 8-element vectors that the rotation pairs, or that lie side by
 // side -- and stays the same for every head of the group; the next head's vectors are on their way while a head is worked on (asked
@@ -16,7 +16,6 @@
 namespace molora {
 namespace {
 
-constexpr int kHeadsPerCta = 8;
 constexpr int kMaxThreads = 1024;      // a page of 128 tokens of 128 elements
 
 // the two vectors of a unit as they lie in memory
@@ -49,7 +48,7 @@ struct AppendArgs {
     const void *k, *v, *q;
     void* q_out;
     int64_t ldk, ldv, ldq, ldqo;
-    int32_t heads, rotary, interleaved, run, k_groups, dim;
+    int32_t heads, rotary, interleaved, run, per_cta, k_groups, dim;      // (per_cta, k_groups: heads of a group, groups of k)
     const float* inv_freq;
     uint32_t* dev_status;
 };
@@ -105,12 +104,18 @@ struct Unit {
 
 __device__ __forceinline__ float finite_amax(const float* x, float m)
 {
+    float t = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float v = fabsf(x[i]);
-        m = fmaxf(m, v <= 3.402823466e38f ? v : 0.f);        // infinities and NaN have no say
+    for (int i = 0; i < 16; ++i) t = fmaxf(t, fabsf(x[i]));  // (NaN has no say)
+    if (t > 3.402823466e38f) {                               // nor have infinities
+        t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float v = fabsf(x[i]);
+            t = fmaxf(t, v <= 3.402823466e38f ? v : 0.f);
+        }
     }
-    return m;
+    return fmaxf(m, t);
 }
 
 __device__ __forceinline__ void store_codes(uint8_t* row, const Unit& u, const float* x, float inv)
@@ -168,8 +173,8 @@ __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_con
     // the group of heads
     const int g = (int)blockIdx.y;
     const int kind = g < a.k_groups ? 0 : g < 2 * a.k_groups ? 1 : 2;                  // k, v, q
-    const int h0 = (kind == 0 ? g : kind == 1 ? g - a.k_groups : g - 2 * a.k_groups) * kHeadsPerCta;
-    const int h1 = min(h0 + kHeadsPerCta, kind == 2 ? a.heads : a.c.kv_heads);
+    const int h0 = (kind == 0 ? g : kind == 1 ? g - a.k_groups : g - 2 * a.k_groups) * a.per_cta;
+    const int h1 = min(h0 + a.per_cta, kind == 2 ? a.heads : a.c.kv_heads);
     const T* src = static_cast<const T*>(kind == 0 ? a.k : kind == 1 ? a.v : a.q);
     const int64_t ld = kind == 0 ? a.ldk : kind == 1 ? a.ldv : a.ldq;
     uint8_t* codes = kind == 0 ? a.c.k : a.c.v;
@@ -312,7 +317,7 @@ molora_status_t launch(const AppendArgs& a, cudaStream_t s)
     // powers of two: single tokens, a warp for four heads of 128; drafts; one unit per thread of the largest piece there can be
     const int most = (1 << a.c.page_log2) * (a.dim >> 4);
     const int threads = a.run == 1 ? 128 : a.run < 16 ? 256 : max(512, min(kMaxThreads, most));
-    const int groups = 2 * a.k_groups + ceil_div(a.heads, kHeadsPerCta);
+    const int groups = 2 * a.k_groups + ceil_div(a.heads, a.per_cta);
     const dim3 grid((unsigned)ceil_div64(a.N, a.run), (unsigned)groups);
     const size_t turns = (size_t)min((int64_t)(1 << a.c.page_log2), a.N) * (a.rotary >> 1) * sizeof(float2);      // at most 64 KB
     static bool ready[kMaxDevices] = {};
@@ -338,10 +343,14 @@ molora_status_t launch_kv_append(const KvView& c, molora_dtype_t dt, int64_t N, 
     a.heads = heads, a.rotary = rotary, a.interleaved = interleaved, a.dim = c.dim;
     a.inv_freq = inv_freq;
     a.dev_status = dev_status;
-    a.k_groups = ceil_div(c.kv_heads, kHeadsPerCta);
     // Rows per CTA: as many as a sequence has on average, a page at most.  A CTA in whose run no piece begins costs its search (2 us, and
     // with runs of 16 rows three of four have none where whole pages of 64 are written), one in whose run many begin takes them in turn.
     a.run = (int32_t)max((int64_t)1, min((int64_t)(1 << c.page_log2), N / c.B));
+    // Heads per CTA: sines and cosines are computed anew by every group, which costs about as much as two heads of 8, so 16 where there are
+    // CTAs enough all the same.
+    a.per_cta = 8;
+    if (ceil_div64(N, a.run) * (2 * ceil_div(c.kv_heads, 16) + ceil_div(heads, 16)) >= 2 * sm_count()) a.per_cta = 16;
+    a.k_groups = ceil_div(c.kv_heads, a.per_cta);
     return dt == MOLORA_F32 ? launch<float>(a, s) : launch<__nv_bfloat16>(a, s);
 }
 
