@@ -66,7 +66,7 @@ struct Unit {
     int token;                 // within the piece
     int off0, off1;
     int kind;                  // 0: not rotated, 1: pairs across the two vectors, 2: neighbours inside each
-    const float4* turn;        // cos, sin, cos, sin of two pairs each
+    const float4* turn;        // cos, sin, cos, sin of two pairs each, `next` apart
     __device__ __forceinline__ Unit(int id, const AppendArgs& a, bool rotate, const float2* turns)
     {
         const int per_token = a.dim >> 4, j = id % per_token;
@@ -76,15 +76,15 @@ struct Unit {
         if (j * 16 < rotary) {
             kind = a.interleaved ? 2 : 1;
             if (!a.interleaved) off0 = j * 8, off1 = j * 8 + rotary / 2;
-            turn = reinterpret_cast<const float4*>(turns + token * (rotary / 2) + j * 8);
+            turn = reinterpret_cast<const float4*>(turns + token * (rotary / 2)) + j;
         }
     }
-    __device__ __forceinline__ void rotate(float* x) const
+    __device__ __forceinline__ void rotate(float* x, int next) const
     {
         if (kind == 0) return;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float4 t = turn[i];
+            const float4 t = turn[i * next];
             if (kind == 1) {
                 turn_pair(x[2 * i], x[8 + 2 * i], t.x, t.y);
                 turn_pair(x[2 * i + 1], x[8 + 2 * i + 1], t.z, t.w);
@@ -163,11 +163,12 @@ __device__ __forceinline__ int sequence_of_row(const int32_t* cu, int B, int64_t
     return base;
 }
 
-template <typename T>
+// WHOLE: there are as many threads as the largest piece has units
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_constant__ AppendArgs a)
 {
     __shared__ float warp_max[kMaxThreads / 32];
-    extern __shared__ __align__(16) float2 turns[];        // [token of the piece][pair]: cosine, sine
+    extern __shared__ __align__(16) float2 turns[];        // cosines, sines: [token of the piece][two pairs of a unit][unit][pair], so that neighbours read neighbours
     ptx::grid_dependency_sync();
     const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31, threads = (int)blockDim.x;
     // the group of heads
@@ -215,7 +216,7 @@ __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_con
         // Threads per head, a power of two: as many as the piece has units, so that several heads are in hand at a time where it is short
         // (what lies inside a warp needs no barrier); a piece of more units than there are threads is gone through twice.
         const int total = count * units;
-        const bool small = total <= threads;
+        const bool small = WHOLE || total <= threads;
         const int sub = small ? 1 << (32 - __clz(max(total - 1, 1))) : threads;
         const bool by_warp = sub <= 32;
         const int mine = tid & (sub - 1), first = h0 + tid / sub, step = threads / sub;
@@ -223,11 +224,11 @@ __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_con
             const int pairs = a.rotary >> 1;
             __syncthreads();                               // (the last piece's are done with)
             for (int z = tid; z < count * pairs; z += threads) {
-                const int token = z / pairs;
-                const double angle = (double)(pos + token) * (double)ptx::ld_dependent(a.inv_freq + (z - token * pairs)) * 0.15915494309189533577;      // 1 / 2 pi
+                const int token = z / pairs, w = z - token * pairs;
+                const double angle = (double)(pos + token) * (double)ptx::ld_dependent(a.inv_freq + w) * 0.15915494309189533577;      // 1 / 2 pi
                 float2 t;
                 sincospif((float)((angle - rint(angle)) * 2.0), &t.y, &t.x);
-                turns[z] = t;
+                turns[token * pairs + ((((w & 7) >> 1) * (pairs >> 3) + (w >> 3)) << 1) + (w & 1)] = t;
             }
             __syncthreads();
         }
@@ -244,7 +245,7 @@ __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_con
             float x[16];
             raw.values(x);
             if (have && h + step < h1) raw.load(row_of(h + step, u), u.off0, u.off1);
-            u.rotate(x);
+            u.rotate(x, a.rotary >> 4);
             if (kind == 2) {
                 auto put = [&](const Unit& v) {
                     T* p = static_cast<T*>(a.q_out) + (i + v.token) * a.ldqo + h * a.dim;
@@ -258,7 +259,7 @@ __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_con
                         Raw<T> w;
                         w.load(row_of(h, v), v.off0, v.off1);
                         w.values(x);
-                        v.rotate(x);
+                        v.rotate(x, a.rotary >> 4);
                         put(v);
                     }
                 continue;
@@ -274,7 +275,7 @@ __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_con
                     float y[16];
                     w.load(row_of(h, v), v.off0, v.off1);
                     w.values(y);
-                    v.rotate(y);
+                    v.rotate(y, a.rotary >> 4);
                     m = finite_amax(y, m);
                 }
             for (int o = min(sub, 32) >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
@@ -299,7 +300,7 @@ __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_con
                     Raw<T> w;
                     w.load(row_of(h, v), v.off0, v.off1);
                     w.values(x);
-                    v.rotate(x);
+                    v.rotate(x, a.rotary >> 4);
                     store_codes(rows + (int64_t)(row0 + v.token) * a.dim, v, x, inv);
                 }
             if (row0 > 0 && scale != old) {
@@ -323,10 +324,12 @@ molora_status_t launch(const AppendArgs& a, cudaStream_t s)
     static bool ready[kMaxDevices] = {};
     bool& done = ready[device_slot()];
     if (!done) {
-        if (cudaFuncSetAttribute(kv_append_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 65536) != cudaSuccess) return MOLORA_ERR_CUDA;
+        if (cudaFuncSetAttribute(kv_append_kernel<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 65536) != cudaSuccess ||
+            cudaFuncSetAttribute(kv_append_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 65536) != cudaSuccess)
+            return MOLORA_ERR_CUDA;
         done = true;
     }
-    return cuda_ok(launch_kernel(kv_append_kernel<T>, grid, dim3((unsigned)threads), turns, s, 1, true, a));
+    return cuda_ok(launch_kernel(threads >= most ? kv_append_kernel<T, true> : kv_append_kernel<T, false>, grid, dim3((unsigned)threads), turns, s, 1, true, a));
 }
 
 }  // namespace
