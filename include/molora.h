@@ -417,7 +417,7 @@ molora_status_t molora_kv_append(const molora_kv_cache_t *cache, const molora_se
  * query head h, reading key / value head h / (heads / kv_heads):
  *     out = sum_j softmax_j(scale * q . K_j) V_j   over j < kv_lens, j <= p if causal, j > p - window if window > 0
  * Rows that see no token get out = 0 and lse = -infinity.
- * q       device [N][heads * dim] of type dt, pitch ldq; out the same, pitch ldo; heads a multiple of kv_heads
+ * q       device [N][heads * dim] of type dt, pitch ldq; out the same, pitch ldo, not overlapping q; heads a multiple of kv_heads
  * lse     device fp32 [N][heads] or NULL: natural logarithm of the softmax's sum
  * window  0, or (causal only) the number of newest tokens that a row sees, itself included
  * max_tokens  the most new tokens that a sequence of this call has, as far as the caller knows (N if it does not); the

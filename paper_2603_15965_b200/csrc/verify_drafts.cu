@@ -6,8 +6,9 @@
 // exchanged through distributed shared memory, and the CTA in which the running sum passes u * total looks at the piece
 // of the warp in which it does once more (from L2), a short run per thread.  So the vocabulary is read once, and the order of
 // summation does not matter to more than the last bits of 64.
-// What bounds it: the two rows, 8 bytes per word of the vocabulary in fp32 (64 sequences, 160,000 words, five drafts: 21.5 us for the
-// 68 MB that these acceptances ask for, 3.2 TB/s); the chain of dependent reads and the exchange take 6 us of any call.
+// What bounds it: the two rows, 8 bytes per word of the vocabulary in fp32 (64 sequences, 160,000 words, five drafts: 21.5 us, 11 of
+// them for the 68 MB that these acceptances ask for, at 6.2 TB/s); the dependent reads in front, the exchange and the second look take the
+// rest.  (Differences in 32 bits with what their rounding leaves, to spare the conversions: 20.5 us, not worth sums that are no longer 64 bits.)
 #include "common.cuh"
 #include "kv_cache.cuh"
 

@@ -45,6 +45,15 @@ PROMPTS = [
 ]
 
 
+@pytest.mark.parametrize("most", [1, 3, 6, 1000])
+def test_longest_sequence_need_not_be_known(most):
+    """max_tokens chooses the kernel; sequences longer than it are served all the same."""
+    new, lens = (5, 70, 1, 200), (900, 70, 30, 450)
+    p = problem(55, new, lens, 8, 2, 128, 64, "bf16")
+    out, lse = run(p, max_tokens=most)
+    check(p, out, lse)
+
+
 @pytest.mark.parametrize("which", range(len(PROMPTS)))
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 200)])
 def test_prompts_of_several_tiles(which, causal, window):
