@@ -97,10 +97,10 @@ molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_se
     a.c = view_of(*cache, *seqs);
     a.N = N;
     a.q = q, a.ldq = ldq, a.out = out, a.ldo = ldo, a.lse = lse;
-    a.heads = heads, a.causal = causal != 0, a.window = window;
+    a.heads = heads, a.group = heads / cache->kv_heads, a.causal = causal != 0, a.window = window;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.dev_status = dev_status;
-    const int64_t rows = max_tokens * (heads / cache->kv_heads);
+    const int64_t rows = max_tokens * a.group;
     if (dt != MOLORA_BF16 || cache->dim != 128) return launch_attend_rows(a, dt, rows, ws, static_cast<cudaStream_t>(stream));
     if (rows <= kMaxStreamRows) return launch_attend_stream(a, rows, ws, static_cast<cudaStream_t>(stream));
     return launch_attend_tiles(a, ws, static_cast<cudaStream_t>(stream));

@@ -86,7 +86,7 @@ struct Walk {
     int b, group;
     Sequence sq;
     Span sp;
-    __device__ explicit Walk(const AttendArgs& args) : a(args), at(0), stop(0), base(0), b(0), group(args.heads / args.c.kv_heads) {}
+    __device__ explicit Walk(const AttendArgs& args) : a(args), at(0), stop(0), base(0), b(0), group(args.group) {}
 
     __device__ void load()
     {
@@ -109,7 +109,8 @@ struct Walk {
         u.tile_row = u.tile * ROWS;
         u.n_rows = (int)min((int64_t)ROWS, (int64_t)sq.n * group - u.tile_row);
         at = u.at + u.last;
-        const int t0 = u.tile_row / group, t1 = (u.tile_row + u.n_rows - 1) / group;
+        const bool one = sq.n == 1;         // (nothing to divide)
+        const int t0 = one ? 0 : u.tile_row / group, t1 = one ? 0 : (u.tile_row + u.n_rows - 1) / group;
         u.hi_min = upper_key(a, sq, t0), u.hi_max = upper_key(a, sq, t1);
         u.lo_min = lower_key(a, sq, t0), u.lo_max = lower_key(a, sq, t1);
         u.u0 = max(u.first - COST, (u.lo_min - sp.lo) / KEYS);
@@ -203,7 +204,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __gr
     const int4 cut = __ldcg(reinterpret_cast<const int4*>(cuts + blockIdx.x));          // sequence, row tile, head, pieces
     if (cut.w == 0) return;
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
-    const int group = a.heads / a.c.kv_heads, r0 = kJoinRows * (int)blockIdx.y;
+    const int group = a.group, r0 = kJoinRows * (int)blockIdx.y;
     const Sequence sq = sequence_of(a.c, cut.x, a.N);
     const int rows = (int)min((int64_t)ROWS, (int64_t)sq.n * group - (int64_t)cut.y * ROWS) - r0;
     if (rows <= 0) return;

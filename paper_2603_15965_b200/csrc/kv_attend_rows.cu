@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
     ptx::grid_dependency_sync();
 
     const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int group = a.heads / a.c.kv_heads;
+    const int group = a.group;
     const int plog = a.c.page_log2;
     uint8_t* const ring = ring_all + warp * kStages * 2 * Sh::kHalfBytes;
     const uint32_t ring_at = ptx::smem_u32(ring);

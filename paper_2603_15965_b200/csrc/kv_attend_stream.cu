@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
     fence_proxy_async_smem();
     grid_dependency_wait();
     if (warp == 1) take_tmem(&s_tmem_base, C::kTmemCols);
-    const int group = a.heads / a.c.kv_heads, plog = a.c.page_log2;
+    const int group = a.group, plog = a.c.page_log2;
     cut_shares<C::kThreads, W>(a, (int64_t)blockIdx.x * W, (int64_t)gridDim.x * W, kMinShare, s_start,
                                [&](const Sequence& sq) { return steps_of<ROWS, kKeys, C::kUnitCost>(a, sq, group); });
     tc_fence_before();
@@ -209,13 +209,14 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
         for (; *abort_flag == 0 && walk.next(u); ++units) {
             int group0 = 0;                                   // first of the 32 pages whose ids and scales the lanes hold
             int32_t page_id = -1;
+            float ks = 0.f, vs = 0.f;
             float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int i = u.u0; i < u.u1; ++i) {
                 const int key0 = u.sp.lo + i * kKeys, page = key0 >> plog;
-                if (i == u.u0 || page + step > group0 + 32) {
+                const bool fresh = i == u.u0 || page + step > group0 + 32;
+                if (fresh) {
                     group0 = page;
                     page_id = -1;
-                    sc = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (((int64_t)(page + lane) << plog) < u.hi_max) {
                         page_id = ld_dependent(a.c.table + (int64_t)u.b * a.c.ld_table + page + lane);
                         if (page_id < 0 || page_id >= a.c.n_pages) {
@@ -223,32 +224,36 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                             if (a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
                         } else {
                             const int64_t block = (int64_t)page_id * a.c.kv_heads + u.head;
-                            const float vs = clamped_scale(ld_dependent(a.c.v_scale + block));
-                            sc = make_float4(ld_dependent(a.c.k_scale + block), log2f(vs), 1.f / vs, 1.f);
+                            ks = ld_dependent(a.c.k_scale + block), vs = ld_dependent(a.c.v_scale + block);
                         }
                     }
                     __syncwarp();
                 }
-                const int mine = (page - group0 + (((lane & 7) * 16) >> plog)) & 31;           // the page of 16 keys
-                float4 g;
-                g.x = __shfl_sync(0xFFFFFFFFu, sc.x, mine), g.y = __shfl_sync(0xFFFFFFFFu, sc.y, mine);
-                g.z = __shfl_sync(0xFFFFFFFFu, sc.z, mine), g.w = __shfl_sync(0xFFFFFFFFu, sc.w, mine);
                 const int32_t id = __shfl_sync(0xFFFFFFFFu, page_id, (page - group0 + lane) & 31);
                 const bool copies = lane < step && id >= 0;
                 const uint32_t bytes = 2u * page_bytes * (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, copies));
                 const int row = (int)((((int64_t)id * a.c.kv_heads + u.head) << plog) + (key0 & ((1 << plog) - 1)));
                 const int s = claim();
                 if (*abort_flag) break;
-                if (lane < 8) s_tiles[s].scale[lane] = g;
-                if (lane == 0) s_tiles[s].kind = (i == u.u0 ? kFirst : 0) | ((units & 1) ? kOdd : 0);
-                __syncwarp();
-                if (lane == 0) mbar_arrive_expect_tx(bar(&ctrl.full[s]), bytes);
-                __syncwarp();
+                // the copies go out while the scales are on their way: the phase does not end before lane 0's arrival, which tells how many bytes they are
                 if (copies) {
                     const uint32_t dst = base + (uint32_t)(s * kStageBytes) + (uint32_t)lane * page_bytes;
                     tma_load_2d(dst, &tm_k, 0, row, bar(&ctrl.full[s]));
                     tma_load_2d(dst + kTileBytes, &tm_v, 0, row, bar(&ctrl.full[s]));
                 }
+                __syncwarp();
+                if (fresh) {
+                    const float v = clamped_scale(vs);
+                    sc = page_id >= 0 ? make_float4(ks, log2f(v), 1.f / v, 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                const int mine = (page - group0 + (((lane & 7) * 16) >> plog)) & 31;           // the page of 16 keys
+                float4 g;
+                g.x = __shfl_sync(0xFFFFFFFFu, sc.x, mine), g.y = __shfl_sync(0xFFFFFFFFu, sc.y, mine);
+                g.z = __shfl_sync(0xFFFFFFFFu, sc.z, mine), g.w = __shfl_sync(0xFFFFFFFFu, sc.w, mine);
+                if (lane < 8) s_tiles[s].scale[lane] = g;
+                if (lane == 0) s_tiles[s].kind = (i == u.u0 ? kFirst : 0) | ((units & 1) ? kOdd : 0);
+                __syncwarp();
+                if (lane == 0) mbar_arrive_expect_tx(bar(&ctrl.full[s]), bytes);
                 ++tiles;
             }
         }

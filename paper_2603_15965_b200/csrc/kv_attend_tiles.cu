@@ -98,7 +98,7 @@ struct TileWalk {
     int b = 0, tile = 0, tiles = 0, group;
     Sequence sq;
     TileSpan sp{0, 1};
-    __device__ explicit TileWalk(const AttendArgs& args) : a(args), group(args.heads / args.c.kv_heads) {}
+    __device__ explicit TileWalk(const AttendArgs& args) : a(args), group(args.group) {}
     __device__ void load(const Sequence& s)
     {
         sq = s;
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint8_t* const smem = smem_raw + (base - raw);
     volatile int* abort_flag = &ctrl.abort_flag;
     auto bar = [](const uint64_t* b) { return smem_u32(b); };
-    const int group = a.heads / a.c.kv_heads;
+    const int group = a.group;
 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {

@@ -86,7 +86,7 @@ struct AttendArgs {
     void* out;
     int64_t ldo;
     float* lse;
-    int32_t heads, causal, window;
+    int32_t heads, group, causal, window;      // group: query heads that share a key / value head
     float scale_log2;      // scale * log2(e): the softmax runs in powers of two
     uint32_t* dev_status;
 };
