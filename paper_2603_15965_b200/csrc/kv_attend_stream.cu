@@ -22,8 +22,8 @@
 // sequences of 100 to 2043 tokens and 20 rows.)
 // Weights are at most 2^8; the scale of a block of K multiplies its scores, that of V is added to the exponent as a logarithm and taken off
 // the sum again, so that weights have the size of what they contribute.
-// What bounds it: for few rows 32 KB a tile from HBM (1.06 GB in 172 us, 6.2 TB/s, 94 % of a copy's rate); for 20 rows the instructions, 6500 of
-// all warps a tile, at 52 % of the schedulers' slots; for a single short sequence (776 tokens: 11.5 us with the join) the chain of first reads --
+// What bounds it: for few rows 32 KB a tile from HBM (1.06 GB in 166 to 171 us, 6.2 to 6.4 TB/s, 95 to 97 % of a copy's rate); for 20 rows the instructions, 6500 of
+// all warps a tile, at 52 % of the schedulers' slots; for a single short sequence (776 tokens: 10.8 us with the join) the chain of first reads --
 // lengths, page, scales, codes -- and two launches.
 #include "kv_attend.cuh"
 #include "pipeline.cuh"
