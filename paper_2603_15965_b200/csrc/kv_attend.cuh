@@ -14,8 +14,9 @@ namespace {
 constexpr float kNone = -1e30f;              // reference of a row that has seen nothing
 
 // What a cut unit leaves behind.
-struct CutUnit {
-    int32_t b, row_tile, head, pieces;       // pieces 0: no unit begins in this share and goes on in the next
+struct alignas(16) CutUnit {
+    int32_t row0, tile_row, rows, head;      // first row of its sequence; of its tile: the first row and how many there are; key / value head
+    int32_t pieces, unused[3];               // 0: no unit begins in this share and goes on in the next
 };
 __host__ __device__ constexpr int slot_floats(int rows, int dim) { return 2 * rows + rows * dim; }
 __host__ __device__ inline size_t cut_bytes(int64_t workers) { return (size_t)((workers * (int64_t)sizeof(CutUnit) + 255) / 256 * 256); }
@@ -190,31 +191,42 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v, float f)
 }
 
 // Joins the pieces of the units that are cut: with M the largest reference, the sum of 2^(m - M) (values, sum) over the pieces,
-// always in the same order.  A CTA looks after 4 rows of the unit that begins in share blockIdx.x and goes on behind it; its four warps take every
-// fourth piece each, four rows at a time, and are added up in order.  (Asked for row by row, the pieces of a unit cut into 55 took 32 us.)
+// always in the same order.  A CTA looks after rows of the unit that begins in share blockIdx.x and goes on behind it, four rows at a time.
+// Units of few rows come in many pieces: four rows a CTA, whose warps take every fourth piece each and are added up in order (asked for row by row,
+// the pieces of a unit cut into 55 took 32 us).  Units of many rows come in few: four rows a warp, all of their pieces (four rows a CTA, a chunk's
+// 148 cut units of 256 rows took 20 us).
 constexpr int kJoinWarps = 4, kJoinRows = 4;
+__host__ __device__ constexpr bool join_by_warp(int rows) { return rows > 32; }
+__host__ constexpr unsigned join_groups(int rows) { return (unsigned)(rows / (join_by_warp(rows) ? kJoinWarps * kJoinRows : kJoinRows)); }
 template <typename T, int D, int ROWS>
 __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __grid_constant__ AttendArgs a, const CutUnit* __restrict__ cuts,
                                                                      const float* __restrict__ slots)
 {
     constexpr int kLanes = D / 4;                          // lanes of four elements
-    __shared__ float4 part[kJoinWarps][kJoinRows][kLanes];
+    constexpr bool kAlone = join_by_warp(ROWS);
+    __shared__ float4 part[kAlone ? 1 : kJoinWarps][kJoinRows][kLanes];
     __shared__ float part_l[kJoinWarps][kJoinRows];
     ptx::grid_dependency_sync();
-    const int4 cut = __ldcg(reinterpret_cast<const int4*>(cuts + blockIdx.x));          // sequence, row tile, head, pieces
-    if (cut.w == 0) return;
+    const int4 cut = __ldcg(reinterpret_cast<const int4*>(cuts + blockIdx.x));
+    const int pieces = __ldcg(&cuts[blockIdx.x].pieces);
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
-    const int group = a.group, r0 = kJoinRows * (int)blockIdx.y;
-    const Sequence sq = sequence_of(a.c, cut.x, a.N);
-    const int rows = (int)min((int64_t)ROWS, (int64_t)sq.n * group - (int64_t)cut.y * ROWS) - r0;
-    if (rows <= 0) return;
+    const int r0 = kJoinRows * (kAlone ? (int)blockIdx.y * kJoinWarps + warp : (int)blockIdx.y), rows = cut.z - r0;
+    if (pieces == 0 || rows <= 0) return;
     const int64_t w0 = blockIdx.x;
     auto slot = [&](int p) { return slots + (p == 0 ? 2 * w0 + 1 : 2 * (w0 + p)) * (int64_t)slot_floats(ROWS, D) + r0; };
+    // row `row` of the unit: its sum, its values and the reference that they are in
+    auto write = [&](int row, float4 v, float sum, float top) {
+        const int r = cut.y + row, token = r / a.group;
+        const int64_t orow = (int64_t)cut.x + token;
+        const int oh = cut.w * a.group + (r - token * a.group);
+        if (lane < kLanes) store4(static_cast<T*>(a.out) + orow * a.ldo + (int64_t)oh * D + lane * 4, v, sum == 0.f ? 0.f : 1.f / sum);
+        if (a.lse != nullptr && lane == 0) a.lse[orow * a.heads + oh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718056f;
+    };
     float M[kJoinRows], L[kJoinRows] = {};
     float4 acc[kJoinRows] = {};
 #pragma unroll
     for (int r = 0; r < kJoinRows; ++r) M[r] = kNone;
-    for (int p = lane; p < cut.w; p += 32) {
+    for (int p = lane; p < pieces; p += 32) {
         const float4 m = __ldcg(reinterpret_cast<const float4*>(slot(p)));
         M[0] = fmaxf(M[0], m.x), M[1] = fmaxf(M[1], m.y), M[2] = fmaxf(M[2], m.z), M[3] = fmaxf(M[3], m.w);
     }
@@ -224,7 +236,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __gr
         for (int r = 0; r < kJoinRows; ++r) M[r] = fmaxf(M[r], __shfl_xor_sync(0xFFFFFFFFu, M[r], o));
     // (rows behind the last hold whatever was there: their M, sums and values are not used)
 #pragma unroll 4
-    for (int p = warp; p < cut.w; p += kJoinWarps) {
+    for (int p = kAlone ? 0 : warp; p < pieces; p += kAlone ? 1 : kJoinWarps) {
         const float* s = slot(p);
         const float4 m = __ldcg(reinterpret_cast<const float4*>(s)), l = __ldcg(reinterpret_cast<const float4*>(s + ROWS));
         const float f[kJoinRows] = {ex2(m.x - M[0]), ex2(m.y - M[1]), ex2(m.z - M[2]), ex2(m.w - M[3])};
@@ -237,27 +249,28 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __gr
                 acc[r].z = fmaf(x.z, f[r], acc[r].z), acc[r].w = fmaf(x.w, f[r], acc[r].w);
             }
     }
+    if constexpr (kAlone) {
 #pragma unroll
-    for (int r = 0; r < kJoinRows; ++r) {
-        if (lane < kLanes) part[warp][r][lane] = acc[r];
-        if (lane == 0) part_l[warp][r] = L[r];
-    }
-    __syncthreads();
-    if (warp >= rows || lane >= kLanes) return;            // a row per warp from here on
-    const int row = r0 + warp;
-    float sum = 0.f, top = warp == 0 ? M[0] : warp == 1 ? M[1] : warp == 2 ? M[2] : M[3];
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int r = 0; r < kJoinRows; ++r)
+            if (r < rows) write(r0 + r, acc[r], L[r], M[r]);
+    } else {
 #pragma unroll
-    for (int z = 0; z < kJoinWarps; ++z) {
-        const float4 x = part[z][warp][lane];
-        v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
-        sum += part_l[z][warp];
+        for (int r = 0; r < kJoinRows; ++r) {
+            if (lane < kLanes) part[warp][r][lane] = acc[r];
+            if (lane == 0) part_l[warp][r] = L[r];
+        }
+        __syncthreads();
+        if (warp >= rows) return;                          // a row per warp from here on
+        float sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int z = 0; z < kJoinWarps; ++z) {
+            const float4 x = part[z][warp][lane % kLanes];
+            v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+            sum += part_l[z][warp];
+        }
+        write(r0 + warp, v, sum, warp == 0 ? M[0] : warp == 1 ? M[1] : warp == 2 ? M[2] : M[3]);
     }
-    const int r = cut.y * ROWS + row, token = r / group;
-    const int64_t orow = (int64_t)sq.row0 + token;
-    const int oh = cut.z * group + (r - token * group);
-    store4(static_cast<T*>(a.out) + orow * a.ldo + (int64_t)oh * D + lane * 4, v, sum == 0.f ? 0.f : 1.f / sum);
-    if (a.lse != nullptr && lane == 0) a.lse[orow * a.heads + oh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718056f;
 }
 
 }  // namespace

@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
     Walk<kRows, kStepKeys, kUnitCost> walk(a);
     cut_shares<kThreads, 1>(a, w, gridDim.x, kMinShare, &s_start, [&](const Sequence& sq) { return steps_of<kRows, kStepKeys, kUnitCost>(a, sq, group); });
     walk.begin(s_start, w, kThreads);
-    CutUnit cut{0, 0, 0, 0};
+    CutUnit cut{};
     Unit un;
     while (walk.next(un)) {
         const Sequence& sq = un.sq;
@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
         const bool begins = un.first == 0, ends = un.last == un.sp.steps, whole = begins && ends;
         float* slot = slots + (2 * w + (begins ? 1 : 0)) * (int64_t)slot_floats(kRows, D);
         if (begins && !ends) {
-            cut.b = un.b, cut.row_tile = un.tile, cut.head = head;
+            cut.row0 = un.sq.row0, cut.tile_row = tile_row, cut.rows = n_rows, cut.head = head;
             cut.pieces = walk.pieces(un, w);
         }
         for (int i = tid; i < n_rows * (D / 4); i += kThreads) {
@@ -498,7 +498,7 @@ molora_status_t launch(const AttendArgs& a, void* ws, cudaStream_t s)
     float* slots = reinterpret_cast<float*>(static_cast<char*>(ws) + cut_bytes(workers));
     if (launch_kernel(attend_rows_kernel<T, D, NT>, dim3((unsigned)workers), dim3(kThreads), Sh::kSmem, s, 1, true, a, cuts, slots) != cudaSuccess)
         return MOLORA_ERR_CUDA;
-    return cuda_ok(launch_kernel(attend_join_kernel<T, D, 8 * NT>, dim3((unsigned)workers, 8 * NT / kJoinRows), dim3(kJoinWarps * 32), 0, s, 1, true, a,
+    return cuda_ok(launch_kernel(attend_join_kernel<T, D, 8 * NT>, dim3((unsigned)workers, join_groups(8 * NT)), dim3(kJoinWarps * 32), 0, s, 1, true, a,
                                  static_cast<const CutUnit*>(cuts), static_cast<const float*>(slots)));
 }
 

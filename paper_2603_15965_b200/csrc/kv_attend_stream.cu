@@ -18,12 +18,12 @@
 //   groups    of four warps, each with 4 or 8 of the rows: a key per thread, weights and their terms into shared memory; at the end of a unit an
 //             element per thread.  Code that runs once a unit is kept short and the state of a unit in shared memory: instructions that are not in the
 //             cache cost more than what they do.
-// (One worker whose groups took alternate units: 196 us against 172 for 256 sequences of 3 to 4095 tokens and two rows, 81 against 65 for 64
+// (One worker whose groups took alternate units: 196 us against 172 for 256 sequences of 3 to 4095 tokens and two rows, 81 against 68 for 64
 // sequences of 100 to 2043 tokens and 20 rows.)
 // Weights are at most 2^8; the scale of a block of K multiplies its scores, that of V is added to the exponent as a logarithm and taken off
 // the sum again, so that weights have the size of what they contribute.
 // What bounds it: for few rows 32 KB a tile from HBM (1.06 GB in 166 to 171 us, 6.2 to 6.4 TB/s, 95 to 97 % of a copy's rate); for 20 rows the instructions, 6500 of
-// all warps a tile, at 52 % of the schedulers' slots; for a single short sequence (776 tokens: 10.8 us with the join) the chain of first reads --
+// all warps a tile, at 52 % of the schedulers' slots; for a single short sequence (776 tokens: 10.3 us with the join) the chain of first reads --
 // lengths, page, scales, codes -- and two launches.
 #include "kv_attend.cuh"
 #include "pipeline.cuh"
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
     } else if (role < kRoleWarps) {
         // ============================================================ the rows of the units, one unit ahead: pairs of rows in turn
         Unit u;
-        CutUnit cut{0, 0, 0, 0};
+        CutUnit cut{};
         const int turn = role - 2;
         for (int k = 0;; ++k) {
             const bool more = walk.next(u);
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 break;
             }
             const bool begins = u.first == 0, whole = begins && u.last == u.sp.steps;
-            if (begins && !whole) cut.b = u.b, cut.row_tile = u.tile, cut.head = u.head, cut.pieces = walk.pieces(u, share);
+            if (begins && !whole) cut.row0 = u.sq.row0, cut.tile_row = u.tile_row, cut.rows = u.n_rows, cut.head = u.head, cut.pieces = walk.pieces(u, share);
             const int n = max(u.u1 - u.u0, 0);
             if (turn == 0 && lane == 0) {
                 rows.tiles = n, rows.key0 = u.sp.lo + u.u0 * kKeys, rows.n_rows = u.n_rows;
@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 if (n > 0) mbar_arrive(bar(&ctrl.q_ready[k & 1]));
             }
         }
-        if (turn == 0 && lane == 0) cuts[share] = *abort_flag == 0 ? cut : CutUnit{0, 0, 0, 0};
+        if (turn == 0 && lane == 0) cuts[share] = *abort_flag == 0 ? cut : CutUnit{};
     } else {
         // ============================================================ a key per thread
         const int q4 = warp & 3, key_lane = q4 * 32 + lane;      // the quarter of TMEM's lanes that this warp may access
@@ -629,7 +629,7 @@ molora_status_t launch(const AttendArgs& a, void* ws, cudaStream_t s)
     float* slots = reinterpret_cast<float*>(static_cast<char*>(ws) + cut_bytes(shares));
     if (launch_kernel(attend_stream_kernel<ROWS>, dim3((unsigned)sm_count()), dim3(C::kThreads), C::kSmem, s, 1, true, a, tm_k, tm_v, cuts, slots) != cudaSuccess)
         return MOLORA_ERR_CUDA;
-    return cuda_ok(launch_kernel(attend_join_kernel<__nv_bfloat16, kDim, ROWS>, dim3((unsigned)shares, ROWS / kJoinRows), dim3(kJoinWarps * 32), 0, s, 1, true, a,
+    return cuda_ok(launch_kernel(attend_join_kernel<__nv_bfloat16, kDim, ROWS>, dim3((unsigned)shares, join_groups(ROWS)), dim3(kJoinWarps * 32), 0, s, 1, true, a,
                                  static_cast<const CutUnit*>(cuts), static_cast<const float*>(slots)));
 }
 

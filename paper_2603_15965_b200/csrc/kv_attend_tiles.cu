@@ -10,15 +10,15 @@
 //                   the other at the latencies of one warp per scheduler, took 3500 cycles per 128 keys.)
 //   warps 16-19     codes -> fp16, two tiles of 128 keys of K and of V ahead, the codes of the next tile on their way in registers
 //   warps 20, 21    the MMAs of tile 0 and of tile 1: O of a step, then S of the step after the next, so that the scores of the next step are there
-//                   when the weights of this one are done.  (One warp for both: 8 % slower; steps of 128 keys, whose S had to wait for all of the
-//                   last P: 8 % slower; S of 64 keys costs the tensor cores 56 cycles per 16 elements where 128 keys cost 64.)
+//                   when the weights of this one are done.  (One warp for both took 8 % longer, with steps of 64 keys and with steps of 128, whose S has
+//                   to wait for all of the last P; S of 64 keys costs the tensor cores 56 cycles per 16 elements where 128 keys cost 64.)
 //   warp 22         units, pages and scales, into queues: what depends on one another there is waited for long before it is needed
 // The tensor cores work in the order of issue: O, which reads P, is through before S is written in its place.
 // TMEM: S_0 S_1 O_0 O_1, 128 columns each, S for even and odd steps.  Shared memory: Q 64 KB, K and V 2 x 32 KB each.
 // Shares, pieces and the join as in kv_attend.cuh, but with the steps that each tile of rows really sees.
-// What bounds it, measured with 2048 rows of 32 heads behind 14336 tokens (640 us, 0.8 PFLOP/s): no unit alone.  Per 128 keys it takes 5200 cycles,
+// What bounds it, measured with 2048 rows of 32 heads behind 14336 tokens (645 us, 0.8 PFLOP/s): no unit alone.  Per 128 keys it takes 5200 cycles,
 // of which the tensor cores are busy 54 %, the special-function units 41 % (256 x 128 exponentials), the schedulers 60 %; taking out the
-// exponentials or seven eighths of the MMAs gains 4 % each, both together with the codes 11 %.  With short prompts (8 of 1024 tokens: 174 us) it
+// exponentials or seven eighths of the MMAs gains 4 % each, both together with the codes 11 %.  With short prompts (8 of 1024 tokens: 172 us) it
 // is what a unit costs by itself, 13,000 cycles, 5500 of them for q.
 #include "kv_attend.cuh"
 #include "pipeline.cuh"
@@ -93,7 +93,7 @@ struct TileWalk {
     const AttendArgs& a;
     int64_t at = 0, stop = 0, base = 0, share = 1;      // next step, end of the share, first step of the tile of rows
     // A share that would end so near to an end of a unit ends there instead: a piece costs its 128 KB in the workspace twice, about as much as
-    // three steps (8 prompts of 1024 tokens, shares of 52 steps: 181 us without, 173 so; more than that costs balance).
+    // three steps (8 prompts of 1024 tokens, shares of 52 steps: 181 us without, 174 so; more than that costs balance).
     __device__ int64_t near() const { return min(share >> 3, (int64_t)6); }
     int b = 0, tile = 0, tiles = 0, group;
     Sequence sq;
@@ -638,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int plog = a.c.page_log2;
         TileWalk walk(a);
         walk.begin(s_start, blockIdx.x);
-        CutUnit cut{0, 0, 0, 0};
+        CutUnit cut{};
         int tiles = 0, units = 0;
         auto push_unit = [&](const UnitInfo& info) {
             const int slot = units % kUnitQueue;
@@ -664,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         TileUnit u{};
         while (*abort_flag == 0 && walk.next(u)) {
             const bool begins = u.first == 0, whole = begins && u.last == u.steps;
-            if (begins && !whole) cut.b = u.b, cut.row_tile = u.tile, cut.head = u.head, cut.pieces = walk.pieces(u, blockIdx.x);
+            if (begins && !whole) cut.row0 = u.sq.row0, cut.tile_row = u.tile_row, cut.rows = u.n_rows, cut.head = u.head, cut.pieces = walk.pieces(u, blockIdx.x);
             UnitInfo info;
             info.row0 = u.sq.row0, info.first_pos = u.sq.first_pos(), info.len = u.sq.len;
             info.tile_row = u.tile_row, info.n_rows = u.n_rows, info.head = u.head;
@@ -713,7 +713,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         KeyTile& tile = claim_tile();
         if (lane == 0) tile.kind = 2;
         hand_over();
-        if (lane == 0) cuts[blockIdx.x] = *abort_flag == 0 ? cut : CutUnit{0, 0, 0, 0};
+        if (lane == 0) cuts[blockIdx.x] = *abort_flag == 0 ? cut : CutUnit{};
       }
     }
     tc_fence_before();
@@ -739,7 +739,7 @@ molora_status_t launch_attend_tiles(const AttendArgs& a, void* ws, cudaStream_t 
     CutUnit* cuts = static_cast<CutUnit*>(ws);
     float* slots = reinterpret_cast<float*>(static_cast<char*>(ws) + cut_bytes(shares));
     if (launch_kernel(attend_tiles_kernel, dim3((unsigned)shares), dim3(kThreads), kSmem, s, 1, true, a, cuts, slots) != cudaSuccess) return MOLORA_ERR_CUDA;
-    return cuda_ok(launch_kernel(attend_join_kernel<__nv_bfloat16, kDim, kUnitRows>, dim3((unsigned)shares, kUnitRows / kJoinRows), dim3(kJoinWarps * 32), 0, s,
+    return cuda_ok(launch_kernel(attend_join_kernel<__nv_bfloat16, kDim, kUnitRows>, dim3((unsigned)shares, join_groups(kUnitRows)), dim3(kJoinWarps * 32), 0, s,
                                  1, true, a, static_cast<const CutUnit*>(cuts), static_cast<const float*>(slots)));
 }
 
