@@ -378,7 +378,7 @@ molora_status_t molora_route_hotset(const int32_t *ids, const int32_t *adapter_i
  *               of q, k, v; rows from cu_tokens[B] on belong to no sequence and are left as they are
  *   kv_lens     device int32 [B]: tokens of sequence b INCLUDING the new ones, so that its j-th of n new tokens stands at
  *               position kv_lens[b] - n + j
- * Pages outside [0, n_pages), lengths beyond max_pages * page and positions below 0 never fault: those tokens are left out
+ * Pages outside [0, n_pages), lengths beyond max_pages * page or 2^30 and positions below 0 never fault: those tokens are left out
  * and MOLORA_DEV_BAD_SEQUENCE is OR-ed into dev_status. */
 typedef struct {
     void *k, *v;

@@ -1,4 +1,5 @@
 // C ABI of the paged cache and of draft verification: argument validation on the host, then enqueue.
+#include <algorithm>
 #include <cmath>
 
 #include "kv_cache.cuh"
@@ -97,7 +98,7 @@ molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_se
     a.c = view_of(*cache, *seqs);
     a.N = N;
     a.q = q, a.ldq = ldq, a.out = out, a.ldo = ldo, a.lse = lse;
-    a.heads = heads, a.group = heads / cache->kv_heads, a.causal = causal != 0, a.window = window;
+    a.heads = heads, a.group = heads / cache->kv_heads, a.causal = causal != 0, a.window = std::min(window, kMaxTokens);
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.dev_status = dev_status;
     const int64_t rows = max_tokens * a.group;

@@ -22,6 +22,7 @@ struct KvView {
 };
 
 // Sequence b of the call, with what cannot be true of it put right: rows inside [0, N], lengths inside the page table.
+constexpr int32_t kMaxTokens = 1 << 30;      // of a sequence: sums of positions, windows and tiles stay within 32 bits
 struct Sequence {
     int32_t row0;     // first of its rows
     int32_t n;        // its rows
@@ -37,7 +38,7 @@ __device__ __forceinline__ Sequence sequence_of(const KvView& c, int b, int64_t 
     const int32_t top = (int32_t)min(N, (int64_t)INT32_MAX);
     s.row0 = max(0, min(a, top));
     s.n = max(0, min(e, top) - s.row0);
-    s.len = (int32_t)max((int64_t)0, min((int64_t)l, min(room, (int64_t)INT32_MAX)));
+    s.len = (int32_t)max((int64_t)0, min((int64_t)l, min(room, (int64_t)kMaxTokens)));
     s.bad = s.row0 != a || (int64_t)e - a != s.n || s.len != l || s.n > s.len;
     return s;
 }

@@ -45,6 +45,17 @@ PROMPTS = [
 ]
 
 
+@pytest.mark.parametrize("dim,dtype", [(128, "bf16"), (64, "f32")])
+@pytest.mark.parametrize("new,lens", [((1, 3), (300, 90)), ((60, 9), (50, 200))])
+def test_a_window_of_everything(dim, dtype, new, lens):
+    """The largest window is no window, also where more tokens are new than there are."""
+    p = problem(56, new, lens, 8, 2, dim, 64, dtype)
+    out, lse = run(p)
+    for window in (2 ** 30, 2 ** 31 - 1):
+        again, z = run(p, window=window)
+        assert torch.equal(out, again) and torch.equal(lse, z)
+
+
 @pytest.mark.parametrize("most", [1, 3, 6, 1000])
 def test_longest_sequence_need_not_be_known(most):
     """max_tokens chooses the kernel; sequences longer than it are served all the same."""
