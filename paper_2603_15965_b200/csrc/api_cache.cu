@@ -91,6 +91,7 @@ molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_se
     if (N == 0 || seqs->B == 0) return MOLORA_OK;
     if (const molora_status_t st = check_rows(q, ldq, (int64_t)heads * cache->dim)) return st;
     if (const molora_status_t st = check_rows(out, ldo, (int64_t)heads * cache->dim)) return st;
+    if (q == out) return MOLORA_ERR_INVALID_ARG;      // (units read rows of q after others have been written)
     if (max_tokens == 0 || max_tokens > N) max_tokens = N;
     const size_t need = molora_kv_attend_workspace_bytes(dt, heads, cache->kv_heads, cache->dim, max_tokens);
     if (need > 0 && (ws == nullptr || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)) return MOLORA_ERR_WORKSPACE;

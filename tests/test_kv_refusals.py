@@ -55,7 +55,7 @@ def nothing_enqueued():
     (dict(s=dict(B=-1)), INVALID), (dict(s=dict(cu_tokens=None)), INVALID), (dict(s=dict(kv_lens=None)), INVALID), (dict(s=dict(page_table=None)), INVALID),
     (dict(s=dict(ld_table=4)), INVALID), (dict(s=dict(max_pages=-1)), INVALID), (dict(N=-1), INVALID), (dict(N=2 ** 31), UNSUPPORTED), (dict(dt=7), UNSUPPORTED),
     (dict(q=None), INVALID), (dict(q=0x1008), INVALID), (dict(ldq=504), INVALID), (dict(ldq=516), UNSUPPORTED), (dict(heads=-1), INVALID),
-    (dict(c=dict(kv_heads=1025)), UNSUPPORTED),
+    (dict(c=dict(kv_heads=1025)), UNSUPPORTED), (dict(c=dict(n_pages=2 ** 24)), UNSUPPORTED), (dict(c=dict(n_pages=2 ** 31 - 1, kv_heads=1024)), UNSUPPORTED),
 ])
 def test_cache_calls(call, kw, status):
     kw = dict(kw)
@@ -77,7 +77,7 @@ def test_append(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(heads=3), INVALID), (dict(heads=0), INVALID), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("inf")), INVALID),
     (dict(scale=float("nan")), INVALID), (dict(window=-1), INVALID), (dict(window=5, causal=0), UNSUPPORTED), (dict(out=None), INVALID), (dict(ldo=256), INVALID),
-    (dict(max_tokens=-1), INVALID), (dict(ws=None), WORKSPACE), (dict(ws_bytes=1000), WORKSPACE), (dict(ws=0x10010), WORKSPACE),
+    (dict(out=P), INVALID), (dict(max_tokens=-1), INVALID), (dict(ws=None), WORKSPACE), (dict(ws_bytes=1000), WORKSPACE), (dict(ws=0x10010), WORKSPACE),
 ])
 def test_attend(kw, status):
     assert attend(**kw) == status
