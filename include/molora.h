@@ -421,7 +421,7 @@ molora_status_t molora_kv_append(const molora_kv_cache_t *cache, const molora_se
  * lse     device fp32 [N][heads] or NULL: natural logarithm of the softmax's sum
  * window  0, or (causal only) the number of newest tokens that a row sees, itself included
  * max_tokens  the most new tokens that a sequence of this call has, as far as the caller knows (N if it does not); the
- *         choice of kernel goes by it, results do not depend on it
+ *         choice of kernel goes by it and by the other sizes; results differ by roundings at most
  * ws, ws_bytes  device scratch of at least molora_kv_attend_workspace_bytes(...) bytes, 256-byte aligned, need not be cleared;
  *         calls that share it must not overlap on the GPU
  * Scores and sums are fp32; q (its rows scaled by powers of two) and the codes enter the tensor cores exactly, fp32 q in 22

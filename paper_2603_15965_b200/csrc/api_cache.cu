@@ -47,6 +47,18 @@ KvView view_of(const molora_kv_cache_t& c, const molora_sequences_t& s)
     return v;
 }
 
+// Whether bf16 rows with heads of 128 go to the kernel for few rows, in units of 32: always up to that, and for more where its units find a worker
+// each and read few keys over again -- two units a sequence, or no more than four tiles of 128 keys a worker if every page of the table is in use.
+// (16 new tokens of one sequence, 4 heads a key / value head, behind 20,000: 36 us against 47; 40 behind 460: 19 against 28; 16 of each of 16
+// sequences, 384 units: 44 both; 32 of each, 640 units: 73 against 46.)
+bool few_rows(int64_t rows, int64_t N, int32_t group, const molora_kv_cache_t& c, const molora_sequences_t& s)
+{
+    if (rows <= kMaxStreamRows) return true;
+    const int64_t units = c.kv_heads * (s.B + N * group / kMaxStreamRows), workers = 2 * sm_count();
+    const int64_t tiles = ((int64_t)s.max_pages * c.page + 127) / 128;
+    return units <= workers && (rows <= 2 * kMaxStreamRows || units * tiles <= 4 * workers);
+}
+
 }  // namespace
 
 extern "C" {
@@ -78,7 +90,8 @@ size_t molora_kv_attend_workspace_bytes(molora_dtype_t dt, int32_t heads, int32_
     if ((dim != 64 && dim != 128) || kv_heads < 1 || heads < 1 || heads % kv_heads != 0 || max_tokens < 1 || (dt != MOLORA_F32 && dt != MOLORA_BF16)) return 0;
     const int64_t rows = max_tokens * (heads / kv_heads);
     if (dt != MOLORA_BF16 || dim != 128) return attend_rows_workspace_bytes(dt, dim, rows);
-    return rows <= kMaxStreamRows ? attend_stream_workspace_bytes(rows) : attend_tiles_workspace_bytes();
+    // (more rows may go to either kernel, by what else the call has)
+    return rows <= kMaxStreamRows ? attend_stream_workspace_bytes(rows) : std::max(attend_stream_workspace_bytes(rows), attend_tiles_workspace_bytes());
 }
 
 molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_sequences_t* seqs, molora_dtype_t dt, int64_t N, const void* q,
@@ -104,7 +117,7 @@ molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_se
     a.dev_status = dev_status;
     const int64_t rows = max_tokens * a.group;
     if (dt != MOLORA_BF16 || cache->dim != 128) return launch_attend_rows(a, dt, rows, ws, static_cast<cudaStream_t>(stream));
-    if (rows <= kMaxStreamRows) return launch_attend_stream(a, rows, ws, static_cast<cudaStream_t>(stream));
+    if (few_rows(rows, N, a.group, *cache, *seqs)) return launch_attend_stream(a, rows, ws, static_cast<cudaStream_t>(stream));
     return launch_attend_tiles(a, ws, static_cast<cudaStream_t>(stream));
 }
 

@@ -94,7 +94,7 @@ struct AttendArgs {
 // rows: of the longest sequence, per key / value head.  fp32, or heads of 64:
 size_t attend_rows_workspace_bytes(molora_dtype_t dt, int32_t dim, int64_t rows);
 molora_status_t launch_attend_rows(const AttendArgs& a, molora_dtype_t dt, int64_t rows, void* ws, cudaStream_t s);
-// bf16, heads of 128; up to kMaxStreamRows rows, and more:
+// bf16, heads of 128; in units of up to kMaxStreamRows rows, and of 256:
 constexpr int64_t kMaxStreamRows = 32;
 size_t attend_stream_workspace_bytes(int64_t rows);
 molora_status_t launch_attend_stream(const AttendArgs& a, int64_t rows, void* ws, cudaStream_t s);

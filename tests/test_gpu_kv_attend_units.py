@@ -41,6 +41,9 @@ PROMPTS = [
     ((2100,), (2100,), 2, 2, 128),
     ((40,), (30000,), 4, 1, 64),                                         # one unit, cut wherever shares end
     ((257, 31, 257, 128, 129), (257, 31, 900, 129, 193), 3, 3, 32),
+    ((1500, 300), (1500, 1300), 4, 2, 32),
+    ((257, 31, 700, 128, 129, 256), (2257, 31, 900, 129, 193, 256), 12, 3, 128),
+    ((90,) * 12, tuple(90 + 70 * i for i in range(12)), 16, 4, 16),
     (tuple(20 + i % 50 for i in range(60)), tuple(20 + i % 50 + (i % 7) * 40 for i in range(60)), 4, 2, 64),
 ]
 
