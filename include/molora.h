@@ -425,8 +425,8 @@ molora_status_t molora_kv_append(const molora_kv_cache_t *cache, const molora_se
  * ws, ws_bytes  device scratch of at least molora_kv_attend_workspace_bytes(...) bytes, 256-byte aligned, need not be cleared;
  *         calls that share it must not overlap on the GPU
  * Scores and sums are fp32; q (its rows scaled by powers of two) and the codes enter the tensor cores exactly, fp32 q in 22
- * bits; weights are rounded to 11 bits (22 for fp32) and, below 2^-14 of a row's largest (bf16, heads of 128, up to 32
- * rows), to steps of 2^-24 of it; one rounding to dt at the end.
+ * bits; weights are rounded to 11 bits (22 for fp32) and, below 2^-14 of a row's largest (bf16, heads of 128), to steps of
+ * 2^-24 of it; one rounding to dt at the end.
  * Tokens that a row does not see leave no trace in it, whatever their codes; a NaN among the codes of a token makes the rows NaN that do
  * see it. */
 size_t molora_kv_attend_workspace_bytes(molora_dtype_t dt, int32_t heads, int32_t kv_heads, int32_t dim, int64_t max_tokens);
