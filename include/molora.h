@@ -420,9 +420,10 @@ molora_status_t molora_kv_append(const molora_kv_cache_t *cache, const molora_se
  * q       device [N][heads * dim] of type dt, pitch ldq; out the same, pitch ldo, not overlapping q; heads a multiple of kv_heads
  * lse     device fp32 [N][heads] or NULL: natural logarithm of the softmax's sum
  * window  0, or (causal only) the number of newest tokens that a row sees, itself included
- * max_tokens  the most new tokens that a sequence of this call has, as far as the caller knows (N if it does not); the
- *         choice of kernel goes by it and by the other sizes; results differ by roundings at most
+ * max_tokens  the most new tokens that a sequence of this call has, as far as the caller knows (N, or 0, if it does not; bounds above
+ *         N count as N); the choice of kernel goes by it and by the other sizes; results differ by roundings at most
  * ws, ws_bytes  device scratch of at least molora_kv_attend_workspace_bytes(...) bytes, 256-byte aligned, need not be cleared;
+ *         the size never falls as max_tokens grows, so one that was made for a step's most tokens serves calls of fewer;
  *         calls that share it must not overlap on the GPU
  * Scores and sums are fp32; q (its rows scaled by powers of two) and the codes enter the tensor cores exactly, fp32 q in 22
  * bits; weights are rounded to 11 bits (22 for fp32) and, below 2^-14 of a row's largest (bf16, heads of 128), to steps of

@@ -47,6 +47,9 @@ KvView view_of(const molora_kv_cache_t& c, const molora_sequences_t& s)
     return v;
 }
 
+// rows of the longest sequence, per key / value head; what is beyond 2^31 tokens is no call's
+int64_t rows_of(int64_t max_tokens, int32_t group) { return std::min(max_tokens, (int64_t)INT32_MAX) * group; }
+
 // Whether bf16 rows with heads of 128 go to the kernel for few rows, in units of 32: always up to that, and for more where its units find a worker
 // each and read few keys over again -- two units a sequence, or no more than four tiles of 128 keys a worker if every page of the table is in use.
 // (16 new tokens of one sequence, 4 heads a key / value head, behind 20,000: 36 us against 47; 40 behind 460: 19 against 28; 16 of each of 16
@@ -88,7 +91,8 @@ molora_status_t molora_kv_append(const molora_kv_cache_t* cache, const molora_se
 size_t molora_kv_attend_workspace_bytes(molora_dtype_t dt, int32_t heads, int32_t kv_heads, int32_t dim, int64_t max_tokens)
 {
     if ((dim != 64 && dim != 128) || kv_heads < 1 || heads < 1 || heads % kv_heads != 0 || max_tokens < 1 || (dt != MOLORA_F32 && dt != MOLORA_BF16)) return 0;
-    const int64_t rows = max_tokens * (heads / kv_heads);
+    const int64_t rows = rows_of(max_tokens, heads / kv_heads);
+    // Enough for fewer rows too: a call is cut down to the tokens that it has, and a workspace made for a step's most serves every step.
     if (dt != MOLORA_BF16 || dim != 128) return attend_rows_workspace_bytes(dt, dim, rows);
     // (more rows may go to either kernel, by what else the call has)
     return rows <= kMaxStreamRows ? attend_stream_workspace_bytes(rows) : std::max(attend_stream_workspace_bytes(rows), attend_tiles_workspace_bytes());
@@ -115,7 +119,7 @@ molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_se
     a.heads = heads, a.group = heads / cache->kv_heads, a.causal = causal != 0, a.window = std::min(window, kMaxTokens);
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
     a.dev_status = dev_status;
-    const int64_t rows = max_tokens * a.group;
+    const int64_t rows = rows_of(max_tokens, a.group);
     if (dt != MOLORA_BF16 || cache->dim != 128) return launch_attend_rows(a, dt, rows, ws, static_cast<cudaStream_t>(stream));
     if (few_rows(rows, N, a.group, *cache, *seqs)) return launch_attend_stream(a, rows, ws, static_cast<cudaStream_t>(stream));
     return launch_attend_tiles(a, ws, static_cast<cudaStream_t>(stream));

@@ -24,6 +24,7 @@
 // What bounds it: the codes, 2 D bytes per (key, key / value head), from HBM: 256 sequences of 3 to 4095 tokens, 16 heads over 8 of 64, take 123 us
 // in bf16 and 132 in fp32 (4.3 and 4.0 TB/s), of 128 in fp32 268 us; for prompts the tensor instruction (8 of 1024 tokens, 32 heads of 64: 480 and
 // 717 us), which reaches a quarter of what tcgen05 would give.
+#include <algorithm>
 #include <type_traits>
 
 #include "kv_attend.cuh"
@@ -535,7 +536,14 @@ struct Launch {
 
 }  // namespace
 
-size_t attend_rows_workspace_bytes(molora_dtype_t dt, int32_t dim, int64_t rows) { return for_variant(dt, dim, rows, BytesNeeded{}); }
+// the most that any number of rows up to this needs (24 rows of bf16, with fewer CTAs, need less than 16)
+size_t attend_rows_workspace_bytes(molora_dtype_t dt, int32_t dim, int64_t rows)
+{
+    size_t most = 0;
+    for (int64_t r = 8; r < 8 * kMaxTiles; r += 8)
+        if (r < rows) most = std::max(most, for_variant(dt, dim, r, BytesNeeded{}));
+    return std::max(most, for_variant(dt, dim, rows, BytesNeeded{}));
+}
 
 molora_status_t launch_attend_rows(const AttendArgs& a, molora_dtype_t dt, int64_t rows, void* ws, cudaStream_t s)
 {

@@ -25,6 +25,8 @@
 // What bounds it: for few rows 32 KB a tile from HBM (1.06 GB in 166 to 171 us, 6.2 to 6.4 TB/s, 95 to 97 % of a copy's rate); for 20 rows the instructions, 6500 of
 // all warps a tile, at 52 % of the schedulers' slots; for a single short sequence (776 tokens: 10.3 us with the join) the chain of first reads --
 // lengths, page, scales, codes -- and two launches.
+#include <algorithm>
+
 #include "kv_attend.cuh"
 #include "pipeline.cuh"
 #include "tensor_map.cuh"
@@ -635,9 +637,15 @@ molora_status_t launch(const AttendArgs& a, void* ws, cudaStream_t s)
 
 }  // namespace
 
+// the most that any number of rows up to this needs (32 rows, with one worker per CTA, need less than 24 or 16)
 size_t attend_stream_workspace_bytes(int64_t rows)
 {
-    return rows <= 4 ? bytes_needed<4>() : rows <= 8 ? bytes_needed<8>() : rows <= 16 ? bytes_needed<16>() : rows <= 24 ? bytes_needed<24>() : bytes_needed<32>();
+    size_t most = bytes_needed<4>();
+    if (rows > 4) most = std::max(most, bytes_needed<8>());
+    if (rows > 8) most = std::max(most, bytes_needed<16>());
+    if (rows > 16) most = std::max(most, bytes_needed<24>());
+    if (rows > 24) most = std::max(most, bytes_needed<32>());
+    return most;
 }
 
 molora_status_t launch_attend_stream(const AttendArgs& a, int64_t rows, void* ws, cudaStream_t s)
