@@ -378,8 +378,10 @@ molora_status_t molora_route_hotset(const int32_t *ids, const int32_t *adapter_i
  *               of q, k, v; rows from cu_tokens[B] on belong to no sequence and are left as they are
  *   kv_lens     device int32 [B]: tokens of sequence b INCLUDING the new ones, so that its j-th of n new tokens stands at
  *               position kv_lens[b] - n + j
- * Pages outside [0, n_pages), lengths beyond max_pages * page or 2^30 and positions below 0 never fault: those tokens are left out
- * and MOLORA_DEV_BAD_SEQUENCE is OR-ed into dev_status. */
+ * Pages outside [0, n_pages), positions below 0 or from max_pages * page (or 2^30) on, and rows from N on never fault: those tokens
+ * are left out and MOLORA_DEV_BAD_SEQUENCE is OR-ed into dev_status.  The others keep their positions.  (A row of q whose token's page
+ * cannot be used is rotated, and attends to what it sees, all the same; one of a position below 0 is not rotated and, if causal, sees
+ * nothing.) */
 typedef struct {
     void *k, *v;
     float *k_scale, *v_scale;

@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_con
         }
         const int64_t j = i - sq.row0;
         if (j < 0) break;                                  // (rows of no sequence: cu does not start at 0)
-        const int pos = sq.first_pos() + (int)j;
+        const int pos = sq.pos0 + (int)j;
         if (sq.bad && tid == 0 && g == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
         if (pos < 0) {                                     // in front of the sequence's beginning: left out
             i = min(end, i - pos);
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_con
             continue;
         }
         const int at = pos >> a.c.page_log2;
-        const int32_t id = at < a.c.max_pages ? ptx::ld_dependent(a.c.table + b * a.c.ld_table + at) : -1;
+        const int32_t id = at < a.c.max_pages && pos < kMaxTokens ? ptx::ld_dependent(a.c.table + b * a.c.ld_table + at) : -1;
         if ((id < 0 || id >= a.c.n_pages) && kind != 2) {
             if (tid == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
             i += count;

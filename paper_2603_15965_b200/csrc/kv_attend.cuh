@@ -33,7 +33,7 @@ __device__ __forceinline__ Span span_of(const Sequence& s, int group, int window
 {
     Span r{0, 0, 0};
     if (s.n == 0) return r;
-    r.lo = window > 0 ? max(0, s.first_pos() - window + 1) & ~(KEYS - 1) : 0;
+    r.lo = window > 0 && s.pos0 >= window ? (s.pos0 - window + 1) & ~(KEYS - 1) : 0;
     r.steps = COST + max(1, (s.len - r.lo + KEYS - 1) / KEYS);
     r.tiles = (int32_t)(((int64_t)s.n * group + ROWS - 1) / ROWS);
     return r;
@@ -58,11 +58,12 @@ struct Unit {
 };
 __device__ __forceinline__ int upper_key(const AttendArgs& a, const Sequence& sq, int token)
 {
-    return a.causal ? max(0, min(sq.first_pos() + token + 1, sq.len)) : sq.len;
+    return a.causal ? max(0, min(sq.pos0 + token + 1, sq.len)) : sq.len;
 }
 __device__ __forceinline__ int lower_key(const AttendArgs& a, const Sequence& sq, int token)
 {
-    return a.window > 0 ? max(0, sq.first_pos() + token - a.window + 1) : 0;
+    const int p = sq.pos0 + token;
+    return a.window > 0 && p >= a.window ? p - a.window + 1 : 0;      // (p may be far below 0)
 }
 
 // a / b of numbers that are not negative; most a are below 2^32, where it is a fifth of the instructions

@@ -60,7 +60,7 @@ struct KeyTile {
 };
 // A unit in the queue.
 struct UnitInfo {
-    int32_t row0, first_pos, len;              // of its sequence
+    int32_t row0, pos0, len;                   // of its sequence
     int32_t tile_row, n_rows, head;
     int32_t key0, n;                           // first key, tiles of keys; n -1: there are no more units
     int32_t steps;                             // of 64 keys: 2 n, or one less where no row sees the last
@@ -284,8 +284,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int mine = t * kTileRows + row, r = u.tile_row + min(mine, u.n_rows - 1);
             const int token = r / group, qh = u.head * group + (r - token * group);
             real = mine < u.n_rows;
-            hi_row = a.causal ? max(0, min(u.first_pos + token + 1, u.len)) : u.len;
-            lo_row = a.window > 0 ? max(0, u.first_pos + token - a.window + 1) : 0;
+            const int p = u.pos0 + token;
+            hi_row = a.causal ? max(0, min(p + 1, u.len)) : u.len;
+            lo_row = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
             const int64_t at = (int64_t)u.row0 + token, in = at * a.ldq + (int64_t)qh * kDim;
             out_at = at * a.ldo + (int64_t)qh * kDim, lse_at = at * a.heads + qh;
             if (u.n <= 0) return;
@@ -666,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool begins = u.first == 0, whole = begins && u.last == u.steps;
             if (begins && !whole) cut.row0 = u.sq.row0, cut.tile_row = u.tile_row, cut.rows = u.n_rows, cut.head = u.head, cut.pieces = walk.pieces(u, blockIdx.x);
             UnitInfo info;
-            info.row0 = u.sq.row0, info.first_pos = u.sq.first_pos(), info.len = u.sq.len;
+            info.row0 = u.sq.row0, info.pos0 = u.sq.pos0, info.len = u.sq.len;
             info.tile_row = u.tile_row, info.n_rows = u.n_rows, info.head = u.head;
             info.key0 = u.lo + u.u0 * kKeys, info.n = max(u.u1 - u.u0, 0);
             info.steps = 2 * info.n - (info.n > 0 && u.lo + u.u1 * kKeys - kStepKeys >= u.hi_max ? 1 : 0);

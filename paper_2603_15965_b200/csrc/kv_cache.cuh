@@ -21,25 +21,28 @@ struct KvView {
     int32_t B, max_pages;
 };
 
-// Sequence b of the call, with what cannot be true of it put right: rows inside [0, N], lengths inside the page table.
-constexpr int32_t kMaxTokens = 1 << 30;      // of a sequence: sums of positions, windows and tiles stay within 32 bits
+// Sequence b of the call, with what cannot be true of it put right: rows inside [0, N], tokens inside the page table.  What is cut off is left out;
+// the tokens that stay keep the positions that the sequence's length as it was given and its rows as they were given make.
+constexpr int32_t kMaxTokens = 1 << 30;      // of a sequence: sums of keys, windows and tiles stay within 32 bits
 struct Sequence {
     int32_t row0;     // first of its rows
     int32_t n;        // its rows
-    int32_t len;      // tokens in the cache
+    int32_t pos0;     // position of the first; the last one's is below 2^31 - 1
+    int32_t len;      // tokens that can be in the cache
     bool bad;         // something had to be put right
-    __device__ int32_t first_pos() const { return len - n; }
 };
 __device__ __forceinline__ Sequence sequence_of(const KvView& c, int b, int64_t N)
 {
     Sequence s;
     const int32_t a = ptx::ld_dependent(c.cu + b), e = ptx::ld_dependent(c.cu + b + 1), l = ptx::ld_dependent(c.kv_lens + b);
-    const int64_t room = (int64_t)c.max_pages << c.page_log2;
+    const int64_t room = min((int64_t)c.max_pages << c.page_log2, (int64_t)kMaxTokens);
     const int32_t top = (int32_t)min(N, (int64_t)INT32_MAX);
     s.row0 = max(0, min(a, top));
     s.n = max(0, min(e, top) - s.row0);
-    s.len = (int32_t)max((int64_t)0, min((int64_t)l, min(room, (int64_t)kMaxTokens)));
-    s.bad = s.row0 != a || (int64_t)e - a != s.n || s.len != l || s.n > s.len;
+    const int32_t given = max(l, 0);
+    s.pos0 = s.n > 0 ? (int32_t)((int64_t)given - e + s.row0) : 0;      // (e > row0: between -2^31 and given - 1)
+    s.len = (int32_t)min((int64_t)given, room);
+    s.bad = s.row0 != a || (int64_t)e - a != s.n || s.len != l || (int64_t)e - a > l;
     return s;
 }
 
