@@ -431,7 +431,7 @@ molora_status_t molora_kv_append(const molora_kv_cache_t *cache, const molora_se
  * bits; weights are rounded to 11 bits (22 for fp32) and, below 2^-14 of a row's largest (bf16, heads of 128), to steps of
  * 2^-24 of it; one rounding to dt at the end.
  * Tokens that a row does not see leave no trace in it, whatever their codes; a NaN among the codes of a token makes the rows NaN that do
- * see it. */
+ * see it.  An infinity or a NaN in a row of q makes that row and its lse NaN, if it sees a token. */
 size_t molora_kv_attend_workspace_bytes(molora_dtype_t dt, int32_t heads, int32_t kv_heads, int32_t dim, int64_t max_tokens);
 molora_status_t molora_kv_attend(const molora_kv_cache_t *cache, const molora_sequences_t *seqs, molora_dtype_t dt, int64_t N,
                                  const void *q, int64_t ldq, void *out, int64_t ldo, float *lse, int32_t heads, float scale,

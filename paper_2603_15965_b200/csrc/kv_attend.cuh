@@ -175,6 +175,19 @@ __device__ __forceinline__ void cut_shares(const AttendArgs& a, int64_t first_sh
     __syncthreads();
 }
 
+// The power of two that brings a row of q, of largest magnitude amax (NaN aside), to [2^TOP, 2^(TOP + 1)), and its reciprocal.  A row with an infinity
+// in it becomes NaN throughout, as its softmax is (scores of both signs, or all of them one infinity): 8-bit terms would saturate instead, and a row
+// whose scores are all -infinity would look like one that sees nothing.
+struct RowScale {
+    float up, down;
+};
+template <int TOP>
+__device__ __forceinline__ RowScale row_scale(float amax)
+{
+    const int e = amax > 0.f ? min(100, TOP - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
+    return {amax > 3.402823466e38f ? __int_as_float(0x7FC00000) : __uint_as_float((uint32_t)(e + 127) << 23), __uint_as_float((uint32_t)(127 - e) << 23)};
+}
+
 // A kernel's columns of TMEM, by one warp: after the wait for its predecessor, which may hold them, and before its successor may start.
 __device__ __forceinline__ void take_tmem(uint32_t* base, uint32_t columns)
 {

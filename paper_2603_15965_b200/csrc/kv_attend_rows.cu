@@ -212,10 +212,8 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
             }
             amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
             amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-            // the row's largest element to [2^14, 2^15)
-            const int e = amax > 0.f ? min(100, 14 - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
-            const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-            const float down = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
+            const RowScale by = row_scale<14>(amax);
+            const float up = by.up, down = a.scale_log2 * by.down;
 #pragma unroll
             for (int f = 0; f < HF; ++f)
 #pragma unroll

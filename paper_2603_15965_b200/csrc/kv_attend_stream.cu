@@ -390,11 +390,10 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
 #pragma unroll
                 for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
-                const int e = amax > 0.f ? min(100, 7 - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
-                const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-                if (chunk == 0) rows.factor[r] = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
+                const RowScale by = row_scale<7>(amax);
+                if (chunk == 0) rows.factor[r] = a.scale_log2 * by.down;
 #pragma unroll
-                for (int z = 0; z < 8; ++z) x[z] *= up;
+                for (int z = 0; z < 8; ++z) x[z] *= by.up;
 #pragma unroll
                 for (int z = 0; z < kTermsQ; ++z) {
                     uint2 c;

@@ -304,17 +304,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
 #pragma unroll
                 for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
-                // the row's largest element to [2^14, 2^15)
-                const int e = amax > 0.f ? min(100, 14 - ((int)(__float_as_uint(amax) >> 23) - 127)) : 0;
-                const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+                const RowScale by = row_scale<14>(amax);
                 uint32_t h[4];
 #pragma unroll
                 for (int z = 0; z < 4; ++z) {
-                    const __half2 p = __floats2half2_rn(x[2 * z] * up, x[2 * z + 1] * up);
+                    const __half2 p = __floats2half2_rn(x[2 * z] * by.up, x[2 * z + 1] * by.up);
                     h[z] = *reinterpret_cast<const uint32_t*>(&p);
                 }
                 const int line = (warp & 3) * 32 + half * 16 + 2 * i + (lane >> 4), chunk = lane & 15;
-                if (chunk == 0) s_pair[t][0][line] = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
+                if (chunk == 0) s_pair[t][0][line] = a.scale_log2 * by.down;
                 *reinterpret_cast<uint4*>(q_tile + (chunk >> 3) * (kOperandBytes / 2) + line * 128 + (((chunk ^ line) & 7) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
             }
             pair_sync();
