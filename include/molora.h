@@ -369,7 +369,7 @@ molora_status_t molora_route_hotset(const int32_t *ids, const int32_t *adapter_i
  *   codes   k, v: device e4m3 [n_pages][kv_heads][page][dim], dense, 16-byte aligned
  *   scales  k_scale, v_scale: device fp32 [n_pages][kv_heads], one for each BLOCK of `page` tokens of one head:
  *           value = code * scale.  molora_kv_append writes powers of two; molora_kv_attend takes any positive finite scale
- *           (those of v are read as if clamped to [2^-100, 2^100]).
+ *           (those of v are read as if clamped to [2^-100, 2^90]).
  * page is 16, 32, 64 or 128 tokens, dim 64 or 128, kv_heads >= 1, n_pages * kv_heads * page < 2^31.
  * The sequences of a step:
  *   page_table  device int32 [B][max_pages], row pitch ld_table: token p of sequence b is row p % page of page

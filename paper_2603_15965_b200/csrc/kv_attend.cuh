@@ -195,16 +195,63 @@ __device__ __forceinline__ void take_tmem(uint32_t* base, uint32_t columns)
     ptx::tmem_relinquish();
 }
 
-// scales of v outside [2^-100, 2^100] are read as its ends
-__device__ __forceinline__ float clamped_scale(float v) { return fminf(fmaxf(v, 7.8886090522e-31f), 1.2676506002e30f); }
+// Scales of V, and the softmax's sum.  With s a score in powers of two, vs the scale of its key's block and m the row's reference, a key adds 2^(s - m) to
+// the sum and is handed to the tensor cores with the weight 2^(s - m) vs, which has the size of what it contributes; m goes by the largest
+// weight, the sum goes by the scores alone.  So fp32 has to hold both ends at once: where the reference was set, a weight was 2^5 or more, and its
+// part of the sum 2^5 / vs; no weight is ever above 2^15, and no part above 2^15 / vs.  Scales are read as if they lay in [2^-100, 2^90], times 2^18
+// (taken off the result): parts reach from 2^-103 to 2^97, sums of 2^30 of them stay below 2^128, and what is flushed, below 2^-126, is 2^-23 of
+// its row's sum at most, at the far ends only.  (2^(s - m) as the weight over vs lost whole blocks where scales lay 2^126 apart.)
+constexpr float kVScaleUp = 262144.f, kVScaleDown = 1.f / 262144.f;
+__device__ __forceinline__ float read_v_scale(float v) { return fminf(fmaxf(v, 7.8886090522e-31f), 1.2379400393e27f) * kVScaleUp; }
 
-__device__ __forceinline__ void store4(float* p, float4 v, float f) { *reinterpret_cast<float4*>(p) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f); }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v, float f)
+// 2^d, d <= 0, as half * half: a sum may move between references that lie further apart than one factor can say.  (A factor and a constant that is
+// 2^-120 where d is below: 2 % slower for prompts with heads of 64.)
+struct Shrink {
+    float half;
+    __device__ __forceinline__ explicit Shrink(float d) : half(ex2(0.5f * d)) {}
+    __device__ __forceinline__ float both() const { return half * half; }
+    __device__ __forceinline__ float of(float sum) const { return sum * half * half; }
+};
+
+// two sums, two products, two products and sums in one instruction each
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
 {
-    *reinterpret_cast<uint2*>(p) = make_uint2(f32x2_to_bf16x2(v.x * f, v.y * f), f32x2_to_bf16x2(v.z * f, v.w * f));
+    float2 r;
+    asm("{\n\t.reg .b64 A, B, C;\n\tmov.b64 A, {%2, %3};\n\tmov.b64 B, {%4, %5};\n\tadd.rn.f32x2 C, A, B;\n\tmov.b64 {%0, %1}, C;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 A, B, C;\n\tmov.b64 A, {%2, %3};\n\tmov.b64 B, {%4, %5};\n\tmul.rn.f32x2 C, A, B;\n\tmov.b64 {%0, %1}, C;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 A, B, C, D;\n\tmov.b64 A, {%2, %3};\n\tmov.b64 B, {%4, %5};\n\tmov.b64 C, {%6, %7};\n\tfma.rn.f32x2 D, A, B, C;\n\tmov.b64 {%0, %1}, D;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
 }
 
-// Joins the pieces of the units that are cut: with M the largest reference, the sum of 2^(m - M) (values, sum) over the pieces,
+// four elements of a row's result: values over sum
+__device__ __forceinline__ float4 over(float4 v, float f)
+{
+    return make_float4(v.x * kVScaleDown * f, v.y * kVScaleDown * f, v.z * kVScaleDown * f, v.w * kVScaleDown * f);
+}
+__device__ __forceinline__ void store4(float* p, float4 v, float f) { *reinterpret_cast<float4*>(p) = over(v, f); }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v, float f)
+{
+    const float4 r = over(v, f);
+    *reinterpret_cast<uint2*>(p) = make_uint2(f32x2_to_bf16x2(r.x, r.y), f32x2_to_bf16x2(r.z, r.w));
+}
+
+// Joins the pieces of the units that are cut: with M the largest reference, the sums of 2^(m - M) (values, sum) over the pieces,
 // always in the same order.  A CTA looks after rows of the unit that begins in share blockIdx.x and goes on behind it, four rows at a time.
 // Units of few rows come in many pieces: four rows a CTA, whose warps take every fourth piece each and are added up in order (asked for row by row,
 // the pieces of a unit cut into 55 took 32 us).  Units of many rows come in few: four rows a warp, all of their pieces (four rows a CTA, a chunk's
@@ -253,8 +300,9 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __gr
     for (int p = kAlone ? 0 : warp; p < pieces; p += kAlone ? 1 : kJoinWarps) {
         const float* s = slot(p);
         const float4 m = __ldcg(reinterpret_cast<const float4*>(s)), l = __ldcg(reinterpret_cast<const float4*>(s + ROWS));
-        const float f[kJoinRows] = {ex2(m.x - M[0]), ex2(m.y - M[1]), ex2(m.z - M[2]), ex2(m.w - M[3])};
-        L[0] = fmaf(l.x, f[0], L[0]), L[1] = fmaf(l.y, f[1], L[1]), L[2] = fmaf(l.z, f[2], L[2]), L[3] = fmaf(l.w, f[3], L[3]);
+        const Shrink by[kJoinRows] = {Shrink(m.x - M[0]), Shrink(m.y - M[1]), Shrink(m.z - M[2]), Shrink(m.w - M[3])};
+        const float f[kJoinRows] = {by[0].both(), by[1].both(), by[2].both(), by[3].both()};
+        L[0] += by[0].of(l.x), L[1] += by[1].of(l.y), L[2] += by[2].of(l.z), L[3] += by[3].of(l.w);
 #pragma unroll
         for (int r = 0; r < kJoinRows; ++r)
             if (r < rows && lane < kLanes) {

@@ -17,8 +17,8 @@
 //                 two keys of one element; the weights come into place by movmatrix, and a lane ends with D / 8 neighbouring
 //                 elements of two rows
 // Every e4m3 value is an fp16 value (one cvt for two); q is brought into fp16 by a power of two per row, exactly for bf16, in two
-// terms of 11 bits for fp32.  The scale of a block of K multiplies its scores; that of V is added, as a logarithm, to the exponent, so
-// that the weights handed to the tensor cores have the size of what they contribute, and the sum takes it off again.
+// terms of 11 bits for fp32.  The scale of a block of K multiplies its scores; that of V multiplies its weights once the sum has them
+// (kv_attend.cuh), so that the weights handed to the tensor cores have the size of what they contribute.
 // Weights are at most 2^15 (fp16 normal down to 2^-29 of a row's largest): the reference of a row moves only when a score is
 // 2^8 over the weight it gave its largest, and then everything is rescaled.
 // What bounds it: the codes, 2 D bytes per (key, key / value head), from HBM: 256 sequences of 3 to 4095 tokens, 16 heads over 8 of 64, take 123 us
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
     constexpr int kMT = D / 16;                         // 16-element tiles of the values
     constexpr bool kPairs = Sh::kPairs;
     __shared__ ShareStart s_start;
-    __shared__ float4 s_scales[kWarpsPerCta][kStages][2];  // of a half: scale of K, logarithm and reciprocal of V's, whether its page can be used
+    __shared__ float4 s_scales[kWarpsPerCta][kStages][2];  // of a half: scale of K, logarithm of V's, V's, whether its page can be used
     __shared__ float s_m[kWarpsPerCta][kRows], s_l[kWarpsPerCta][kRows];
     extern __shared__ __align__(16) uint8_t ring_all[];
     ptx::grid_dependency_sync();
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
         const int32_t* table = a.c.table + (int64_t)un.b * a.c.ld_table;
         int group0 = -1;                              // first of the 32 pages whose ids and scales the lanes hold
         int32_t page_id = -1;
-        float page_ks = 0.f, page_lvs = 0.f, page_inv = 0.f;
+        float page_ks = 0.f, page_lvs = 0.f, page_vs = 0.f;
         auto load_pages = [&](int page) {
             group0 = page;
             page_id = -1;
@@ -155,8 +155,8 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
                 } else {
                     const int64_t block = (int64_t)page_id * a.c.kv_heads + head;
                     page_ks = ptx::ld_dependent(a.c.k_scale + block);
-                    const float vs = clamped_scale(ptx::ld_dependent(a.c.v_scale + block));
-                    page_lvs = log2f(vs), page_inv = 1.f / vs;
+                    page_vs = read_v_scale(ptx::ld_dependent(a.c.v_scale + block));
+                    page_lvs = log2f(page_vs);
                 }
             }
         };
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
                 if (group0 < 0 || page >= group0 + 32 || (plog == 4 && page + 1 >= group0 + 32)) load_pages(page);
                 const uint32_t dst = ring_at + (uint32_t)(put * 2 * Sh::kHalfBytes);
                 const int32_t id = __shfl_sync(0xFFFFFFFFu, page_id, page - group0);
-                const float4 sc = make_float4(page_ks, page_lvs, page_inv, page_id >= 0 ? 1.f : 0.f);
+                const float4 sc = make_float4(page_ks, page_lvs, page_vs, page_id >= 0 ? 1.f : 0.f);
                 const int64_t row = (((int64_t)id * a.c.kv_heads + head) << plog) + (key & ((1 << plog) - 1));
                 if (lane == page - group0) s_scales[warp][put][0] = sc;
                 if (id >= 0) copy_half(row, dst);
@@ -325,20 +325,21 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
                             }
                     }
             }
-            // sc: scale of K, logarithm of V's, its reciprocal
+            // sc: scale of K, logarithm of V's, V's
             float c[SUBS][NT][2], top = -INFINITY, y[SUBS][NT][4];
 #pragma unroll
             for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int n = 0; n < NT; ++n) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        c[u][n][i] = fmaxf(rowf[n][i] * sc[u].x, 1.17549435e-38f);      // (never 0: a hidden score is -infinity times it)
-                        const float off = sc[u].y - m[n][i];
-                        y[u][n][i] = fmaf(x[u][n][i], c[u][n][i], off);
-                        y[u][n][2 + i] = fmaf(x[u][n][2 + i], c[u][n][i], off);
-                        top = fmaxf(top, fmaxf(y[u][n][i], y[u][n][2 + i]));
+                    for (int i = 0; i < 2; ++i) c[u][n][i] = fmaxf(rowf[n][i] * sc[u].x, 1.17549435e-38f);      // (never 0: a hidden score is -infinity times it)
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        const float2 z = fma2(make_float2(x[u][n][e], x[u][n][e + 1]), make_float2(c[u][n][0], c[u][n][1]), make_float2(-m[n][0], -m[n][1]));
+                        y[u][n][e] = z.x, y[u][n][e + 1] = z.y;
                     }
+                    top = fmaxf(top, fmaxf(fmaxf(y[u][n][0], y[u][n][1]), fmaxf(y[u][n][2], y[u][n][3])) + sc[u].y);
+                }
             if (__any_sync(0xFFFFFFFFu, top > kTop + 8.f)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
@@ -350,15 +351,16 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
 #pragma unroll
                         for (int z = 4; z < 32; z <<= 1) raw = fmaxf(raw, __shfl_xor_sync(0xFFFFFFFFu, raw, z));
                         const float next = raw - m[n][i] > kTop ? raw - kTop : m[n][i];
-                        const float shrink = ex2(m[n][i] - next);
+                        const Shrink by(m[n][i] - next);
+                        const float shrink = by.both();
                         m[n][i] = next;
-                        l[n][i] *= shrink;
+                        l[n][i] = by.of(l[n][i]);
 #pragma unroll
                         for (int d = 0; d < kMT; ++d) o[n][d][i] *= shrink, o[n][d][2 + i] *= shrink;
 #pragma unroll
                         for (int u = 0; u < SUBS; ++u) {
-                            y[u][n][i] = fmaf(x[u][n][i], c[u][n][i], sc[u].y - next);
-                            y[u][n][2 + i] = fmaf(x[u][n][2 + i], c[u][n][i], sc[u].y - next);
+                            y[u][n][i] = fmaf(x[u][n][i], c[u][n][i], -next);
+                            y[u][n][2 + i] = fmaf(x[u][n][2 + i], c[u][n][i], -next);
                         }
                     }
             }
@@ -369,8 +371,13 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
                 for (int n = 0; n < NT; ++n) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) y[u][n][e] = ex2(y[u][n][e]);
-                    l[n][0] = fmaf(y[u][n][0] + y[u][n][2], sc[u].z, l[n][0]);
-                    l[n][1] = fmaf(y[u][n][1] + y[u][n][3], sc[u].z, l[n][1]);
+                    const float2 sum = add2(make_float2(l[n][0], l[n][1]), add2(make_float2(y[u][n][0], y[u][n][1]), make_float2(y[u][n][2], y[u][n][3])));
+                    l[n][0] = sum.x, l[n][1] = sum.y;
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        const float2 z = mul2(make_float2(y[u][n][e], y[u][n][e + 1]), make_float2(sc[u].z, sc[u].z));
+                        y[u][n][e] = z.x, y[u][n][e + 1] = z.y;
+                    }
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const uint32_t p = pack_f16(y[u][n][2 * j], y[u][n][2 * j + 1]);
@@ -431,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
                 float top = s_m[0][row];
 #pragma unroll
                 for (int z = 1; z < kWarpsPerCta; ++z) top = fmaxf(top, s_m[z][row]);
-                const float f = ex2(m[n][i] - top);
+                const float f = Shrink(m[n][i] - top).both();
                 float r[kVBytes];
 #pragma unroll
                 for (int d = 0; d < kMT; ++d) r[2 * d] = o[n][d][i] * f, r[2 * d + 1] = o[n][d][2 + i] * f;
@@ -452,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas)
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int z = 0; z < kWarpsPerCta; ++z) {
-                sum = fmaf(s_l[z][row], ex2(s_m[z][row] - top), sum);
+                sum += Shrink(s_m[z][row] - top).of(s_l[z][row]);
                 const float4 x = *reinterpret_cast<const float4*>(ring_all + z * kStages * 2 * Sh::kHalfBytes + (row * D + d) * 4);
                 v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
             }

@@ -20,8 +20,8 @@
 //             cache cost more than what they do.
 // (One worker whose groups took alternate units: 196 us against 172 for 256 sequences of 3 to 4095 tokens and two rows, 81 against 68 for 64
 // sequences of 100 to 2043 tokens and 20 rows.)
-// Weights are at most 2^8; the scale of a block of K multiplies its scores, that of V is added to the exponent as a logarithm and taken off
-// the sum again, so that weights have the size of what they contribute.
+// Weights are at most 2^8; the scale of a block of K multiplies its scores, that of V its weights once the sum has them (kv_attend.cuh), so that
+// weights have the size of what they contribute.
 // What bounds it: for few rows 32 KB a tile from HBM (1.06 GB in 166 to 171 us, 6.2 to 6.4 TB/s, 95 to 97 % of a copy's rate); for 20 rows the instructions, 6500 of
 // all warps a tile, at 52 % of the schedulers' slots; for a single short sequence (776 tokens: 10.3 us with the join) the chain of first reads --
 // lengths, page, scales, codes -- and two launches.
@@ -71,8 +71,7 @@ struct Control {
     uint64_t q_full[2], q_ready[2], q_empty[2];
     uint64_t drained;
 };
-// A tile in the ring: the scales of every 16 keys (of K, logarithm and reciprocal of V's, whether their page can be used), and where in its unit it
-// stands.
+// A tile in the ring: the scales of every 16 keys (of K, logarithm of V's, V's, whether their page can be used), and where in its unit it stands.
 struct Tile {
     float4 scale[8];
     int32_t kind;                             // kFirst: begins a unit, kOdd: of an odd one; kLast: no tile, there are no more
@@ -245,8 +244,8 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 }
                 __syncwarp();
                 if (fresh) {
-                    const float v = clamped_scale(vs);
-                    sc = page_id >= 0 ? make_float4(ks, log2f(v), 1.f / v, 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    const float v = read_v_scale(vs);
+                    sc = page_id >= 0 ? make_float4(ks, log2f(v), v, 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
                 const int mine = (page - group0 + (((lane & 7) * 16) >> plog)) & 31;           // the page of 16 keys
                 float4 g;
@@ -455,12 +454,12 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 if (lane == 0) mbar_arrive(bar(&ctrl.s_empty[b]));
                 const int key = key0 + key_lane;
                 const bool border = key0 + kKeys > hi_min || key0 < lo_max;
-                // y: the logarithm of what the key contributes to the row, over the row's reference
-                float c[RPG], e[RPG], top = -INFINITY;
+                // e: the logarithm of the key's part of the row's sum, over the row's reference; with V's, that of its weight
+                float e[RPG], top = -INFINITY;
 #pragma unroll
                 for (int r = 0; r < RPG; ++r) {
-                    c[r] = rows.factor[r0 + r] * sc.x;
-                    e[r] = fmaf(y[r], c[r], sc.y - m[r]);
+                    y[r] *= rows.factor[r0 + r] * sc.x;
+                    e[r] = y[r] - m[r];
                 }
                 const bool hidden = sc.w == 0.f || key >= hi_max || key < lo_min;      // no row sees the key, or its page cannot be used
                 if (border || hidden) {
@@ -486,17 +485,16 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
 #pragma unroll
                     for (int r = 0; r < RPG; ++r) {
                         const bool sees = !hidden && key < rows.upper[r0 + r] && key >= rows.lower[r0 + r];
-                        if (!sees || nan) y[r] = e[r] = sees ? kNan : -INFINITY, c[r] = 1.f;
+                        if (!sees || nan) y[r] = e[r] = sees ? kNan : -INFINITY;
                     }
                 }
 #pragma unroll
                 for (int r = 0; r < RPG; ++r) top = fmaxf(top, e[r]);
-                if (threads_any<128>(1 + all, top > kTop + kSlack)) {
+                if (threads_any<128>(1 + all, top + sc.y > kTop + kSlack)) {
                     float shrink[RPG];
 #pragma unroll
                     for (int r = 0; r < RPG; ++r) {
-                        y[r] = fmaf(y[r], c[r], sc.y);      // (not from e: m may be the reference of a row that has seen nothing)
-                        const float most = warp_max(y[r]);
+                        const float most = warp_max(y[r] + sc.y);
                         if (lane == 0) s_part[all][q4][r] = most;
                     }
                     sync_threads_of<128>(1 + all);
@@ -504,9 +502,10 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                     for (int r = 0; r < RPG; ++r) {
                         const float top = fmaxf(fmaxf(s_part[all][0][r], s_part[all][1][r]), fmaxf(s_part[all][2][r], s_part[all][3][r]));
                         const float next = top - m[r] > kTop ? top - kTop : m[r];
-                        shrink[r] = ex2(m[r] - next);
+                        const Shrink by(m[r] - next);
+                        shrink[r] = by.both();
                         m[r] = next;
-                        l[r] *= shrink[r];
+                        l[r] = by.of(l[r]);
                         e[r] = y[r] - next;
                     }
                     if (i > 0) {                      // what is in O already: the MMAs of the tile before are done, those of this one wait for its weights
@@ -531,9 +530,11 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 uint8_t* const p = smem + (p_at - base) + r0 * 128;
 #pragma unroll
                 for (int r = 0; r < RPG; r += 2) {
-                    const float w0 = ex2(e[r]), w1 = ex2(e[r + 1]);
-                    l[r] = fmaf(w0, sc.z, l[r]), l[r + 1] = fmaf(w1, sc.z, l[r + 1]);
-                    __half2 rest = __floats2half2_rn(w0, w1);
+                    float2 w = make_float2(ex2(e[r]), ex2(e[r + 1]));
+                    const float2 sum = add2(make_float2(l[r], l[r + 1]), w);
+                    l[r] = sum.x, l[r + 1] = sum.y;
+                    w = mul2(w, make_float2(sc.z, sc.z));
+                    __half2 rest = __floats2half2_rn(w.x, w.y);
 #pragma unroll
                     for (int z = 0; z < kTermsP; ++z) {
                         const uint32_t code = __nv_cvt_halfraw2_to_fp8x2(rest, __NV_SATFINITE, __NV_E4M3);
@@ -584,7 +585,7 @@ __global__ void __launch_bounds__(Cfg<ROWS>::kThreads, 1)
                 if (row >= n_rows || !live) continue;
                 const float sum = (s_part[all][0][r] + s_part[all][1][r]) + (s_part[all][2][r] + s_part[all][3][r]);
                 if (at_slot < 0) {
-                    static_cast<__nv_bfloat16*>(a.out)[rows.out[row] + key_lane] = __float2bfloat16(sum == 0.f ? 0.f : __fdividef(o[r], sum));
+                    static_cast<__nv_bfloat16*>(a.out)[rows.out[row] + key_lane] = __float2bfloat16(sum == 0.f ? 0.f : __fdividef(o[r] * kVScaleDown, sum));
                     if (a.lse != nullptr && key_lane == 0) a.lse[rows.lse[row]] = sum == 0.f ? -INFINITY : (m[r] + log2f(sum)) * 0.69314718056f;
                 } else {
                     slot[2 * ROWS + row * kDim + key_lane] = o[r];

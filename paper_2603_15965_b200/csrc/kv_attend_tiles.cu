@@ -52,7 +52,7 @@ constexpr int kUnitReaders = kConvWarp0 + 2;                  // the warps of ro
 
 // A tile of keys in the queue.
 struct KeyTile {
-    float4 scale[8];                           // of 16 keys: scale of K, logarithm and reciprocal of V's, whether their page can be used
+    float4 scale[8];                           // of 16 keys: scale of K, logarithm of V's, V's, whether their page can be used
     int64_t line[8];                           // of 16 keys: the first one's line in the pool, -1: none
     uint32_t nan[4];                           // keys with a NaN among the codes of V, where not every row sees every key
     int32_t key0, hi_max, lo_min;
@@ -170,24 +170,6 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// two sums, two products and sums in one instruction each
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    float2 r;
-    asm("{\n\t.reg .b64 A, B, C;\n\tmov.b64 A, {%2, %3};\n\tmov.b64 B, {%4, %5};\n\tadd.rn.f32x2 C, A, B;\n\tmov.b64 {%0, %1}, C;\n\t}"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    float2 r;
-    asm("{\n\t.reg .b64 A, B, C, D;\n\tmov.b64 A, {%2, %3};\n\tmov.b64 B, {%4, %5};\n\tmov.b64 C, {%6, %7};\n\tfma.rn.f32x2 D, A, B, C;\n\tmov.b64 {%0, %1}, D;\n\t}"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return r;
-}
-
 // 16 codes of element chunk c (of 16) of line r of a [2][128][64] fp16 operand with 128-byte swizzle
 __device__ __forceinline__ void store_codes_f16(uint8_t* operand, int r, int c, uint4 w)
 {
@@ -389,9 +371,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                         s_pair[t][half][row] = top;
                         pair_sync();
                         top = fmaxf(top, s_pair[t][half ^ 1][row]);
-                        const float next = top - m > kTop + kSlack ? top - kTop : m, shrink = ex2(m - next);
+                        const float next = top - m > kTop + kSlack ? top - kTop : m;
+                        const Shrink by(m - next);
+                        const float shrink = by.both();
                         m = next;
-                        l *= shrink;
+                        l = by.of(l);
                         if (i > 0) {
                             wait_bar(bar(&ctrl.o_done[t][b ^ 1]), (uint32_t)((own - 1) >> 1) & 1u, abort_flag, a.dev_status);
                             __syncwarp();
@@ -411,21 +395,22 @@ __global__ void __launch_bounds__(kThreads, 1)
                     // ---- the weights, two to a column, over scores that have been read
                     uint32_t p[16];
                     if (seen) {
+                        float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
                         for (int g = 0; g < 2; ++g) {
-                            const float f = g == 0 ? f0 : f1, off = (g == 0 ? sc0.y : sc1.y) - m;
-                            float2 sum = make_float2(0.f, 0.f);
+                            const float f = g == 0 ? f0 : f1, vs = g == 0 ? sc0.z : sc1.z;
 #pragma unroll
                             for (int z = 0; z < 8; ++z) {
                                 float2 x = make_float2(__uint_as_float(v[16 * g + 2 * z]), __uint_as_float(v[16 * g + 2 * z + 1]));
-                                x = fma2(x, make_float2(f, f), make_float2(off, off));
+                                x = fma2(x, make_float2(f, f), make_float2(-m, -m));
                                 x = make_float2(ex2(x.x), ex2(x.y));
                                 sum = add2(sum, x);
+                                x = mul2(x, make_float2(vs, vs));
                                 const __half2 w2 = __floats2half2_rn(x.x, x.y);
                                 p[8 * g + z] = *reinterpret_cast<const uint32_t*>(&w2);
                             }
-                            l = fmaf(sum.x + sum.y, g == 0 ? sc0.z : sc1.z, l);
                         }
+                        l += sum.x + sum.y;
                     } else {
 #pragma unroll
                         for (int z = 0; z < 16; ++z) p[z] = 0;
@@ -453,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             pair_sync();
             l += s_pair[t][half ^ 1][row];
             const bool whole = slot_at < 0, store = real_was && *abort_flag == 0;       // (nothing of an aborted call is stored)
-            const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+            const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l, down = whole ? kVScaleDown : 1.f;
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + out_was;
             float* slot = slots + max(slot_at, 0) * (int64_t)slot_floats(kUnitRows, kDim);
 #pragma unroll 1
@@ -468,7 +453,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 float x[16];
 #pragma unroll
-                for (int z = 0; z < 16; ++z) x[z] = __uint_as_float(v[z]) * inv;
+                for (int z = 0; z < 16; ++z) x[z] = __uint_as_float(v[z]) * down * inv;
                 if (!store) continue;
                 const int at = half * 64 + g * 16;
                 if (whole) {
@@ -687,8 +672,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
                         } else {
                             const int64_t block = (int64_t)id * a.c.kv_heads + u.head;
-                            const float vs = clamped_scale(ld_dependent(a.c.v_scale + block));
-                            sc = make_float4(ld_dependent(a.c.k_scale + block), log2f(vs), 1.f / vs, 1.f);
+                            const float vs = read_v_scale(ld_dependent(a.c.v_scale + block));
+                            sc = make_float4(ld_dependent(a.c.k_scale + block), log2f(vs), vs, 1.f);
                             line = (block << plog) + (key & ((1 << plog) - 1));
                         }
                     }

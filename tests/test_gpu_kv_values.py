@@ -40,3 +40,48 @@ def test_a_row_that_sees_nothing_is_zero_whatever_its_q(dim, dtype, new):
     p["q"][0], p["q"][1, 2, 5] = math.inf, math.nan
     out, lse = run(p)
     assert bool((out[:2] == 0).all()) and bool((lse[:2] == -math.inf).all()) and bool(out[2:].isfinite().all())
+
+SPREADS = [(80, -80), (-80, 80), (90, -100), (-100, 90), (64, -64), (-64, 64)]
+
+
+@pytest.mark.parametrize("kind", range(len(KINDS)))
+@pytest.mark.parametrize("first,then", SPREADS)
+def test_scales_of_v_far_apart_with_equal_scores(kind, first, then):
+    """Every key has the same weight, whatever the scale of its values."""
+    dim, dtype, heads, kv_heads, new, _ = KINDS[kind]
+    n = new[0]
+    p = problem(130 + kind, new, (n + 255,), heads, kv_heads, dim, 16, dtype)
+    pool, table = p["pool"], p["table"][0].long()
+    pool.k[:] = 0
+    half = len(table) // 2
+    pool.v_scale[table[:half]], pool.v_scale[table[half:]] = 2.0 ** first, 2.0 ** then
+    out, lse = run(p)
+    check(p, out, lse)
+
+
+@pytest.mark.parametrize("kind", range(len(KINDS)))
+@pytest.mark.parametrize("spread", [(-100, 90), (-64, 64)])
+def test_scales_of_v_far_apart_with_scores_and_cut_units(kind, spread):
+    """A long sequence that many shares divide, its pieces in scales of their own, beside a short one."""
+    dim, dtype, heads, kv_heads, new, _ = KINDS[kind]
+    n = new[0]
+    p = problem(140 + kind, (n, 1), (n + 6000, 40), heads, kv_heads, dim, 64, dtype)
+    pool = p["pool"]
+    pool.v_scale[:] = torch.pow(2.0, torch.randint(spread[0], spread[1] + 1, pool.v_scale.shape, generator=p["gen"]).float())
+    long_runs = p["table"][0, :48].long()                                # and runs of pages of one scale, longer than a share
+    pool.v_scale[long_runs[:24]], pool.v_scale[long_runs[24:]] = 2.0 ** spread[0], 2.0 ** spread[1]
+    out, lse = run(p)
+    check(p, out, lse)
+
+
+@pytest.mark.parametrize("kind", range(len(KINDS)))
+def test_scales_of_v_beyond_the_range_count_as_its_ends(kind):
+    dim, dtype, heads, kv_heads, new, lens = KINDS[kind]
+    p = problem(150 + kind, new, lens, heads, kv_heads, dim, 64, dtype)
+    pool = p["pool"]
+    pool.v_scale[::2], pool.v_scale[1::2] = 2.0 ** -100, 2.0 ** 90
+    want = run(p)
+    check(p, *want)
+    pool.v_scale[::2], pool.v_scale[1::2] = 2.0 ** -126, 2.0 ** 120
+    again = run(p)
+    assert torch.equal(want[0], again[0]) and torch.equal(want[1], again[1])
