@@ -374,8 +374,8 @@ molora_status_t molora_route_hotset(const int32_t *ids, const int32_t *adapter_i
  * The sequences of a step:
  *   page_table  device int32 [B][max_pages], row pitch ld_table: token p of sequence b is row p % page of page
  *               page_table[b][p / page]; entries behind a sequence's last token are not read
- *   cu_tokens   device int32 [B + 1], non-decreasing from 0: sequence b's NEW tokens are rows cu_tokens[b] .. cu_tokens[b+1] - 1
- *               of q, k, v; rows from cu_tokens[B] on belong to no sequence and are left as they are
+ *   cu_tokens   device int32 [B + 1], non-decreasing: sequence b's NEW tokens are rows cu_tokens[b] .. cu_tokens[b+1] - 1 of q, k, v;
+ *               rows before cu_tokens[0] (0 as a rule) and from cu_tokens[B] on belong to no sequence and are left as they are
  *   kv_lens     device int32 [B]: tokens of sequence b INCLUDING the new ones, so that its j-th of n new tokens stands at
  *               position kv_lens[b] - n + j
  * Pages outside [0, n_pages), positions below 0 or from max_pages * page (or 2^30) on, and rows from N on never fault: those tokens

@@ -194,7 +194,10 @@ __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_con
             continue;
         }
         const int64_t j = i - sq.row0;
-        if (j < 0) break;                                  // (rows of no sequence: cu does not start at 0)
+        if (j < 0) {                                       // rows of no sequence, in front of the first one's
+            i = sq.row0;
+            continue;
+        }
         const int pos = sq.pos0 + (int)j;
         if (sq.bad && tid == 0 && g == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, MOLORA_DEV_BAD_SEQUENCE);
         if (pos < 0) {                                     // in front of the sequence's beginning: left out

@@ -122,3 +122,27 @@ def test_attention_moves_no_token(cu, lens, causal, window, dim, dtype, heads, k
             continue
         p = dict(q=q[row:row + 1], pool=pool, table=table[b:b + 1], new=(1,), lens=(seen,))
         T.check(p, out[row:row + 1], lse[row:row + 1], causal=True, window=left)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("front", [1, 3, 40])
+@pytest.mark.parametrize("new", [(1, 1, 1), (5, 0, 30), (70, 2, 9)])
+def test_rows_in_front_of_the_first_sequence(front, new, dtype):
+    """A call whose first sequence does not begin with row 0 leaves what the same rows leave as a call of their own."""
+    n = sum(new)
+    p = A.problem(160, new, (10, 0, 25), 4, 2, 64, PAGE, dtype, 64)
+    f, table, lens = p["f"].cuda(), p["table"].cuda(), torch.tensor(p["lens"], dtype=torch.int32).cuda()
+    rows = torch.cat([torch.randn(front, 8, 64).to(p["wide"].dtype), p["wide"]]).cuda()
+    results = []
+    for at, w in ((0, rows[front:].contiguous()), (front, rows)):
+        cache, status = p["pool"].cuda(M), torch.zeros(1, dtype=torch.int32, device="cuda")
+        cu = (R.offsets(new) + at).cuda()
+        q = torch.full((at + n, 4, 64), 7.0, dtype=rows.dtype, device="cuda")
+        M.molora_kv_append(w[:, 4:6], w[:, 6:], cache, table, cu, lens, q=w[:, :4], inv_freq=f, q_out=q, dev_status=status)
+        out, lse = torch.full_like(q, 7.0), torch.full((at + n, 4), 7.0, device="cuda")
+        M.molora_kv_attend(q, cache, table, cu, lens, max_tokens=max(new), out=out, lse=lse, dev_status=status)
+        torch.cuda.synchronize()
+        assert int(status) == 0 and all(bool((t[:at] == 7).all()) for t in (q, out, lse))
+        results.append([q[at:], out[at:], lse[at:], cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.k_scale, cache.v_scale])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
