@@ -404,10 +404,10 @@ typedef struct {
  * older tokens stand in has already; where it grows, their codes are divided by the growth (exact but for values that become subnormal).
  * New codes are rounded to nearest even; infinities saturate, NaN stays NaN.
  * k, v    device [N][kv_heads * dim] of type dt, pitches ldk, ldv (multiples of 8 elements), 16-byte aligned
- * q       device [N][heads * dim], pitch ldq, or NULL (heads then 0); q_out the same with pitch ldqo, may be q itself but may
- *         not overlap it otherwise
+ * q       device [N][heads * dim], pitch ldq, or NULL (heads then 0); q_out the same with pitch ldqo, may be q itself; rows of it that
+ *         overlap rows of q otherwise, or of k or v, are refused (slices of one packed buffer do not overlap)
  * inv_freq  device fp32 [rotary / 2], or NULL if rotary is 0; rotary a multiple of 16, at most dim
- * The pages that a call writes belong to one sequence each (shared ones are copied by the caller first); tokens of a
+ * The pages that a call writes belong to one sequence each, at one place of it (shared ones are copied by the caller first); tokens of a
  * block behind a sequence's new length (drafts that were refused) are overwritten by the next append and count for nothing
  * else than the scale, which never shrinks while the block is in use. */
 molora_status_t molora_kv_append(const molora_kv_cache_t *cache, const molora_sequences_t *seqs, molora_dtype_t dt, int64_t N,
@@ -419,7 +419,8 @@ molora_status_t molora_kv_append(const molora_kv_cache_t *cache, const molora_se
  * query head h, reading key / value head h / (heads / kv_heads):
  *     out = sum_j softmax_j(scale * q . K_j) V_j   over j < kv_lens, j <= p if causal, j > p - window if window > 0
  * Rows that see no token get out = 0 and lse = -infinity.
- * q       device [N][heads * dim] of type dt, pitch ldq; out the same, pitch ldo, not overlapping q; heads a multiple of kv_heads
+ * q       device [N][heads * dim] of type dt, pitch ldq; out the same, pitch ldo, refused where its rows overlap those of q; heads a
+ *         multiple of kv_heads
  * lse     device fp32 [N][heads] or NULL: natural logarithm of the softmax's sum
  * window  0, or (causal only) the number of newest tokens that a row sees, itself included
  * max_tokens  the most new tokens that a sequence of this call has, as far as the caller knows (N, or 0, if it does not; bounds above
@@ -448,7 +449,8 @@ molora_status_t molora_kv_attend(const molora_kv_cache_t *cache, const molora_se
  * draft   device [B][S][V] likewise, or NULL: the drafted tokens are certain (q_i(x_i) = 1, 0 elsewhere)
  * drafted device int32 [B][S];  n_drafted  device int32 [B], each in [0, S] (clamped), or NULL: S for all
  * uniform device fp32 [B][S + 1]: u_0 .. u_{S-1} for the drafts, u_S for the drawn token
- * tokens  device int32 [B][S + 1]: the accepted tokens, the drawn one, then -1;  accepted  device int32 [B]
+ * tokens  device int32 [B][S + 1]: the accepted tokens, the drawn one, then -1;  accepted  device int32 [B]; neither may overlap
+ *         what the call reads
  * 0 <= S <= MOLORA_MAX_DRAFTS, 1 <= V < 2^30.  A drafted token outside [0, V) is refused, a distribution without mass gives
  * token -1; both set MOLORA_DEV_BAD_DRAFT. */
 #define MOLORA_MAX_DRAFTS 31

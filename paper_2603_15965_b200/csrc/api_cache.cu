@@ -1,6 +1,8 @@
 // C ABI of the paged cache and of draft verification: argument validation on the host, then enqueue.
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
+#include <utility>
 
 #include "kv_cache.cuh"
 
@@ -30,6 +32,23 @@ molora_status_t check_rows(const void* p, int64_t ld, int64_t width)
 {
     if (p == nullptr || !aligned16(p) || ld < width) return MOLORA_ERR_INVALID_ARG;
     return ld % 8 == 0 ? MOLORA_OK : MOLORA_ERR_UNSUPPORTED;
+}
+
+// Whether N rows of width_a bytes from pa on, lda bytes apart, share a byte with N rows of width_b bytes from pb on (pitches of at least the widths).
+bool rows_overlap(const void* pa, int64_t lda, int64_t width_a, const void* pb, int64_t ldb, int64_t width_b, int64_t N)
+{
+    const int64_t a = (int64_t)reinterpret_cast<intptr_t>(pa), b = (int64_t)reinterpret_cast<intptr_t>(pb);
+    if (a + (N - 1) * lda + width_a <= b || b + (N - 1) * ldb + width_b <= a) return false;
+    if (N == 1) return true;
+    if (lda == ldb) {                                 // slices of one buffer: row j of b begins r bytes behind the beginning of row j + k of a
+        const int64_t k = (b - a >= 0 ? b - a : b - a - lda + 1) / lda, r = b - a - k * lda;
+        return (r < width_a && std::abs(k) < N) || (r + width_b > lda && std::abs(k + 1) < N);
+    }
+    for (int64_t i = 0; i < N; ++i) {                 // the first row of b that ends behind the beginning of a's row i
+        const int64_t at = a + i * lda, j = at < b + width_b ? 0 : (at - b - width_b) / ldb + 1;
+        if (j < N && b + j * ldb < at + width_a) return true;
+    }
+    return false;
 }
 
 KvView view_of(const molora_kv_cache_t& c, const molora_sequences_t& s)
@@ -82,7 +101,10 @@ molora_status_t molora_kv_append(const molora_kv_cache_t* cache, const molora_se
     if (heads > 0) {
         if (const molora_status_t st = check_rows(q, ldq, (int64_t)heads * cache->dim)) return st;
         if (const molora_status_t st = check_rows(q_out, ldqo, (int64_t)heads * cache->dim)) return st;
-        if (q == q_out && ldq != ldqo) return MOLORA_ERR_INVALID_ARG;
+        const int64_t size = dt == MOLORA_F32 ? 4 : 2, q_bytes = (int64_t)heads * cache->dim * size;
+        if (q == q_out ? ldq != ldqo && N > 1 : rows_overlap(q, ldq * size, q_bytes, q_out, ldqo * size, q_bytes, N)) return MOLORA_ERR_INVALID_ARG;
+        for (const auto& [p, ld] : {std::pair<const void*, int64_t>(k, ldk), std::pair<const void*, int64_t>(v, ldv)})      // (read by other CTAs)
+            if (rows_overlap(p, ld * size, wide * size, q_out, ldqo * size, q_bytes, N)) return MOLORA_ERR_INVALID_ARG;
     }
     return launch_kv_append(view_of(*cache, *seqs), dt, N, k, ldk, v, ldv, q, ldq, q_out, ldqo, heads, inv_freq, rotary, interleaved != 0, dev_status,
                             static_cast<cudaStream_t>(stream));
@@ -108,7 +130,8 @@ molora_status_t molora_kv_attend(const molora_kv_cache_t* cache, const molora_se
     if (N == 0 || seqs->B == 0) return MOLORA_OK;
     if (const molora_status_t st = check_rows(q, ldq, (int64_t)heads * cache->dim)) return st;
     if (const molora_status_t st = check_rows(out, ldo, (int64_t)heads * cache->dim)) return st;
-    if (q == out) return MOLORA_ERR_INVALID_ARG;      // (units read rows of q after others have been written)
+    const int64_t size = dt == MOLORA_F32 ? 4 : 2, row_bytes = (int64_t)heads * cache->dim * size;
+    if (rows_overlap(q, ldq * size, row_bytes, out, ldo * size, row_bytes, N)) return MOLORA_ERR_INVALID_ARG;      // (units read rows of q after others have been written)
     if (max_tokens == 0 || max_tokens > N) max_tokens = N;
     const size_t need = molora_kv_attend_workspace_bytes(dt, heads, cache->kv_heads, cache->dim, max_tokens);
     if (need > 0 && (ws == nullptr || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)) return MOLORA_ERR_WORKSPACE;
