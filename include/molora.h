@@ -396,8 +396,8 @@ typedef struct {
 } molora_sequences_t;
 
 /* Position rotation of q and k, and k and v into the cache, in one launch.  With p the position of a token and
- * w_i = p * inv_freq[i] (product and reduction in 64 bits), i < rotary / 2, the pair (a, b) of a head's elements
- * (i, i + rotary / 2) -- or (2i, 2i + 1) if interleaved -- becomes
+ * w_i = p * inv_freq[i] (product and reduction to half a turn in 64 bits, cosine and sine of that to 2^-23.4), i < rotary / 2, the
+ * pair (a, b) of a head's elements (i, i + rotary / 2) -- or (2i, 2i + 1) if interleaved -- becomes
  *     (a cos w_i - b sin w_i, b cos w_i + a sin w_i);
  * elements from `rotary` on, and all of v, stay.  A block's scale becomes the smallest power of two s with
  * amax <= 448 s over its NEW values (the finite ones; at least 2^-64, at most 2^64), but never less than what a block that

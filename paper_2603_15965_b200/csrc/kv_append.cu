@@ -7,7 +7,7 @@
 //   grid.x   runs of `run` consecutive rows; a CTA takes the pieces (rows of one sequence inside one page) that begin in its run
 //   grid.y   groups of heads of k, of v, of q
 // Sines and cosines are computed once per piece, into shared memory, in turns: p * f / 2 pi in 64 bits, reduced to half a turn, then
-// sinpi / cospi in fp32.  A thread's unit is 16 elements of a row -- two 8-element vectors that the rotation pairs, or that lie side by
+// sinpi / cospi in fp32, turned by what fp32 leaves of the reduced angle.  A thread's unit is 16 elements of a row -- two 8-element vectors that the rotation pairs, or that lie side by
 // side -- and stays the same for every head of the group; the next head's vectors are on their way while a head is worked on (asked
 // for when its turn came, two units a thread, sines in registers: 71 us against 45 for 8192 tokens of 32 + 2 x 8 heads of 128, 185 MB, 4.1 TB/s).
 // What bounds it there: instructions (58 % of the issue slots, conversions and packing above all) and 16 warps per SM; a token each: the chain
@@ -230,8 +230,11 @@ __global__ void __launch_bounds__(kMaxThreads) kv_append_kernel(const __grid_con
             for (int z = tid; z < count * pairs; z += threads) {
                 const int token = z / pairs, w = z - token * pairs;
                 const double angle = (double)(pos + token) * (double)ptx::ld_dependent(a.inv_freq + w) * 0.15915494309189533577;      // 1 / 2 pi
-                float2 t;
-                sincospif((float)((angle - rint(angle)) * 2.0), &t.y, &t.x);
+                const double half_turns = (angle - rint(angle)) * 2.0;
+                const float near = (float)half_turns, rest = (float)(half_turns - (double)near) * 3.14159265f;
+                float sn, cs;
+                sincospif(near, &sn, &cs);
+                const float2 t = make_float2(fmaf(-sn, rest, cs), fmaf(cs, rest, sn));
                 turns[token * pairs + ((((w & 7) >> 1) * (pairs >> 3) + (w >> 3)) << 1) + (w & 1)] = t;
             }
             __syncthreads();
