@@ -428,9 +428,12 @@ molora_status_t molora_kv_append(const molora_kv_cache_t *cache, const molora_se
  * ws, ws_bytes  device scratch of at least molora_kv_attend_workspace_bytes(...) bytes, 256-byte aligned, need not be cleared;
  *         the size never falls as max_tokens grows, so one that was made for a step's most tokens serves calls of fewer;
  *         calls that share it must not overlap on the GPU
- * Scores and sums are fp32; q (its rows scaled by powers of two) and the codes enter the tensor cores exactly, fp32 q in 22
- * bits; weights are rounded to 11 bits (22 for fp32) and, below 2^-14 of a row's largest (bf16, heads of 128), to steps of
- * 2^-24 of it; one rounding to dt at the end.
+ * Scores and sums are fp32.  The codes enter the tensor cores exactly, and so does bf16 q but for elements far below the largest of
+ * their row: in calls of few rows (bf16, heads of 128, 32 rows per key / value head and what else goes that way) those below
+ * 2^-14 of it are off by 2^-22 of it at most, elsewhere those below 2^-31 by 2^-39.  fp32 q enters in 22 bits, below 2^-17 of the
+ * largest in steps of 2^-38 of it.  A weight, a key's part of the softmax times the scale of its block of V, is rounded to 11 bits
+ * (22 for fp32), and far below the row's largest to steps of it: of 2^-24 below 2^-14 (bf16, heads of 128, few rows), of 2^-31
+ * below 2^-21 (other bf16) or 2^-10 (fp32).  The softmax's sum takes the parts before that rounding.  One rounding to dt at the end.
  * Tokens that a row does not see leave no trace in it, whatever their codes; a NaN among the codes of a token makes the rows NaN that do
  * see it.  An infinity or a NaN in a row of q makes that row and its lse NaN, if it sees a token. */
 size_t molora_kv_attend_workspace_bytes(molora_dtype_t dt, int32_t heads, int32_t kv_heads, int32_t dim, int64_t max_tokens);

@@ -72,7 +72,8 @@ int64_t rows_of(int64_t max_tokens, int32_t group) { return std::min(max_tokens,
 // Whether bf16 rows with heads of 128 go to the kernel for few rows, in units of 32: always up to that, and for more where its units find a worker
 // each and read few keys over again -- two units a sequence, or no more than four tiles of 128 keys a worker if every page of the table is in use.
 // (16 new tokens of one sequence, 4 heads a key / value head, behind 20,000: 36 us against 47; 40 behind 460: 19 against 28; 16 of each of 16
-// sequences, 384 units: 44 both; 32 of each, 640 units: 73 against 46.)
+// sequences, 384 units: 44 both; 32 of each, 640 units: 73 against 46.)  The lengths are on the device, so what stands for them is the width of
+// the page table: calls of more than 2 kMaxStreamRows rows with a table much wider than their sequences go to the other kernel.
 bool few_rows(int64_t rows, int64_t N, int32_t group, const molora_kv_cache_t& c, const molora_sequences_t& s)
 {
     if (rows <= kMaxStreamRows) return true;

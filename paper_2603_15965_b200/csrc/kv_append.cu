@@ -9,8 +9,8 @@
 // Sines and cosines are computed once per piece, into shared memory, in turns: p * f / 2 pi in 64 bits, reduced to half a turn, then
 // sinpi / cospi in fp32, turned by what fp32 leaves of the reduced angle.  A thread's unit is 16 elements of a row -- two 8-element vectors that the rotation pairs, or that lie side by
 // side -- and stays the same for every head of the group; the next head's vectors are on their way while a head is worked on (asked
-// for when its turn came, two units a thread, sines in registers: 71 us against 45 for 8192 tokens of 32 + 2 x 8 heads of 128, 185 MB, 4.1 TB/s).
-// What bounds it there: instructions (58 % of the issue slots, conversions and packing above all) and 16 warps per SM; a token each: the chain
+// for when its turn came, two units a thread, sines in registers: 71 us against 45 for 8192 tokens of 32 + 2 x 8 heads of 128, 185 MB; 45.6 now, 4.05 TB/s).
+// What bounds it there: instructions (66 % of the issue slots, conversions and packing above all) and 16 warps per SM; a token each: the chain
 // of dependent reads.
 #include "kv_cache.cuh"
 

@@ -19,11 +19,11 @@
 // Every e4m3 value is an fp16 value (one cvt for two); q is brought into fp16 by a power of two per row, exactly for bf16, in two
 // terms of 11 bits for fp32.  The scale of a block of K multiplies its scores; that of V multiplies its weights once the sum has them
 // (kv_attend.cuh), so that the weights handed to the tensor cores have the size of what they contribute.
-// Weights are at most 2^15 (fp16 normal down to 2^-29 of a row's largest): the reference of a row moves only when a score is
-// 2^8 over the weight it gave its largest, and then everything is rescaled.
-// What bounds it: the codes, 2 D bytes per (key, key / value head), from HBM: 256 sequences of 3 to 4095 tokens, 16 heads over 8 of 64, take 123 us
-// in bf16 and 132 in fp32 (4.3 and 4.0 TB/s), of 128 in fp32 268 us; for prompts the tensor instruction (8 of 1024 tokens, 32 heads of 64: 480 and
-// 717 us), which reaches a quarter of what tcgen05 would give.
+// Weights are at most 2^15: the reference of a row moves only when a score is 2^8 over the weight it gave its largest, 2^7, and then everything
+// is rescaled.  So fp16 has all 11 bits down to 2^-21 of a row's largest weight, and steps of 2^-31 of it below (22 bits down to 2^-10 in two terms).
+// What bounds it: the codes, 2 D bytes per (key, key / value head), from HBM: 256 sequences of 3 to 4095 tokens, 16 heads over 8 of 64, take 122 to 126 us
+// in bf16 and 130 to 136 in fp32 (4.2 and 4.0 TB/s), of 128 in fp32 271 to 286 us; for prompts the tensor instruction (8 of 1024 tokens, 32 heads
+// of 64: 521 and 724 us, of 128 in fp32 1354), which reaches a quarter of what tcgen05 would give.
 #include <algorithm>
 #include <type_traits>
 

@@ -4,7 +4,7 @@
 // memory, tcgen05.mma (kind::f8f6f4) reads them there, and no thread ever touches them.  What is not 8 bits wide is
 // written as a sum of e4m3 terms, each in columns of its own:
 //   q (8 significant bits) = t1 + t2 / 32, exactly: the rest that rounding to 4 bits leaves of 8 fits 4; a power of two per row brings the largest
-//       element to [2^7, 2^8), so elements below 2^-14 of it are off by at most 2^-23 of it
+//       element to [2^7, 2^8), so elements below 2^-14 of it are off by at most 2^-22 of it
 //   a weight, rounded to fp16 (11 bits), = t1 + t2 / 32 + t3 / 1024, exactly (to 2^-20 where a row's largest is 32 or more)
 //   S^T [128 keys x 2 rows]   = K Q^T     A = K tile, keys the 128 lanes of TMEM; B = q's terms
 //   O^T [128 elements x 3 rows] += V^T P^T  A = V tile read across (MN-major); B = the weights' terms
@@ -22,9 +22,9 @@
 // sequences of 100 to 2043 tokens and 20 rows.)
 // Weights are at most 2^8; the scale of a block of K multiplies its scores, that of V its weights once the sum has them (kv_attend.cuh), so that
 // weights have the size of what they contribute.
-// What bounds it: for few rows 32 KB a tile from HBM (1.06 GB in 166 to 171 us, 6.2 to 6.4 TB/s, 95 to 97 % of a copy's rate); for 20 rows the instructions, 6500 of
-// all warps a tile, at 52 % of the schedulers' slots; for a single short sequence (776 tokens: 10.3 us with the join) the chain of first reads --
-// lengths, page, scales, codes -- and two launches.
+// What bounds it: for few rows 32 KB a tile from HBM (1.06 GB in 166 to 170 us, 6.2 to 6.4 TB/s, 95 to 97 % of a copy's rate); for 20 rows the instructions, 6500 of
+// all warps a tile, at 51 % of the schedulers' slots (158 MB in 68 us); for a single short sequence (776 tokens: 10.6 to 11.2 us with the join) the
+// chain of first reads -- lengths, page, scales, codes -- and two launches.
 #include <algorithm>
 
 #include "kv_attend.cuh"

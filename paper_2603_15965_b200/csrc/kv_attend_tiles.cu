@@ -16,9 +16,9 @@
 // The tensor cores work in the order of issue: O, which reads P, is through before S is written in its place.
 // TMEM: S_0 S_1 O_0 O_1, 128 columns each, S for even and odd steps.  Shared memory: Q 64 KB, K and V 2 x 32 KB each.
 // Shares, pieces and the join as in kv_attend.cuh, but with the steps that each tile of rows really sees.
-// What bounds it, measured with 2048 rows of 32 heads behind 14336 tokens (645 us, 0.8 PFLOP/s): no unit alone.  Per 128 keys it takes 5200 cycles,
-// of which the tensor cores are busy 54 %, the special-function units 41 % (256 x 128 exponentials), the schedulers 60 %; taking out the
-// exponentials or seven eighths of the MMAs gains 4 % each, both together with the codes 11 %.  With short prompts (8 of 1024 tokens: 172 us) it
+// What bounds it, measured with 2048 rows of 32 heads behind 14336 tokens (651 to 659 us, 0.8 PFLOP/s): no unit alone.  Per 128 keys it takes 5300
+// cycles, of which the tensor cores are busy 52 %, the special-function units 39 % (256 x 128 exponentials), the schedulers 60 %; taking out the
+// exponentials or seven eighths of the MMAs gained 4 % each, both together with the codes 11 %.  With short prompts (8 of 1024 tokens: 174 us) it
 // is what a unit costs by itself, 13,000 cycles, 5500 of them for q.
 #include "kv_attend.cuh"
 #include "pipeline.cuh"
