@@ -40,8 +40,6 @@ class Step:
         self.draft, self.drafted = torch.zeros(SEQS, drafts, V, device="cuda"), torch.zeros(SEQS, drafts, dtype=torch.int32, device="cuda")
         self.n_drafted, self.uniform = torch.zeros(SEQS, dtype=torch.int32, device="cuda"), torch.zeros(SEQS, drafts + 1, device="cuda")
         self.tokens, self.accepted = torch.zeros(SEQS, drafts + 1, dtype=torch.int32, device="cuda"), torch.zeros(SEQS, dtype=torch.int32, device="cuda")
-        for r in (self.route,):                                          # (first calls set up what is kept per device, which a capture must not)
-            M.molora_group(r, C)
 
     def calls(self):
         h = self.heads
@@ -87,7 +85,7 @@ def _source(s, drafts, seed):
 def test_a_captured_step_serves_every_step(heads, dim, rows, most, steps):
     drafts = 5
     eager, replayed = Step(heads, dim, rows, most, drafts, 3), Step(heads, dim, rows, most, drafts, 3)
-    warm = Step(heads, dim, rows, most, drafts, 3)
+    warm = Step(heads, dim, rows, most, drafts, 3)                       # (first calls set up what is kept per device, which a capture must not)
     warm.calls()
     torch.cuda.synchronize()
     graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()

@@ -101,7 +101,17 @@ def test_append_moves_no_token(cu, lens, dtype):
 @pytest.mark.parametrize("causal,window", [(True, 0), (True, 12), (False, 0)])
 @pytest.mark.parametrize("cu,lens", CALLS + [((0, 40, 56), (ROOM + 21, ROOM + 9)), ((0, 40, 70), (60, 40))])
 def test_attention_moves_no_token(cu, lens, causal, window, dim, dtype, heads, kv_heads):
-    N = min(cu[-1], 56 if cu[1] == 40 else 16)
+    _attention(cu, lens, causal, window, dim, dtype, heads, kv_heads, min(cu[-1], 56 if cu[1] == 40 else 16))
+
+
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 12), (False, 0)])
+@pytest.mark.parametrize("cu,lens", [((0, 700, 1290), (ROOM + 600, ROOM + 9)), ((0, 700, 1400), (ROOM - 5, ROOM + 300)), ((-30, 700, 1290), (2 ** 31 - 1, ROOM + 1))])
+def test_attention_of_prompts_moves_no_token(cu, lens, causal, window):
+    """More units of 32 rows than the kernel for few rows is given."""
+    _attention(cu, lens, causal, window, 128, "bf16", 16, 8, 1290)
+
+
+def _attention(cu, lens, causal, window, dim, dtype, heads, kv_heads, N):
     gen = torch.Generator().manual_seed(8)
     table, pages = R.tables([ROOM, ROOM], PAGE, gen)
     pool = R.Pool(pages, kv_heads, PAGE, dim, gen)

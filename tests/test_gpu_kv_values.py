@@ -10,7 +10,8 @@ pytestmark = pytest.mark.gpu
 
 # dim, type, heads, kv_heads, new tokens, tokens: a few rows, a few that fill a unit, many
 KINDS = [(128, "bf16", 4, 2, (1,), (300,)), (128, "bf16", 4, 2, (9,), (90,)), (128, "bf16", 8, 1, (4,), (700,)), (128, "bf16", 4, 2, (140,), (300,)),
-         (64, "bf16", 4, 2, (9,), (90,)), (64, "f32", 4, 2, (3,), (90,)), (128, "f32", 4, 2, (40,), (90,))]
+         (64, "bf16", 4, 2, (9,), (90,)), (64, "f32", 4, 2, (3,), (90,)), (128, "f32", 4, 2, (40,), (90,)),
+         (128, "bf16", 16, 8, (640,), (700,))]                           # more units of 32 rows than the kernel for few rows is given
 
 
 @pytest.mark.parametrize("kind", range(len(KINDS)))
@@ -34,7 +35,7 @@ def test_a_row_of_q_that_is_not_finite_is_nan(kind, value, one_sign):
 
 
 @pytest.mark.parametrize("dim,dtype", [(128, "bf16"), (64, "bf16"), (128, "f32")])
-@pytest.mark.parametrize("new", [3, 150])
+@pytest.mark.parametrize("new", [3, 150, 2400])
 def test_a_row_that_sees_nothing_is_zero_whatever_its_q(dim, dtype, new):
     p = problem(120, (new,), (new - 2,), 4, 2, dim, 64, dtype)
     p["q"][0], p["q"][1, 2, 5] = math.inf, math.nan
@@ -65,11 +66,13 @@ def test_scales_of_v_far_apart_with_scores_and_cut_units(kind, spread):
     """A long sequence that many shares divide, its pieces in scales of their own, beside a short one."""
     dim, dtype, heads, kv_heads, new, _ = KINDS[kind]
     n = new[0]
-    p = problem(140 + kind, (n, 1), (n + 6000, 40), heads, kv_heads, dim, 64, dtype)
+    length = 12000 if n == 140 else n + (1500 if n > 140 else 6000)      # (140 tokens: so long that they go to the kernel for many rows)
+    p = problem(140 + kind, (n, 1), (length, 40), heads, kv_heads, dim, 64, dtype)
     pool = p["pool"]
     pool.v_scale[:] = torch.pow(2.0, torch.randint(spread[0], spread[1] + 1, pool.v_scale.shape, generator=p["gen"]).float())
-    long_runs = p["table"][0, :48].long()                                # and runs of pages of one scale, longer than a share
-    pool.v_scale[long_runs[:24]], pool.v_scale[long_runs[24:]] = 2.0 ** spread[0], 2.0 ** spread[1]
+    long_runs = p["table"][0, :min(48, length // 64 // 2 * 2)].long()                                # and runs of pages of one scale, longer than a share
+    half = len(long_runs) // 2
+    pool.v_scale[long_runs[:half]], pool.v_scale[long_runs[half:]] = 2.0 ** spread[0], 2.0 ** spread[1]
     out, lse = run(p)
     check(p, out, lse)
 
